@@ -341,6 +341,123 @@ pcg_status pcg_verify_thinning(const void *target_logits, const void *draft_logi
                                int32_t *out_trials, void *workspace, size_t workspace_bytes, pcg_stream stream,
                                const pcg_event *stage_events);
 
+/*
+ * The rest of a decoding round: the paged key/value cache of the sequences being verified, and the attention over it.
+ *
+ * A round feeds every sequence its last token and its drafted tokens (K + 1 rows), attends from those rows to all that
+ * is cached, and verifies the drafts with the logits that come of it.  pcg_cache_plan turns the accept lengths that
+ * pcg_verify left on the device into the next round's lengths, block tables, slots and positions; pcg_cache_append
+ * writes a layer's new keys and values to the slots; pcg_cache_attention is the attention of the new rows over the
+ * cache; pcg_prompt_attention is the causal attention of whole prompts that no cache is read for.
+ *
+ * A cache is a pool of n_blocks blocks of block_size tokens.  Keys and values of one layer are two dense arrays
+ *     [n_blocks, kv_heads, block_size, head_dim]
+ * so that one head's tokens of a block are one contiguous run.  Slot s is row s % block_size of block s / block_size.
+ * A sequence's token at position p lies in block block_table[b, p / block_size], row p % block_size.
+ */
+typedef struct {
+    int32_t n_blocks;   /* blocks in the pool; n_blocks * block_size < 2^31 */
+    int32_t block_size; /* tokens of a block: 16, 32, 64, 128 or 256 */
+    int32_t kv_heads;   /* 1 .. 1024 */
+    int32_t head_dim;   /* a multiple of 8, 8 .. 256 */
+    pcg_dtype dtype;
+    void *k, *v;        /* 16-byte aligned, [n_blocks, kv_heads, block_size, head_dim] each */
+} pcg_cache;
+
+/* Bits of out_flags[b] written by pcg_cache_plan.  A flagged sequence gets no block and no slot in this plan. */
+#define PCG_FLAG_NO_BLOCKS 16 /* it and the sequences before it that need blocks ask for more than the ring holds */
+#define PCG_FLAG_TOO_LONG 32  /* its tokens would need more than max_blocks blocks */
+#define PCG_FLAG_NO_ROWS 64   /* its new tokens end behind the last of `rows` rows */
+
+/*
+ * Lengths, block tables, slots and positions of the next round, from lengths that are on the device.
+ *
+ * For sequence b:
+ *   new_len[b] < 0: it has finished.  Its held[b] blocks go to the free ring's tail, in the order of (b, table entry);
+ *     its outputs are 0.
+ *   otherwise  c = cached_len[b] + accept_len[b] + 1 tokens stay cached (c = cached_len[b] where accept_len is NULL):
+ *     of the last round's chunk its first token and its accepted drafts; accept_len[b] = -1 says that there was no
+ *     such round.  n = new_len[b] tokens follow them, at positions c .. c + n - 1, in rows row_start[b] ..
+ *     row_start[b] + n - 1 of the round's packed rows.  The block table keeps its first held[b] entries; entries
+ *     held[b] .. ceil((c + n) / block_size) - 1 are filled with blocks from the ring's head, sequence by sequence.
+ *     Blocks that a shorter sequence no longer needs stay with it.
+ *   denied (out_flags): PCG_FLAG_NO_ROWS, else PCG_FLAG_TOO_LONG, else PCG_FLAG_NO_BLOCKS (its blocks and those of the
+ *     sequences before it are more than the ring holds; one that needs no block is never denied for this).  It takes
+ *     no block; its rows have slot and position -1, its out_kv_len is 0 (pcg_cache_attention then gives zero rows),
+ *     its out_cached_len is c: it can be planned again, with accept_len[b] = -1.  Rows are counted for it all the same.
+ *
+ *   cached_len, accept_len (or NULL), new_len, held   [B]
+ *   block_table  [B, max_blocks], in and out: only the entries named above are written
+ *   free_ring    [ring_size], in and out: block ids; the free ones are the ring_state[1] entries from ring_state[0]
+ *                on, cyclically.  Released blocks are written behind them (they are not handed out by the same call).
+ *                ring_size >= n_blocks, so that the ring holds every block; entries beyond that are dropped.
+ *   rows         capacity of the packed rows (the host's bound for the sum of the new lengths)
+ *   out_cached_len = c, out_kv_len = c + n, out_held  [B];  out_row_start [B + 1], entries at most `rows`
+ *   out_slots    [rows], out_positions [rows] or NULL; rows behind the last sequence are -1
+ *   out_ring_state [2], the ring's next head and count;  out_flags [B] or NULL
+ * Outputs may not overlap inputs (a caller keeps two sets of lengths and swaps them), so a call that is repeated
+ * with the same inputs gives the same outputs.  Negative cached_len, and held outside 0 .. max_blocks, are clamped.
+ * One launch; no workspace.  B = 0 is allowed.
+ * Errors: INVALID_ARG (null, negative sizes, ring_size or max_blocks < 1, bad block_size, memory that is not the
+ * current device's), UNSUPPORTED (B > 16384), CUDA.
+ */
+pcg_status pcg_cache_plan(int32_t B, const int32_t *cached_len, const int32_t *accept_len, const int32_t *new_len,
+                          const int32_t *held, int32_t block_size, int32_t max_blocks, int32_t *block_table,
+                          int32_t *free_ring, int32_t ring_size, const int32_t *ring_state, int32_t rows,
+                          int32_t *out_cached_len, int32_t *out_kv_len, int32_t *out_held, int32_t *out_row_start,
+                          int32_t *out_slots, int32_t *out_positions, int32_t *out_ring_state, int32_t *out_flags,
+                          pcg_stream stream);
+
+/*
+ * Write the keys and values of `rows` tokens to their slots.
+ *   k, v   [rows, kv_heads, head_dim] of the cache's type; token r at k + r * k_stride elements, its heads dense.
+ *          16-byte aligned, strides a multiple of 16 bytes and at least kv_heads * head_dim elements
+ *   slots  [rows]; a slot outside the cache (a negative one) is skipped.  Two rows with one slot leave that slot
+ *          with values of either.
+ * Nothing else of the cache is written.  rows = 0 is a no-op.  Errors: INVALID_ARG, CUDA.
+ */
+pcg_status pcg_cache_append(const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t rows,
+                            const int32_t *slots, const pcg_cache *cache, pcg_stream stream);
+
+/* Bytes of workspace that the two attention calls need (256-byte aligned base required). Never 0. */
+size_t pcg_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t kv_heads, int32_t head_dim, pcg_dtype dtype);
+
+/*
+ * Attention of packed rows over a paged cache, causal inside each sequence's new rows:
+ *     out[r, h] = sum_{p < lim} softmax_{p < lim}(scale * q[r, h] . k[p, g]) v[p, g],   g = h / (q_heads / kv_heads)
+ * Sequence b's rows are row_start[b] .. row_start[b+1] - 1; with n of them, row i has lim = kv_len[b] - n + i + 1:
+ * the new tokens' keys and values are in the cache already, behind what was cached before.  A row with lim <= 0 is 0.
+ *
+ *   q          [rows, q_heads, head_dim] of the cache's type, token r at q + r * q_stride elements (16-byte aligned,
+ *              stride a multiple of 16 bytes and at least q_heads * head_dim elements)
+ *   row_start  [B + 1], kv_len [B], block_table [B, max_blocks]; kv_len is clamped to 0 .. max_blocks * block_size
+ *   out        [rows, q_heads, head_dim], dense, 16-byte aligned; rows outside every sequence are left as they were
+ *   scale      > 0, finite
+ *   workspace  >= pcg_attention_workspace_bytes(...), contents irrelevant on entry; calls that share one must not
+ *              overlap on the device
+ * What the cache holds behind a sequence's last token, and block table entries behind its last block, are not used.
+ * A used entry outside 0 .. n_blocks - 1 stands for a block of zeros.  Scores, the softmax and the sums are kept in 32
+ * bits; of the 16-bit types, head dimensions 64 and 128 run on the tensor cores, where the weights are rounded to the
+ * type before they meet the values.  Values of tokens that a sequence does attend to have to be finite there: a row
+ * also comes out NaN where a value of a LATER token of its own chunk is infinite or NaN.
+ * Results are bit-identical from run to run.
+ * Errors: INVALID_ARG, UNSUPPORTED (q_heads / kv_heads > 128, B > 16384), WORKSPACE, CUDA.
+ */
+pcg_status pcg_cache_attention(const void *q, int64_t q_stride, int32_t rows, int32_t q_heads,
+                               const int32_t *row_start, const int32_t *kv_len, const int32_t *block_table, int32_t B,
+                               int32_t max_blocks, const pcg_cache *cache, float scale, void *out, void *workspace,
+                               size_t workspace_bytes, pcg_stream stream);
+
+/*
+ * Causal attention of whole prompts, packed one after the other: pcg_cache_attention where every sequence's keys and
+ * values are the rows of k and v themselves (lim = i + 1) and no cache is read.
+ *   q [rows, q_heads, head_dim], k and v [rows, kv_heads, head_dim] of `dtype`, strides and alignment as above
+ */
+pcg_status pcg_prompt_attention(const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *v,
+                                int64_t v_stride, pcg_dtype dtype, int32_t rows, int32_t q_heads, int32_t kv_heads,
+                                int32_t head_dim, const int32_t *row_start, int32_t B, float scale, void *out,
+                                void *workspace, size_t workspace_bytes, pcg_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import numpy as np
 
@@ -18,6 +18,7 @@ from . import build as _build
 
 PCG_F32, PCG_BF16, PCG_F16 = 0, 1, 2
 FLAG_BAD_DRAFT_TOKEN, FLAG_ZERO_RESIDUAL, FLAG_NONFINITE, FLAG_THINNING_EXHAUSTED = 1, 2, 4, 8
+FLAG_NO_BLOCKS, FLAG_TOO_LONG, FLAG_NO_ROWS = 16, 32, 64
 VERIFY_DEFAULT, VERIFY_DENSE, VERIFY_CLUSTER_TERMINAL, VERIFY_BATCHED_TERMINAL = 0, 1, 2, 4
 STATUS_NAMES = {0: "PCG_OK", 1: "PCG_ERR_INVALID_ARG", 2: "PCG_ERR_INVALID_GROUPS", 3: "PCG_ERR_UNSUPPORTED",
                 4: "PCG_ERR_WORKSPACE", 5: "PCG_ERR_CUDA"}
@@ -27,6 +28,7 @@ EXPORTS = [
     "pcg_groups_set_accept_bias",
     "pcg_group_probs", "pcg_group_probs_workspace_bytes", "pcg_group_probs_ws", "pcg_verify_workspace_bytes", "pcg_verify", "pcg_verify_host_arena_bytes", "pcg_verify_host",
     "pcg_verify_static", "pcg_verify_thinning_workspace_bytes", "pcg_verify_thinning", "pcg_asg_create", "pcg_asg_info", "pcg_asg_csr", "pcg_asg_destroy",
+    "pcg_cache_plan", "pcg_cache_append", "pcg_attention_workspace_bytes", "pcg_cache_attention", "pcg_prompt_attention",
 ]
 
 
@@ -52,6 +54,23 @@ class AsgInfo(ctypes.Structure):
     _fields_ = [("V", ctypes.c_int32), ("M", ctypes.c_int32), ("nnz", ctypes.c_int64),
                 ("max_group_size", ctypes.c_int32), ("max_degree", ctypes.c_int32),
                 ("similarity_ms", ctypes.c_float), ("total_ms", ctypes.c_float), ("tensor_path", ctypes.c_int32)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class CachePlan(NamedTuple):
+    """What ``pcg_cache_plan`` writes (int32 CUDA tensors), beside the block table and the free ring."""
+    cached_len: object  # [B]
+    kv_len: object  # [B]
+    held: object  # [B]
+    row_start: object  # [B + 1]
+    slots: object  # [rows]
+    positions: object  # [rows]
+    ring_state: object  # [2]
+    flags: object  # [B]
 
 
 _lib = None
@@ -108,6 +127,16 @@ def load(build_if_missing: bool = True):
     lib.pcg_asg_info.argtypes, lib.pcg_asg_info.restype = [vp, ctypes.POINTER(AsgInfo)], ctypes.c_int
     lib.pcg_asg_csr.argtypes, lib.pcg_asg_csr.restype = [vp, ctypes.POINTER(_Csr)], ctypes.c_int
     lib.pcg_asg_destroy.argtypes, lib.pcg_asg_destroy.restype = [vp], None
+    cache = ctypes.POINTER(_Cache)
+    lib.pcg_cache_plan.argtypes = [i32, vp, vp, vp, vp, i32, i32, vp, vp, i32, vp, i32] + [vp] * 9
+    lib.pcg_cache_plan.restype = ctypes.c_int
+    lib.pcg_cache_append.argtypes, lib.pcg_cache_append.restype = [vp, i64, vp, i64, i32, vp, cache, vp], ctypes.c_int
+    lib.pcg_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, ctypes.c_int]
+    lib.pcg_attention_workspace_bytes.restype = sz
+    lib.pcg_cache_attention.argtypes = [vp, i64, i32, i32, vp, vp, vp, i32, i32, cache, f32, vp, vp, sz, vp]
+    lib.pcg_cache_attention.restype = ctypes.c_int
+    lib.pcg_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, ctypes.c_int, i32, i32, i32, i32, vp, i32, f32, vp, vp, sz, vp]
+    lib.pcg_prompt_attention.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -398,3 +427,152 @@ class Asg:
             self.close()
         except Exception:
             pass
+
+
+# ---- the paged key/value cache of a decoding round ---------------------------------------------------------
+def _need(ok: bool, text: str):
+    if not ok:
+        raise ValueError(text)
+
+
+def _check_here(*tensors):
+    """CUDA tensors of the current device: the library launches there."""
+    import torch
+
+    here = None
+    for t in tensors:
+        if t is None:
+            continue
+        if here is None and t.is_cuda:
+            here = torch.cuda.current_device()
+        if here is None or t.get_device() != here:
+            raise ValueError(f"expected CUDA tensors of the current device, got one on {t.device}")
+
+
+def _check_ints(n: int, *tensors):
+    import torch
+
+    for t in tensors:
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous()):
+            raise ValueError(f"expected a contiguous int32 tensor [{n}], got {t.dtype} {tuple(t.shape)}")
+
+
+def _row_stride(t, name: str) -> int:
+    """Elements between the tokens of [rows, heads, d] whose heads are dense (a slice of a fused projection is)."""
+    _need(t.dim() == 3, f"{name} must be [rows, heads, head_dim]")
+    n, h, d = t.shape
+    s = t.stride()
+    _need((s[2] == 1 or d == 1) and (s[1] == d or h == 1), f"{name}: a token's heads must be dense")
+    return s[0] if n > 1 else h * d
+
+
+def _cache_struct(k_cache, v_cache) -> _Cache:
+    _need(k_cache.dim() == 4 and k_cache.shape == v_cache.shape and k_cache.dtype == v_cache.dtype
+          and k_cache.is_contiguous() and v_cache.is_contiguous(),
+          "k_cache and v_cache must be contiguous [n_blocks, kv_heads, block_size, head_dim] of one type")
+    n, h, bs, d = k_cache.shape
+    return _Cache(n, bs, h, d, dtype_code(k_cache), k_cache.data_ptr(), v_cache.data_ptr())
+
+
+def pcg_cache_plan(cached_len, new_len, held, block_table, free_ring, ring_state, block_size: int, rows: int,
+                   accept_len=None, out: Optional[CachePlan] = None, stream=None) -> CachePlan:
+    """``pcg_cache_plan``: the next round's lengths, blocks, slots and positions, from lengths on the device.
+
+    ``accept_len`` is what ``pcg_verify`` returned for the last round (None: every cached token stays).  Writes new
+    entries of ``block_table`` [B, max_blocks] and released blocks of ``free_ring`` in place; everything else comes
+    back in a ``CachePlan`` (``out`` optionally supplies it; its tensors may not be those of the inputs)."""
+    import torch
+
+    B = cached_len.shape[0]
+    _check_ints(B, cached_len, new_len, held, accept_len)
+    _check_ints(2, ring_state)
+    _check_ints(free_ring.shape[0], free_ring)
+    _need(block_table.dim() == 2 and block_table.shape[0] == B and block_table.dtype == torch.int32
+          and block_table.is_contiguous(), "block_table must be a contiguous int32 tensor [B, max_blocks]")
+    if out is None:
+        sizes = (B, B, B, B + 1, rows, rows, 2, B)
+        out = CachePlan(*torch.empty(sum(sizes), dtype=torch.int32, device=cached_len.device).split(sizes))
+    else:
+        _check_ints(B, out.cached_len, out.kv_len, out.held, out.flags)
+        _check_ints(B + 1, out.row_start)
+        _check_ints(rows, out.slots, out.positions)
+        _check_ints(2, out.ring_state)
+    _check_here(cached_len, new_len, held, accept_len, block_table, free_ring, ring_state, *out)
+    _check(load().pcg_cache_plan(B, cached_len.data_ptr(), None if accept_len is None else accept_len.data_ptr(),
+                                 new_len.data_ptr(), held.data_ptr(), block_size, block_table.shape[1],
+                                 block_table.data_ptr(), free_ring.data_ptr(), free_ring.shape[0], ring_state.data_ptr(),
+                                 rows, *(None if t is None else t.data_ptr() for t in out), _stream_ptr(stream)))
+    return out
+
+
+def pcg_cache_append(k, v, slots, k_cache, v_cache, stream=None):
+    """``pcg_cache_append``: the keys and values [rows, kv_heads, head_dim] of new tokens into the cache's slots."""
+    cache = _cache_struct(k_cache, v_cache)
+    rows = k.shape[0]
+    ks, vs = _row_stride(k, "k"), _row_stride(v, "v")
+    _need(k.shape == v.shape and k.shape[1:] == (cache.kv_heads, cache.head_dim) and k.dtype == v.dtype == k_cache.dtype,
+          "k and v must be [rows, kv_heads, head_dim] of the cache's type")
+    _check_ints(rows, slots)
+    _check_here(k, v, slots, k_cache, v_cache)
+    _check(load().pcg_cache_append(k.data_ptr(), ks, v.data_ptr(), vs, rows, slots.data_ptr(), ctypes.byref(cache),
+                                   _stream_ptr(stream)))
+    return k_cache, v_cache
+
+
+def pcg_attention_workspace_bytes(B: int, q_heads: int, kv_heads: int, head_dim: int, dtype: int) -> int:
+    return int(load().pcg_attention_workspace_bytes(B, q_heads, kv_heads, head_dim, dtype))
+
+
+def _attention_buffers(q, row_start, kv_heads, out, workspace):
+    import torch
+
+    rows, q_heads, d = q.shape
+    B = row_start.shape[0] - 1
+    _check_ints(max(B, 0) + 1, row_start)
+    if out is None:
+        out = torch.empty((rows, q_heads, d), dtype=q.dtype, device=q.device)
+    else:
+        _need(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "out must be contiguous, of q's shape and type")
+    if workspace is None:
+        need = pcg_attention_workspace_bytes(B, q_heads, kv_heads, d, dtype_code(q))
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    return B, out, workspace
+
+
+def pcg_cache_attention(q, row_start, kv_len, block_table, k_cache, v_cache, scale: Optional[float] = None, out=None,
+                        workspace=None, stream=None):
+    """``pcg_cache_attention``: q [rows, q_heads, head_dim], the packed new rows of B sequences whose keys and values
+    are in the cache already, over each sequence's ``kv_len`` cached tokens, causal among the new rows.
+
+    ``scale`` defaults to 1 / sqrt(head_dim).  ``workspace`` is a uint8 CUDA tensor of at least
+    ``pcg_attention_workspace_bytes`` bytes (allocated here if omitted)."""
+    import torch
+
+    cache = _cache_struct(k_cache, v_cache)
+    stride = _row_stride(q, "q")
+    _need(q.shape[2] == cache.head_dim and q.dtype == k_cache.dtype, "q must have the cache's head_dim and type")
+    B, out, workspace = _attention_buffers(q, row_start, cache.kv_heads, out, workspace)
+    _check_ints(B, kv_len)
+    _need(block_table.dim() == 2 and block_table.shape[0] == B and block_table.dtype == torch.int32
+          and block_table.is_contiguous(), "block_table must be a contiguous int32 tensor [B, max_blocks]")
+    _check_here(q, row_start, kv_len, block_table, k_cache, v_cache, out, workspace)
+    _check(load().pcg_cache_attention(q.data_ptr(), stride, q.shape[0], q.shape[1], row_start.data_ptr(), kv_len.data_ptr(),
+                                      block_table.data_ptr(), B, block_table.shape[1], ctypes.byref(cache),
+                                      q.shape[2] ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
+                                      workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return out
+
+
+def pcg_prompt_attention(q, k, v, row_start, scale: Optional[float] = None, out=None, workspace=None, stream=None):
+    """``pcg_prompt_attention``: causal attention of whole prompts packed one after the other; q [rows, q_heads,
+    head_dim], k and v [rows, kv_heads, head_dim] (slices of a fused projection will do), row_start [B + 1]."""
+    qs, ks, vs = _row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v")
+    _need(k.shape == v.shape and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2] and q.dtype == k.dtype == v.dtype,
+          "k and v must be [rows, kv_heads, head_dim] with q's rows, head_dim and type")
+    B, out, workspace = _attention_buffers(q, row_start, k.shape[1], out, workspace)
+    _check_here(q, k, v, row_start, out, workspace)
+    _check(load().pcg_prompt_attention(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dtype_code(q), q.shape[0],
+                                       q.shape[1], k.shape[1], q.shape[2], row_start.data_ptr(), B,
+                                       q.shape[2] ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
+                                       workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    return out
