@@ -6,19 +6,9 @@
 
 #include <cmath>
 
-#include "pcg_cache.cuh"
+#include "pcg_attention.cuh"
 
 namespace pcg {
-
-struct AttnArgs {
-    const void *q, *k, *v;  // k, v: the cache's arrays, or the packed rows
-    void *out;
-    const int32_t *row_start, *kv_len, *block_table;  // kv_len null: the packed rows are the keys
-    int64_t q_stride, k_stride, v_stride;  // elements between tokens (k, v: packed rows only)
-    int32_t rows, B, q_heads, kv_heads, d;
-    int32_t max_blocks, n_blocks, bs_shift;
-    float scale_log2;
-};
 
 // Rounding a float to the element type (nearest even), once.
 template <typename T>
@@ -35,17 +25,6 @@ template <>
 struct Narrow<f16_t> {
     static __device__ __forceinline__ void store(f16_t *p, float x) { p->bits = __half_as_ushort(__float2half_rn(x)); }
 };
-
-// Rows of sequence b, cut to the packed rows whatever row_start holds, and the keys that its last row may see.
-__device__ __forceinline__ void attn_sequence(const AttnArgs &a, int b, int &begin, int &n, int &len) {
-    begin = min(max(a.row_start[b], 0), a.rows);
-    n = max(min(a.row_start[b + 1], a.rows) - begin, 0);
-    len = n;
-    if (a.kv_len) {
-        const int64_t room = (int64_t)a.max_blocks << a.bs_shift;
-        len = (int)min((int64_t)max(a.kv_len[b], 0), room);
-    }
-}
 
 // ---------------------------------------------------------------------------------------------- any type and head size
 // One block per (row, query head): its eight warps take keys 32 at a time in turn, a lane scores one key (16-byte loads,
@@ -173,8 +152,6 @@ void launch_simple(const AttnArgs &a, cudaStream_t s) {
         attention_simple_kernel<T, 8><<<grid, kSimpleThreads, 0, s>>>(a);
 }
 
-constexpr int kAttnMaxB = 16384, kAttnMaxGroup = 128;
-
 pcg_status run_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, size_t workspace_bytes,
                          cudaStream_t stream) {
     const size_t need = pcg_attention_workspace_bytes(a.B, a.q_heads, a.kv_heads, a.d, dtype);
@@ -184,6 +161,7 @@ pcg_status run_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, vo
     }
     pcg_status st = check_here(who, a.out);
     if (st != PCG_OK) return st;
+    if (attention_tc_takes(a.d, dtype)) return attention_tc(who, a, dtype, workspace, stream);
     PCG_DISPATCH_DTYPE(dtype, launch_simple<LogitT>(a, stream));
     cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
@@ -216,7 +194,7 @@ using namespace pcg;
 
 extern "C" size_t pcg_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                                                 pcg_dtype dtype) {
-    return 256;
+    return attention_tc_takes(head_dim, dtype) ? attention_tc_workspace_bytes(B, head_dim) : 256;
 }
 
 extern "C" pcg_status pcg_cache_attention(const void *q, int64_t q_stride, int32_t rows, int32_t q_heads,

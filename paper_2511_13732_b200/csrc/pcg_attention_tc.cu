@@ -1,0 +1,882 @@
+// Attention on the 5th-generation tensor cores: bfloat16 and float16, head dimensions 64 and 128.
+//
+// The rows of one key head -- G = q_heads / kv_heads query heads for each of a sequence's new tokens -- are packed
+// token by token into tiles of 128 rows (TQ = 128 / G tokens), so that a key or value is fetched once for the heads that
+// share it and a drafted chunk's few tokens fill as much of a tile as there is.  An ITEM is a (sequence, key head, pair of
+// row tiles); it meets its keys 128 at a time (a KEY TILE).  A block works on an item with two SLOTS, each a warpgroup
+// with its own scores and its own output accumulator in tensor memory:
+//   two row tiles (chunks of prompts):      slot s has row tile s, and every key tile goes to both;
+//   one row tile (tokens, drafted chunks):  both slots have that row tile and take the key tiles in turn, so that one
+//                                           slot's softmax runs under the other's products; their sums meet at the end.
+//
+// attention_schedule_kernel  numbers all (item, key tile) units of the call and cuts the numbers into one equal run per
+//                            block, whatever the lengths are: no block waits for another, and an item may be shared.
+// attention_tc_kernel        a block's run of units: 8 softmax warps (two slots), a warp that fetches (TMA), a warp that
+//                            issues tcgen05.mma.  An item that a block has to itself is written out; a part of one goes
+//                            to the workspace as an unscaled sum with its reference and its sum of weights.
+// attention_combine_kernel   joins the parts of items that were shared, in the order of the blocks.
+//
+// Tensor memory: scores S0, S1 (128 columns each, fp32), outputs O0, O1 (D columns each, fp32).  The weights of a tile
+// replace the scores they come from, packed to 16 bits in the first 64 columns, and are the A operand of the product with
+// the values straight from there.  The next scores of a slot are issued behind that product by the same thread: the
+// tensor pipe runs a block's products in the order of their issue, so the weights have been read by then, and the
+// barrier that announces the new scores also says that the product before them is complete.
+#include <cuda.h>  // CUtensorMap and its enums only; the encoder is fetched through the runtime, not linked
+#include <cuda_bf16.h>
+
+#include "pcg_attention.cuh"
+
+namespace pcg {
+
+constexpr int kTile = 128;       // rows of a row tile = lanes of tensor memory; keys of a key tile
+constexpr int kMaxBlocks = 148;  // blocks of the main kernel: one per SM of a B200 (more or fewer SMs only change the pace)
+constexpr int kSoftmaxWarps = 8;
+constexpr int kThreads = 32 * (kSoftmaxWarps + 4);  // a warpgroup of fetch, products and two idle warps behind them
+// Registers are launched as 168 a thread (384 * 168 = 64512) and then moved to the softmax warps, whose threads hold a
+// row of 128 scores: 256 * 216 + 128 * 64 = 63488.
+constexpr int kRegsSoftmax = 216, kRegsOther = 64;
+constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
+
+// ---------------------------------------------------------------------------------------------- workspace
+struct Run {       // one block's units
+    int64_t first;  // number of its first unit
+    int32_t b, h, pair, tile;  // where that is
+    int32_t count;  // units
+    int32_t pad;
+};
+struct WorkspaceHead {
+    int32_t error;  // set when a bounded wait ran out: the call's outputs are then NaN
+    int32_t pad[63];
+    Run run[kMaxBlocks + 1];
+};
+// Partial sums: [block][2: a part that does not begin its item, one that does][2 * 128 rows], D sums each stored
+// [D][256] so that a warp's 32 rows are adjacent, then reference and sum of weights.
+constexpr int kPartRows = 2 * kTile;
+template <int D>
+__host__ __device__ constexpr size_t part_floats() {
+    return (size_t)kPartRows * (D + 2);
+}
+constexpr size_t kHeadBytes = (sizeof(WorkspaceHead) + 255) / 256 * 256;
+
+__device__ __forceinline__ float *part_base(void *ws, int block, int which, int D) {
+    return reinterpret_cast<float *>((char *)ws + kHeadBytes) + ((size_t)block * 2 + which) * kPartRows * (D + 2);
+}
+
+// ---------------------------------------------------------------------------------------------- items
+struct Shape {
+    int G, TQ;  // query heads per key head, tokens of a row tile
+};
+__host__ __device__ __forceinline__ int pairs_of(int n, int TQ) { return (n + 2 * TQ - 1) / (2 * TQ); }
+// Key tiles of pair p: up to what its last row sees, and one where it sees nothing.
+__device__ __forceinline__ int tiles_of(int n, int len, int TQ, int p) {
+    const int lim = len - n + min((p + 1) * 2 * TQ, n);
+    return lim <= kTile ? 1 : (lim + kTile - 1) / kTile;
+}
+
+// Sum over 0 <= i < n of floor((a i + b) / m), a, b >= 0 (Euclid's steps on a and m).
+__device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+    int64_t s = 0;
+    while (n > 0) {
+        if (a >= m) {
+            s += n * (n - 1) / 2 * (a / m);
+            a %= m;
+        }
+        if (b >= m) {
+            s += n * (b / m);
+            b %= m;
+        }
+        const int64_t y = a * n + b;
+        if (y < m) break;
+        n = y / m;
+        b = y % m;
+        const int64_t t = a;
+        a = m;
+        m = t;
+    }
+    return s;
+}
+// Key tiles of a sequence's first p pairs.
+__device__ int64_t tiles_before(int n, int len, int TQ, int p) {
+    const int whole = n / (2 * TQ), q = min(p, whole);  // pairs of 2 * TQ tokens
+    // pairs whose last row sees at most one tile of keys count 1 each: (i + 1) * 2 TQ <= 128 - (len - n)
+    const int64_t base = (int64_t)len - n, step = 2 * TQ;
+    const int64_t head = base >= kTile ? 0 : min((int64_t)q, (kTile - base) / step);
+    int64_t s = head;
+    s += floor_sum(q - head, kTile, step, base + (head + 1) * step + kTile - 1);
+    if (p > whole) s += tiles_of(n, len, TQ, whole);
+    return s;
+}
+
+// ---------------------------------------------------------------------------------------------- schedule
+constexpr int kScheduleThreads = 1024;
+
+// One block.  Thread t sums the units of a run of sequences, a scan numbers them, and then thread c finds where block c's
+// run begins: by bisection over the sequences, then over the pairs of one.
+__global__ void __launch_bounds__(kScheduleThreads) attention_schedule_kernel(const __grid_constant__ AttnArgs a, WorkspaceHead *ws) {
+    extern __shared__ int64_t before[];  // [B + 1] units of the sequences before b
+    __shared__ int64_t scratch[kScheduleThreads / 32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
+    const int per = (a.B + kScheduleThreads - 1) / kScheduleThreads, lo = min(a.B, tid * per), hi = min(a.B, lo + per);
+    auto units_of = [&](int b) -> int64_t {
+        int begin, n, len;
+        attn_sequence(a, b, begin, n, len);
+        return n == 0 ? 0 : tiles_before(n, len, TQ, pairs_of(n, TQ)) * a.kv_heads;
+    };
+    int64_t sum = 0;
+    for (int b = lo; b < hi; ++b) {
+        before[b] = sum;
+        sum += units_of(b);
+    }
+    int64_t inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += up;
+    }
+    if (lane == 31) scratch[warp] = inc;
+    __syncthreads();
+    int64_t base = inc - sum, total = 0;
+    for (int w = 0; w < kScheduleThreads / 32; ++w) {
+        if (w < warp) base += scratch[w];
+        total += scratch[w];
+    }
+    for (int b = lo; b < hi; ++b) before[b] += base;
+    if (tid == 0) before[a.B] = total;
+    __syncthreads();
+    if (tid == 0) ws->error = 0;
+    if (tid > kMaxBlocks) return;
+    const int blocks = (int)min((int64_t)kMaxBlocks, max(total, (int64_t)1));
+    const int64_t u = tid >= blocks ? total : total / blocks * tid + total % blocks * tid / blocks;
+    const int64_t next = tid + 1 >= blocks ? total : total / blocks * (tid + 1) + total % blocks * (tid + 1) / blocks;
+    Run r{u, 0, 0, 0, 0, (int32_t)(next - u), 0};
+    if (u < total) {
+        int x = 0, y = a.B - 1;  // the last sequence whose units begin at or before u: empty ones share their number
+        while (x < y) {
+            const int mid = (x + y + 1) >> 1;
+            if (before[mid] <= u)
+                x = mid;
+            else
+                y = mid - 1;
+        }
+        int begin, n, len;
+        attn_sequence(a, x, begin, n, len);
+        const int pairs = pairs_of(n, TQ);
+        const int64_t per_head = tiles_before(n, len, TQ, pairs), in = u - before[x];
+        const int64_t rest = in % per_head;
+        int p = 0, q = pairs - 1;
+        while (p < q) {
+            const int mid = (p + q + 1) >> 1;
+            if (tiles_before(n, len, TQ, mid) <= rest)
+                p = mid;
+            else
+                q = mid - 1;
+        }
+        r.b = x;
+        r.h = (int)(in / per_head);
+        r.pair = p;
+        r.tile = (int)(rest - tiles_before(n, len, TQ, p));
+    }
+    ws->run[tid] = r;
+}
+
+// A block's run of units, item by item: the same walk in every role.
+struct Segment {
+    int b, h, pair, begin, n, len;
+    int tiles, t0, nt;  // key tiles of the item, the first of this part, how many
+    bool two;           // two row tiles
+};
+struct Walk {
+    int b, h, pair, tile, left;
+    int begin, n, len;
+    __device__ __forceinline__ void start(const AttnArgs &a, const Run &r) {
+        b = r.b;
+        h = r.h;
+        pair = r.pair;
+        tile = r.tile;
+        left = r.count;
+        if (left > 0) attn_sequence(a, b, begin, n, len);
+    }
+    __device__ __forceinline__ bool next(const AttnArgs &a, int TQ, Segment &s) {
+        if (left <= 0) return false;
+        s.b = b;
+        s.h = h;
+        s.pair = pair;
+        s.begin = begin;
+        s.n = n;
+        s.len = len;
+        s.tiles = tiles_of(n, len, TQ, pair);
+        s.t0 = tile;
+        s.nt = min(left, s.tiles - tile);
+        s.two = n - pair * 2 * TQ > TQ;
+        left -= s.nt;
+        tile = 0;
+        if (left > 0 && ++pair == pairs_of(n, TQ)) {
+            pair = 0;
+            if (++h == a.kv_heads) {
+                h = 0;
+                do {
+                    ++b;
+                    attn_sequence(a, b, begin, n, len);
+                } while (n == 0);  // units are left, so a sequence with rows follows
+            }
+        }
+        return true;
+    }
+};
+
+// ---------------------------------------------------------------------------------------------- device primitives
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// Bounded wait for a phase of an mbarrier: false = gave up, or another role has.  A poll suspends the thread for up to
+// about a microsecond, so the limit is some seconds at most and some tens of milliseconds at least.
+constexpr uint32_t kPolls = 1u << 21;
+__device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity), "r"(1000u)
+        : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed) {
+    for (uint32_t i = 0; i < kPolls; ++i) {
+        if (bar_poll(bar, parity)) return true;
+        if (*failed) return false;
+    }
+    *failed = 1;
+    return false;
+}
+// The same without a look at the failure flag: what is in flight is waited for after a failure too.
+__device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+    for (uint32_t i = 0; i < kPolls; ++i)
+        if (bar_poll(bar, parity)) return;
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Arrives when all products that this thread has issued are complete.
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+        : "memory");
+}
+// Operand descriptors, 128-byte swizzle (layout type 2 at bit 61, version 1 at bit 46); byte offsets >> 4.
+// K-major (queries and keys: rows of 64 head dimensions, 128 bytes): groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// MN-major (values: rows are keys, the product's inner index; 64 head dimensions a row): blocks of 64 head dimensions
+// 128 * 128 bytes apart (leading offset), groups of 8 keys 1024 bytes apart (stride offset).
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)((kTile * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+        : "memory");
+}
+#define PCG_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define PCG_W8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// 32 columns of the warp's 32 lanes; the caller waits (tmem_wait_ld / _st)
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : PCG_R8(v, 0), PCG_R8(v, 8), PCG_R8(v, 16), PCG_R8(v, 24)
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t *v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        PCG_W8(v, 0), PCG_W8(v, 8), PCG_W8(v, 16), PCG_W8(v, 24)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t *v) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : PCG_R8(v, 0), PCG_R8(v, 8)
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+        PCG_W8(v, 0), PCG_W8(v, 8)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    uint32_t r;
+    if (BF16)
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// ---------------------------------------------------------------------------------------------- main kernel
+template <int D>
+struct Sizes {
+    static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
+    static constexpr int kStages = D == 128 ? 5 : 10;        // ring of key and value tiles: 160 KB
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;  // room to start on a 1024-byte boundary
+};
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kThreads, 1)
+    attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap qmap,
+                        const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap, void *ws) {
+    constexpr int S = Sizes<D>::kStages, kParts = D / 64, kTileBytes = Sizes<D>::kTileBytes;
+    // instruction descriptors: D = fp32, A and B of one 16-bit type, M = 128; N = 128 keys, B K-major; N = D, B MN-major
+    constexpr uint32_t kType = BF16 ? (1u << 7) | (1u << 10) : 0u;
+    constexpr uint32_t kIdescQK = (1u << 4) | kType | ((kTile >> 3) << 17) | ((kTile >> 4) << 24);
+    constexpr uint32_t kIdescPV = (1u << 4) | kType | (1u << 16) | ((D >> 3) << 17) | ((kTile >> 4) << 24);
+    // float16's weights are kept 2^7 higher than the reference says, out of the range where they lose bits: 2^8 above the
+    // reference is then 2^15 at most.  The sums carry the same factor, so it cancels.
+    constexpr float kLift = BF16 ? 0.f : 7.f;
+
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * S + 16];
+    __shared__ float other_m[kTile], other_l[kTile];  // slot 1's, for the end of an item with one row tile
+    __shared__ uint32_t tmem_slot;
+    __shared__ int failed_flag;
+    volatile int *failed = &failed_flag;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = smem_u32(bars);
+    const uint32_t qbuf = base, ring = base + 2 * kTileBytes;
+    auto full_bar = [&](int s) { return bar0 + 8u * s; };         // a stage has landed
+    auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };  // a stage has been read
+    const uint32_t q_full = bar0 + 8u * (2 * S), q_empty = q_full + 8, drain = q_full + 16;
+    auto s_full = [&](int s) { return q_full + 24u + 8u * s; };   // a slot's scores are complete
+    auto p_full = [&](int s) { return q_full + 40u + 8u * s; };   // ... its weights are in place
+    auto o_full = [&](int s) { return q_full + 56u + 8u * s; };   // ... its last product is complete
+    const uint32_t merge_full = q_full + 72, merge_done = q_full + 80;  // slot 1's reference and sum are handed over, read
+
+    if (tid == 0) {
+        for (int i = 0; i < 2 * S + 12; ++i) {
+            // by warps: the weights of a slot (4), the hand-over (4 and 4); by one thread or the hardware: all others
+            const uint32_t bar = bar0 + 8u * i;
+            const uint32_t count = bar == p_full(0) || bar == p_full(1) || bar == merge_full || bar == merge_done ? 4 : 1;
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        failed_flag = 0;
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = tmem_slot;
+    auto s_col = [&](int s) { return tmem + (uint32_t)(s * kTile); };
+    auto o_col = [&](int s) { return tmem + (uint32_t)(2 * kTile + s * D); };
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
+    Walk walk;
+    walk.start(a, reinterpret_cast<const WorkspaceHead *>(ws)->run[blockIdx.x]);
+    Segment g;
+    if (warp < kSoftmaxWarps)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    else
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+
+    if (warp < kSoftmaxWarps) {
+        // ------------------------------------------------------------------ softmax: thread = row of the slot's row tile
+        const int slot = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const uint32_t sc = s_col(slot) + lanes, oc = o_col(slot) + lanes;
+        const int tok = row / G, head = row - tok * G;
+        uint32_t sn = 0, on = 0, on_other = 0, mn = 0;  // phases met so far
+        uint32_t loads = 0;                             // stages filled so far
+        bool ok = true;
+        while (ok && walk.next(a, TQ, g)) {
+            const int t_row = g.pair * 2 * TQ + (g.two ? slot * TQ : 0) + tok;  // the row's token in its sequence
+            const bool valid = tok < TQ && t_row < g.n;
+            const int lim = valid ? g.len - g.n + t_row + 1 : 0x7fffffff;  // padding rows never ask for masking
+            const bool warp_valid = __any_sync(0xffffffffu, valid);
+            const int first = g.two ? 0 : slot, step = g.two ? 1 : 2;
+            float m = kNegInf, l = 0.f;
+            for (int t = first; t < g.nt; t += step, ++sn) {
+                ok = __all_sync(0xffffffffu, bar_wait(s_full(slot), sn & 1, failed));
+                if (!ok) break;
+                fence_after();
+                const int k0 = (g.t0 + t) * kTile;
+                if (t == g.nt - 1 && k0 + kTile > g.len && (!g.two || slot == 0)) {
+                    // Values behind the sequence's last token may hold anything, and 0 * NaN is NaN: they are zeroed
+                    // where they lie.  This stage is the last of the part; the slot's weights are announced after it, and
+                    // slot 1's product comes behind slot 0's.
+                    const uint32_t i = loads + 2 * g.nt - 1;
+                    ok = __all_sync(0xffffffffu, bar_wait(full_bar(i % S), (i / S) & 1, failed));
+                    if (!ok) break;
+                    if (k0 + row >= g.len) {
+                        const uint32_t at = ring + (i % S) * kTileBytes + row * 128;
+#pragma unroll
+                        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                            for (int c = 0; c < 8; ++c)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + part * (kTile * 128) + c * 16), "r"(0u)
+                                             : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                if (warp_valid) {
+                    uint32_t v[kTile];
+#pragma unroll
+                    for (int c = 0; c < kTile; c += 32) tmem_ld32(sc + c, v + c);
+                    tmem_wait_ld();
+                    if (__any_sync(0xffffffffu, lim < k0 + kTile)) {
+#pragma unroll
+                        for (int c = 0; c < kTile; ++c)
+                            if (k0 + c >= lim) v[c] = __float_as_uint(kNegInf);
+                    }
+                    float top[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+#pragma unroll
+                    for (int c = 0; c < kTile; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(v[c]));
+                    const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                    // also when the first score above -inf is met; a row's reference depends on its own scores alone, and
+                    // padding rows, whose scores are arbitrary, have none
+                    const bool move = valid && mt > m + kSlack;
+                    if (__any_sync(0xffffffffu, move)) {
+                        const float mnew = move ? mt : m, f = move ? ex2(m - mt) : 1.f;
+                        l *= f;
+                        if (t > first) {
+#pragma unroll
+                            for (int c = 0; c < D; c += 16) {
+                                uint32_t o[16];
+                                tmem_ld16(oc + c, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tmem_st16(oc + c, o);
+                            }
+                        }
+                        m = mnew;
+                    }
+                    // a row that has met no score above -inf yet weighs everything 0
+                    const float shift = (m == kNegInf ? 0.f : -m) + kLift;
+                    float part[4] = {0.f, 0.f, 0.f, 0.f};
+                    uint32_t p[32];
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2) {
+                            const float x = ex2(fmaf(__uint_as_float(v[half * 64 + c]), a.scale_log2, shift));
+                            const float y = ex2(fmaf(__uint_as_float(v[half * 64 + c + 1]), a.scale_log2, shift));
+                            part[c & 2] += x;
+                            part[(c & 2) + 1] += y;
+                            p[c / 2] = pack2<BF16>(x, y);
+                        }
+                        tmem_st32(sc + half * 32, p);
+                    }
+                    l += (part[0] + part[1]) + (part[2] + part[3]);
+                    tmem_wait_st();
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full(slot));
+            }
+            if (!ok) break;
+            loads += 2 * g.nt;
+            // ---- end of the part
+            const bool mine = first < g.nt;                    // this slot has had a key tile
+            const bool shared = !g.two && g.nt > 1;            // both have, of one row tile
+            if (mine) ok = __all_sync(0xffffffffu, bar_wait(o_full(slot), on++ & 1, failed));
+            if (!ok) break;
+            if (shared) {
+                if (slot == 1) {
+                    other_m[row] = m;
+                    other_l[row] = l;
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(merge_full);
+                    ok = __all_sync(0xffffffffu, bar_wait(merge_done, mn++ & 1, failed));  // slot 0 has read this slot's sums
+                    continue;
+                }
+                ok = __all_sync(0xffffffffu, bar_wait(o_full(1), on_other++ & 1, failed)) &&
+                     __all_sync(0xffffffffu, bar_wait(merge_full, mn++ & 1, failed));
+                if (!ok) break;
+            } else if (g.two) {
+                ++on_other;
+            }
+            if (!mine) continue;
+            fence_after();
+            if (warp_valid) {
+                float f0 = 1.f, f1 = 0.f;
+                if (shared) {
+                    const float m1 = other_m[row], l1 = other_l[row], mx = fmaxf(m, m1);
+                    f0 = m == mx ? 1.f : ex2(m - mx);  // equal, or both -inf: nothing to scale
+                    f1 = m1 == mx ? 1.f : ex2(m1 - mx);
+                    l = l * f0 + l1 * f1;
+                    m = mx;
+                }
+                const bool whole = g.t0 == 0 && g.nt == g.tiles;
+                // a row that sees no key has weights of 0 alone; one that sees scores of -inf alone ends as 0 / 0 = NaN
+                const float inv = lim <= 0 ? 0.f : 1.f / l;
+                char *out = (char *)a.out + (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2);
+                const int prow = (g.two ? slot * kTile : 0) + row;
+                float *part = part_base(ws, blockIdx.x, g.t0 == 0 ? 1 : 0, D);
+#pragma unroll
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(oc + c, o);
+                    tmem_wait_ld();
+                    if (shared) {
+                        uint32_t o1[32];
+                        tmem_ld32(o_col(1) + lanes + c, o1);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+                    }
+                    if (valid && whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            uint32_t w[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                w[j] = lim <= 0 ? 0u
+                                                : pack2<BF16>(__uint_as_float(o[i + 2 * j]) * inv, __uint_as_float(o[i + 2 * j + 1]) * inv);
+                            *reinterpret_cast<uint4 *>(out + (c + i) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    } else if (valid) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) part[(size_t)(c + i) * kPartRows + prow] = __uint_as_float(o[i]);
+                    }
+                    __syncwarp();  // the next columns are read by the whole warp
+                }
+                if (valid && !whole) {
+                    part[(size_t)D * kPartRows + prow] = m;
+                    part[(size_t)(D + 1) * kPartRows + prow] = l;
+                }
+            }
+            fence_before();
+            if (shared) {
+                __syncwarp();
+                if (lane == 0) bar_arrive(merge_done);
+            }
+        }
+    } else if (warp == kSoftmaxWarps) {
+        // ------------------------------------------------------------------ fetch: one lane per page and 64 dimensions
+        const bool paged = a.kv_len != nullptr;
+        const int box = paged ? min(1 << a.bs_shift, kTile) : kTile;  // rows of one copy
+        const int copies = kTile / box;
+        const int my_row = (lane % copies) * box, my_part = lane / copies;  // at most 8 * 2 lanes have a copy
+        uint32_t it = 0, items = 0;
+        bool ok = true;
+        while (ok && walk.next(a, TQ, g)) {
+            auto page_of = [&](int t) -> int32_t {  // the block of this lane's rows of key tile t
+                const int p = (g.t0 + t) * kTile + my_row;
+                if (!paged || my_part >= kParts || t >= g.nt || p >= g.len) return -1;
+                const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
+                return block < 0 || block >= a.n_blocks ? a.n_blocks : block;  // behind the tensor: reads zeros
+            };
+            auto fetch = [&](const CUtensorMap *map, int t, int32_t page) -> bool {
+                const int s = it % S;
+                if (it >= S && !__all_sync(0xffffffffu, bar_wait(empty_bar(s), ((it / S) - 1) & 1, failed))) return false;
+                const int k0 = (g.t0 + t) * kTile;
+                // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
+                const int n_copies = paged ? min(copies, (max(g.len - k0, 0) + box - 1) / box) : 1;
+                if (lane == 0) bar_expect(full_bar(s), n_copies * box * D * 2);
+                __syncwarp();
+                if (my_part < kParts && my_row < n_copies * box) {
+                    const uint32_t dst = ring + s * kTileBytes + my_part * (kTile * 128) + my_row * 128;
+                    if (paged)
+                        tma_load(dst, map, my_part * 64, (k0 + my_row) & ((1 << a.bs_shift) - 1), g.h, page, full_bar(s));
+                    else
+                        tma_load(dst, map, my_part * 64, g.h, g.begin + k0, 0, full_bar(s));
+                }
+                ++it;
+                return true;
+            };
+            // the queries: G heads of TQ tokens at a time, which is the row tile's order
+            if (items > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (items - 1) & 1, failed));
+            if (!ok) break;
+            ++items;
+            if (lane == 0) {
+                const int tiles = g.two ? 2 : 1;
+                bar_expect(q_full, tiles * kParts * G * TQ * 128);
+                for (int r = 0; r < tiles; ++r)
+                    for (int part = 0; part < kParts; ++part)
+                        tma_load(qbuf + r * kTileBytes + part * (kTile * 128), &qmap, part * 64, 0, g.h,
+                                 g.begin + (g.pair * 2 + r) * TQ, q_full);
+            }
+            __syncwarp();
+            // keys lead by the number of slots that a key tile does not go to both of
+            const int ahead = g.two ? 1 : 2;
+            int32_t page0 = page_of(0), page1 = page_of(1), page2 = page_of(2);  // blocks of the tiles t .. t + 2
+            ok = fetch(&kmap, 0, page0);
+            if (ok && ahead == 2 && g.nt > 1) ok = fetch(&kmap, 1, page1);
+            for (int t = 0; ok && t < g.nt; ++t) {
+                const int32_t page3 = page_of(t + 3);  // its latency passes under the waits
+                ok = fetch(&vmap, t, page0);
+                if (ok && t + ahead < g.nt) ok = fetch(&kmap, t + ahead, ahead == 2 ? page2 : page1);
+                page0 = page1;
+                page1 = page2;
+                page2 = page3;
+            }
+        }
+        if (*failed) {  // giving up: copies already asked for may still be landing
+            if (items > 0) bar_drain(q_full, (items - 1) & 1);
+            for (uint32_t back = 1; back <= S && back <= it; ++back) bar_drain(full_bar((it - back) % S), ((it - back) / S) & 1);
+        }
+    } else if (warp == kSoftmaxWarps + 1 && lane == 0) {
+        // ------------------------------------------------------------------ products: one thread
+        uint32_t it = 0, items = 0, pn0 = 0, pn1 = 0;  // pn: phases of a slot's weights
+        bool ok = true;
+        auto wait_stage = [&](uint32_t i) { return bar_wait(full_bar(i % S), (i / S) & 1, failed); };
+        auto scores = [&](int slot, int rows, uint32_t i) {
+            const uint32_t q = qbuf + rows * kTileBytes, k = ring + (i % S) * kTileBytes;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t off = (kk >> 2) * (kTile * 128) + (kk & 3) * 32;
+                mma_ss(s_col(slot), desc_k(q + off), desc_k(k + off), kIdescQK, kk > 0);
+            }
+            mma_commit(s_full(slot));
+        };
+        while (ok && walk.next(a, TQ, g)) {
+            ok = bar_wait(q_full, items & 1, failed);
+            ++items;
+            const int ahead = g.two ? 1 : 2;
+            for (int t = 0; ok && t < min(ahead, g.nt); ++t, ++it) {
+                ok = wait_stage(it);
+                if (!ok) break;
+                fence_after();
+                if (g.two) {
+                    scores(0, 0, it);
+                    scores(1, 1, it);
+                } else {
+                    scores(t, 0, it);
+                }
+                mma_commit(empty_bar(it % S));
+                if (t == g.nt - 1) mma_commit(q_empty);
+            }
+            for (int t = 0; ok && t < g.nt; ++t) {
+                const uint32_t vi = it++;
+                const bool more = t + ahead < g.nt;
+                const uint32_t ki = it;
+                if (more) ++it;
+                ok = wait_stage(vi);
+                for (int r = 0; ok && r < (g.two ? 2 : 1); ++r) {
+                    const int slot = g.two ? r : t & 1;
+                    ok = bar_wait(p_full(slot), (slot ? pn1++ : pn0++) & 1, failed);
+                    if (!ok) break;
+                    fence_after();
+                    const uint32_t v = ring + (vi % S) * kTileBytes;
+                    const bool begun = t >= (g.two ? 1 : 2);
+#pragma unroll
+                    for (int kk = 0; kk < kTile / 16; ++kk)
+                        mma_ts(o_col(slot), s_col(slot) + kk * 8, desc_mn(v + kk * 2048), kIdescPV, begun || kk > 0);
+                    if (!g.two || r == 1) mma_commit(empty_bar(vi % S));
+                    if (more) {
+                        if (r == 0) ok = wait_stage(ki);
+                        if (!ok) break;
+                        fence_after();
+                        scores(slot, g.two ? r : 0, ki);
+                        if (!g.two || r == 1) {
+                            mma_commit(empty_bar(ki % S));
+                            if (t + ahead == g.nt - 1) mma_commit(q_empty);
+                        }
+                    } else {
+                        mma_commit(o_full(slot));
+                    }
+                }
+            }
+        }
+        if (*failed) {  // products already issued may still be writing tensor memory: it is freed when they have retired
+            mma_commit(drain);
+            bar_drain(drain, 0);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (tid == 0 && failed_flag) atomicMax(&reinterpret_cast<WorkspaceHead *>(ws)->error, 1);
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+}
+
+// ---------------------------------------------------------------------------------------------- combine
+// Block (c, y): the item that block c of the main kernel began and did not end, if there is one; 32 rows at a time,
+// thread = row (lane) and D / 8 head dimensions (warp).
+constexpr int kCombineThreads = 256, kCombineRows = 4;
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(const __grid_constant__ AttnArgs a, void *ws) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;");
+    const WorkspaceHead *head = reinterpret_cast<const WorkspaceHead *>(ws);
+    const int tid = threadIdx.x, lane = tid & 31, dims = (tid >> 5) * (D / 8);
+    if (head->error) {  // a wait ran out: no row may pass for a result
+        const uint32_t nan2 = 0x7fff7fffu;  // NaN in both types
+        const int64_t vecs = (int64_t)a.rows * a.q_heads * (D / 8);
+        for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kCombineThreads + tid; i < vecs;
+             i += (int64_t)gridDim.x * gridDim.y * kCombineThreads)
+            reinterpret_cast<uint4 *>(a.out)[i] = make_uint4(nan2, nan2, nan2, nan2);
+        return;
+    }
+    const int c = blockIdx.x;
+    const Run next = head->run[c + 1];
+    if (next.tile == 0 || next.count == 0 || next.first - next.tile < head->run[c].first) return;
+    const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
+    int begin, n, len;
+    attn_sequence(a, next.b, begin, n, len);
+    const int64_t end = next.first - next.tile + tiles_of(n, len, TQ, next.pair);
+    int last = c + 1;  // the block that ends the item
+    while (last + 1 < kMaxBlocks && head->run[last + 1].first < end) ++last;
+    const int tokens = min(n - next.pair * 2 * TQ, 2 * TQ);
+    const int rows = tokens > TQ ? kPartRows : kTile;
+    for (int r0 = blockIdx.y * 32; r0 < rows; r0 += 32 * kCombineRows) {
+        const int r = r0 + lane, in = r & (kTile - 1);
+        const int tok = (r / kTile) * TQ + in / G;
+        if (in / G >= TQ || tok >= tokens) continue;
+        float m = kNegInf;
+        for (int k = c; k <= last; ++k) m = fmaxf(m, part_base(ws, k, k == c, D)[(size_t)D * kPartRows + r]);
+        float l = 0.f, o[D / 8];
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) o[i] = 0.f;
+        for (int k = c; k <= last; ++k) {
+            const float *p = part_base(ws, k, k == c, D);
+            const float mk = p[(size_t)D * kPartRows + r];
+            const float f = mk == kNegInf ? 0.f : mk == m ? 1.f : ex2(mk - m);
+            l += p[(size_t)(D + 1) * kPartRows + r] * f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i) o[i] += p[(size_t)(dims + i) * kPartRows + r] * f;
+        }
+        const int t_row = next.pair * 2 * TQ + tok;
+        const bool empty = len - n + t_row + 1 <= 0;
+        const float inv = 1.f / l;
+        char *out = (char *)a.out + ((((int64_t)begin + t_row) * a.q_heads + next.h * G + in % G) * D + dims) * 2;
+#pragma unroll
+        for (int i = 0; i < D / 8; i += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = empty ? 0u : pack2<BF16>(o[i + 2 * j] * inv, o[i + 2 * j + 1] * inv);
+            *reinterpret_cast<uint4 *>(out + i * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+namespace {
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {
+    static const EncodeTiled fn = []() -> EncodeTiled {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            return nullptr;
+        return (EncodeTiled)p;
+    }();
+    return fn;
+}
+
+// Rank 4, 64 elements (128 bytes, swizzled) of the innermost dimension a copy; what lies outside reads as zero.
+CUresult encode(CUtensorMap *map, bool bf16, const void *p, const cuuint64_t (&dim)[4], const cuuint64_t (&stride)[3],
+                const cuuint32_t (&box)[4]) {
+    const cuuint32_t one[4] = {1u, 1u, 1u, 1u};
+    return encoder()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(p),
+                     dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+// Launches behind the stream's last kernel without waiting for its end (the kernels wait for it themselves).
+template <typename... KArgs, typename... Args>
+cudaError_t launch_behind(void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
+}
+
+template <int D, bool BF16>
+cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, void *ws, cudaStream_t stream) {
+    cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D>::kSmem);
+    const size_t smem = (size_t)(a.B + 1) * 8;
+    if (e == cudaSuccess && smem > 40 * 1024)
+        e = cudaFuncSetAttribute(attention_schedule_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kAttnMaxB + 1) * 8);
+    if (e == cudaSuccess)
+        e = launch_behind(attention_schedule_kernel, dim3(1), kScheduleThreads, smem, stream, a, (WorkspaceHead *)ws);
+    if (e == cudaSuccess)
+        e = launch_behind(attention_tc_kernel<D, BF16>, dim3(kMaxBlocks), kThreads, (size_t)Sizes<D>::kSmem, stream, a, q, k, v, ws);
+    if (e == cudaSuccess)
+        e = launch_behind(attention_combine_kernel<D, BF16>, dim3(kMaxBlocks, kCombineRows), kCombineThreads, 0, stream, a, ws);
+    return e;
+}
+
+}  // namespace
+
+size_t attention_tc_workspace_bytes(int32_t B, int32_t d) {
+    return (kHeadBytes + (size_t)kMaxBlocks * 2 * kPartRows * (d + 2) * 4 + 255) / 256 * 256;
+}
+
+pcg_status attention_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream) {
+    if (!encoder()) {
+        set_error("%s: the driver does not provide cuTensorMapEncodeTiled", who);
+        return PCG_ERR_CUDA;
+    }
+    const bool bf16 = dtype == PCG_BF16;
+    const cuuint64_t d = a.d, G = a.q_heads / a.kv_heads, heads = a.kv_heads, rows = a.rows;
+    const cuuint32_t g = (cuuint32_t)G, tokens = (cuuint32_t)(kTile / G);
+    alignas(64) CUtensorMap q, k, v;
+    CUresult r = encode(&q, bf16, a.q, {d, G, heads, rows}, {d * 2, G * d * 2, (cuuint64_t)a.q_stride * 2}, {64u, g, 1u, tokens});
+    if (a.kv_len) {
+        const cuuint64_t bs = 1ull << a.bs_shift, blocks = a.n_blocks;
+        const cuuint32_t box = bs < kTile ? (cuuint32_t)bs : kTile;
+        if (r == CUDA_SUCCESS) r = encode(&k, bf16, a.k, {d, bs, heads, blocks}, {d * 2, bs * d * 2, heads * bs * d * 2}, {64u, box, 1u, 1u});
+        if (r == CUDA_SUCCESS) r = encode(&v, bf16, a.v, {d, bs, heads, blocks}, {d * 2, bs * d * 2, heads * bs * d * 2}, {64u, box, 1u, 1u});
+    } else {
+        const cuuint64_t ks = (cuuint64_t)a.k_stride * 2, vs = (cuuint64_t)a.v_stride * 2;
+        if (r == CUDA_SUCCESS) r = encode(&k, bf16, a.k, {d, heads, rows, 1}, {d * 2, ks, rows * ks}, {64u, 1u, kTile, 1u});
+        if (r == CUDA_SUCCESS) r = encode(&v, bf16, a.v, {d, heads, rows, 1}, {d * 2, vs, rows * vs}, {64u, 1u, kTile, 1u});
+    }
+    if (r != CUDA_SUCCESS) {
+        set_error("%s: cuTensorMapEncodeTiled failed (%d)", who, (int)r);
+        return PCG_ERR_CUDA;
+    }
+    cudaError_t e;
+    if (a.d == 128)
+        e = bf16 ? launch<128, true>(a, q, k, v, workspace, stream) : launch<128, false>(a, q, k, v, workspace, stream);
+    else
+        e = bf16 ? launch<64, true>(a, q, k, v, workspace, stream) : launch<64, false>(a, q, k, v, workspace, stream);
+    return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
+}
+
+}  // namespace pcg
