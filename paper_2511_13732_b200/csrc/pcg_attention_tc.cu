@@ -31,10 +31,8 @@ namespace pcg {
 constexpr int kTile = 128;       // rows of a row tile = lanes of tensor memory; keys of a key tile
 constexpr int kMaxBlocks = 148;  // blocks of the main kernel: one per SM of a B200 (more or fewer SMs only change the pace)
 constexpr int kSoftmaxWarps = 8;
-constexpr int kThreads = 32 * (kSoftmaxWarps + 4);  // a warpgroup of fetch, products and two idle warps behind them
-// Registers are launched as 168 a thread (384 * 168 = 64512) and then moved to the softmax warps, whose threads hold a
-// row of 128 scores: 256 * 216 + 128 * 64 = 63488.
-constexpr int kRegsSoftmax = 216, kRegsOther = 64;
+constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
+constexpr int kFmaShare = 10;    // of 32 weights, how many are computed on the FMA pipes
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
 
 // ---------------------------------------------------------------------------------------------- workspace
@@ -230,15 +228,15 @@ struct Walk {
 // ---------------------------------------------------------------------------------------------- device primitives
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// Bounded wait for a phase of an mbarrier: false = gave up, or another role has.  A poll suspends the thread for up to
-// about a microsecond, so the limit is some seconds at most and some tens of milliseconds at least.
+// Bounded wait for a phase of an mbarrier: false = gave up, or another role has.  A poll may suspend the thread for a
+// time that the hardware sets (microseconds), so the limit is some tens of milliseconds at least and seconds at most.
 constexpr uint32_t kPolls = 1u << 21;
 __device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(done)
-        : "r"(bar), "r"(parity), "r"(1000u)
+        : "r"(bar), "r"(parity)
         : "memory");
     return done != 0;
 }
@@ -260,6 +258,14 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 }
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// One lane of a converged warp, the same one every time.  The tensor-core and copy instructions take their operands from the
+// warp's uniform registers: where one lane is chosen by a comparison, each of them is issued by a loop over the lanes
+// (about 90 cycles an instruction), and behind this one at once.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
 }
 // Arrives when all products that this thread has issued are complete.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
@@ -325,7 +331,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t *v) {
         PCG_W8(v, 0), PCG_W8(v, 8)
         : "memory");
 }
+// Waits for the loads so far.  A load's registers are named again behind the wait, so that no use moves ahead of it.
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void tmem_loaded(uint32_t *v) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        asm volatile("" : "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]),
+                     "+r"(v[i + 7]));
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -338,6 +352,74 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     else
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+// Two floats in a 64-bit register pair, for the packed fp32 instructions.
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t r, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// NaN if one of the three is.
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// 2^x of two values on the FMA pipes, for x <= 16 and finite, or -inf (which gives 2^-126): the special-function unit makes
+// 16 a clock and SM, which is half of what the tensor cores could use, so that some of a tile's weights come from here.
+// Cody and Waite's reduction, x = n + f with n = round(x) by adding 1.5 * 2^23, and a polynomial of degree 4 for 2^f on
+// [-1/2, 1/2], fitted by Remez' exchange to the least relative error: 2.7e-6 in fp32.
+__device__ __forceinline__ uint64_t exp2_fma(uint64_t x) {
+    constexpr float kRound = 12582912.f;
+    float a, b;
+    unpair(x, a, b);
+    x = pair(fmaxf(a, -126.f), fmaxf(b, -126.f));
+    const uint64_t r = add2(x, pair(kRound, kRound));
+    const uint64_t n = add2(r, pair(-kRound, -kRound));
+    const uint64_t f = fma2(n, pair(-1.f, -1.f), x);
+    uint64_t y = fma2(f, pair(0.009570102207362652f, 0.009570102207362652f), pair(0.05591785907745361f, 0.05591785907745361f));
+    y = fma2(f, y, pair(0.240247443318367f, 0.240247443318367f));
+    y = fma2(f, y, pair(0.6931217908859253f, 0.6931217908859253f));
+    y = fma2(f, y, pair(0.9999992847442627f, 0.9999992847442627f));
+    float ra, rb, ya, yb;
+    unpair(r, ra, rb);
+    unpair(y, ya, yb);
+    return pair(__uint_as_float((__float_as_uint(ra) << 23) + __float_as_uint(ya)),
+                __uint_as_float((__float_as_uint(rb) << 23) + __float_as_uint(yb)));
+}
+
+// 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs.  kFmaShare of them by exp2_fma.
+template <bool BF16>
+__device__ __forceinline__ void weights(const uint32_t *v, uint64_t scale, uint64_t shift, uint64_t (&sum)[4], uint32_t *p) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        uint64_t x = fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale, shift);
+        float a, b;
+        if ((i * kFmaShare) % 32 < kFmaShare) {
+            x = exp2_fma(x);
+            unpair(x, a, b);
+        } else {
+            unpair(x, a, b);
+            a = ex2(a);
+            b = ex2(b);
+            x = pair(a, b);
+        }
+        sum[i & 3] = add2(sum[i & 3], x);
+        p[i] = pack2<BF16>(a, b);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- main kernel
@@ -376,13 +458,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto s_full = [&](int s) { return q_full + 24u + 8u * s; };   // a slot's scores are complete
     auto p_full = [&](int s) { return q_full + 40u + 8u * s; };   // ... its weights are in place
     auto o_full = [&](int s) { return q_full + 56u + 8u * s; };   // ... its last product is complete
+    auto p_half = [&](int s) { return q_full + 88u + 8u * s; };   // ... those of the first 64 keys
     const uint32_t merge_full = q_full + 72, merge_done = q_full + 80;  // slot 1's reference and sum are handed over, read
 
     if (tid == 0) {
-        for (int i = 0; i < 2 * S + 12; ++i) {
+        for (int i = 0; i < 2 * S + 13; ++i) {
             // by warps: the weights of a slot (4), the hand-over (4 and 4); by one thread or the hardware: all others
             const uint32_t bar = bar0 + 8u * i;
-            const uint32_t count = bar == p_full(0) || bar == p_full(1) || bar == merge_full || bar == merge_done ? 4 : 1;
+            const uint32_t count = bar == p_full(0) || bar == p_full(1) || bar == p_half(0) || bar == p_half(1) || bar == merge_full || bar == merge_done ? 4 : 1;
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -404,11 +487,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     Walk walk;
     walk.start(a, reinterpret_cast<const WorkspaceHead *>(ws)->run[blockIdx.x]);
     Segment g;
-    if (warp < kSoftmaxWarps)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-    else
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax: thread = row of the slot's row tile
         const int slot = warp >> 2, row = (warp & 3) * 32 + lane;
@@ -425,6 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool warp_valid = __any_sync(0xffffffffu, valid);
             const int first = g.two ? 0 : slot, step = g.two ? 1 : 2;
             float m = kNegInf, l = 0.f;
+            bool bad = false;
             for (int t = first; t < g.nt; t += step, ++sn) {
                 ok = __all_sync(0xffffffffu, bar_wait(s_full(slot), sn & 1, failed));
                 if (!ok) break;
@@ -449,19 +528,38 @@ __global__ void __launch_bounds__(kThreads, 1)
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 if (warp_valid) {
-                    uint32_t v[kTile];
-#pragma unroll
-                    for (int c = 0; c < kTile; c += 32) tmem_ld32(sc + c, v + c);
-                    tmem_wait_ld();
-                    if (__any_sync(0xffffffffu, lim < k0 + kTile)) {
-#pragma unroll
-                        for (int c = 0; c < kTile; ++c)
-                            if (k0 + c >= lim) v[c] = __float_as_uint(kNegInf);
-                    }
+                    uint32_t v[64];
                     float top[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
+                    const bool masked = __any_sync(0xffffffffu, lim < k0 + kTile);
+                    const int seen = lim - k0;
+                    auto mask = [&](int from) {
 #pragma unroll
-                    for (int c = 0; c < kTile; ++c) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(v[c]));
-                    const float mt = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.scale_log2;
+                        for (int c = 0; c < 64; ++c)
+                            if (from + c >= seen) v[c] = __float_as_uint(kNegInf);
+                    };
+                    {
+                        uint32_t u[64];
+                        tmem_ld32(sc, v);
+                        tmem_ld32(sc + 32, v + 32);
+                        tmem_ld32(sc + 64, u);
+                        tmem_ld32(sc + 96, u + 32);
+                        tmem_wait_ld();
+                        tmem_loaded<64>(v);
+                        tmem_loaded<64>(u);
+                        if (masked) {
+                            mask(0);
+#pragma unroll
+                            for (int c = 0; c < 64; ++c)
+                                if (64 + c >= seen) u[c] = __float_as_uint(kNegInf);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2) {
+                            top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                            top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(u[c]), __uint_as_float(u[c + 1]));
+                        }
+                    }
+                    const float mt = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * a.scale_log2;
+                    bad = bad || !(mt < -kNegInf);
                     // also when the first score above -inf is met; a row's reference depends on its own scores alone, and
                     // padding rows, whose scores are arbitrary, have none
                     const bool move = valid && mt > m + kSlack;
@@ -469,11 +567,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                         const float mnew = move ? mt : m, f = move ? ex2(m - mt) : 1.f;
                         l *= f;
                         if (t > first) {
-#pragma unroll
+#pragma unroll 1
                             for (int c = 0; c < D; c += 16) {
                                 uint32_t o[16];
                                 tmem_ld16(oc + c, o);
                                 tmem_wait_ld();
+                                tmem_loaded<16>(o);
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                                 tmem_st16(oc + c, o);
@@ -481,29 +580,46 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         m = mnew;
                     }
-                    // a row that has met no score above -inf yet weighs everything 0
-                    const float shift = (m == kNegInf ? 0.f : -m) + kLift;
-                    float part[4] = {0.f, 0.f, 0.f, 0.f};
-                    uint32_t p[32];
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                        for (int c = 0; c < 64; c += 2) {
-                            const float x = ex2(fmaf(__uint_as_float(v[half * 64 + c]), a.scale_log2, shift));
-                            const float y = ex2(fmaf(__uint_as_float(v[half * 64 + c + 1]), a.scale_log2, shift));
-                            part[c & 2] += x;
-                            part[(c & 2) + 1] += y;
-                            p[c / 2] = pack2<BF16>(x, y);
+                    // a row that has met no score above -inf yet weighs everything 0 (or 2^-126: its sums are dropped)
+                    const float by = (m == kNegInf ? 0.f : -m) + kLift;
+                    const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), by2 = pair(by, by);
+                    uint64_t sum[4] = {0, 0, 0, 0};
+                    // Half the keys at a time: the product with the first half's values starts while the other weights are
+                    // computed.  The second half's scores are read again, into the registers that the first half leaves: a
+                    // loop of two turns keeps the code in the instruction cache, which 128 scores in line do not fit.  (The
+                    // first half's weights lie where its own scores were.)
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t p[32];
+                        if (h) {
+                            tmem_wait_ld();
+                            tmem_loaded<64>(v);
+                            if (masked) mask(64);
                         }
-                        tmem_st32(sc + half * 32, p);
+                        weights<BF16>(v, scale2, by2, sum, p);
+                        if (!h) tmem_ld32(sc + 64, v);
+                        weights<BF16>(v + 32, scale2, by2, sum, p + 16);
+                        if (!h) tmem_ld32(sc + 96, v + 32);
+                        tmem_st32(sc + h * 32, p);
+                        tmem_wait_st();
+                        if (!h) {
+                            fence_before();
+                            __syncwarp();
+                            if (lane == 0) bar_arrive(p_half(slot));
+                        }
                     }
-                    l += (part[0] + part[1]) + (part[2] + part[3]);
-                    tmem_wait_st();
+                    float s0, s1;
+                    unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
+                    l += s0 + s1;
+                } else {
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(p_half(slot));
                 }
                 fence_before();
                 __syncwarp();
                 if (lane == 0) bar_arrive(p_full(slot));
             }
+            if (bad) l = __int_as_float(0x7fffffff);  // a score of +inf or NaN
             if (!ok) break;
             loads += 2 * g.nt;
             // ---- end of the part
@@ -538,20 +654,22 @@ __global__ void __launch_bounds__(kThreads, 1)
                     m = mx;
                 }
                 const bool whole = g.t0 == 0 && g.nt == g.tiles;
-                // a row that sees no key has weights of 0 alone; one that sees scores of -inf alone ends as 0 / 0 = NaN
-                const float inv = lim <= 0 ? 0.f : 1.f / l;
+                // a row that sees no key is 0 (below); one that sees scores of -inf alone is NaN, as 0 / 0 is
+                const float inv = m == kNegInf ? __int_as_float(0x7fffffff) : 1.f / l;
                 char *out = (char *)a.out + (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2);
                 const int prow = (g.two ? slot * kTile : 0) + row;
                 float *part = part_base(ws, blockIdx.x, g.t0 == 0 ? 1 : 0, D);
-#pragma unroll
+#pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     uint32_t o[32];
                     tmem_ld32(oc + c, o);
                     tmem_wait_ld();
+                    tmem_loaded<32>(o);
                     if (shared) {
                         uint32_t o1[32];
                         tmem_ld32(o_col(1) + lanes + c, o1);
                         tmem_wait_ld();
+                        tmem_loaded<32>(o1);
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
                             o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
@@ -584,35 +702,47 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
         }
     } else if (warp == kSoftmaxWarps) {
-        // ------------------------------------------------------------------ fetch: one lane per page and 64 dimensions
+        // ------------------------------------------------------------------ fetch: a lane per page looks its block up, one issues
         const bool paged = a.kv_len != nullptr;
         const int box = paged ? min(1 << a.bs_shift, kTile) : kTile;  // rows of one copy
         const int copies = kTile / box;
-        const int my_row = (lane % copies) * box, my_part = lane / copies;  // at most 8 * 2 lanes have a copy
-        uint32_t it = 0, items = 0;
+        uint32_t it = 0, stage = 0, stage_phase = 1, items = 0;  // a stage's first fill waits for nothing: parity 1 has passed
         bool ok = true;
         while (ok && walk.next(a, TQ, g)) {
-            auto page_of = [&](int t) -> int32_t {  // the block of this lane's rows of key tile t
-                const int p = (g.t0 + t) * kTile + my_row;
-                if (!paged || my_part >= kParts || t >= g.nt || p >= g.len) return -1;
+            auto page_of = [&](int t) -> int32_t {  // the block of key tile t's rows from lane * box on
+                const int p = (g.t0 + t) * kTile + lane * box;
+                if (!paged || lane >= copies || t >= g.nt || p >= g.len) return -1;
                 const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
                 return block < 0 || block >= a.n_blocks ? a.n_blocks : block;  // behind the tensor: reads zeros
             };
             auto fetch = [&](const CUtensorMap *map, int t, int32_t page) -> bool {
-                const int s = it % S;
-                if (it >= S && !__all_sync(0xffffffffu, bar_wait(empty_bar(s), ((it / S) - 1) & 1, failed))) return false;
+                const uint32_t s = stage;
+                if (!__all_sync(0xffffffffu, bar_wait(empty_bar(s), stage_phase, failed))) return false;
+                if (++stage == S) {
+                    stage = 0;
+                    stage_phase ^= 1;
+                }
                 const int k0 = (g.t0 + t) * kTile;
                 // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
                 const int n_copies = paged ? min(copies, (max(g.len - k0, 0) + box - 1) / box) : 1;
-                if (lane == 0) bar_expect(full_bar(s), n_copies * box * D * 2);
-                __syncwarp();
-                if (my_part < kParts && my_row < n_copies * box) {
-                    const uint32_t dst = ring + s * kTileBytes + my_part * (kTile * 128) + my_row * 128;
-                    if (paged)
-                        tma_load(dst, map, my_part * 64, (k0 + my_row) & ((1 << a.bs_shift) - 1), g.h, page, full_bar(s));
-                    else
-                        tma_load(dst, map, my_part * 64, g.h, g.begin + k0, 0, full_bar(s));
+                for (int c = 0; c < n_copies; ++c) {
+                    const int32_t block = __shfl_sync(0xffffffffu, page, c);
+                    if (elect_one()) {
+                        if (c == 0) bar_expect(full_bar(s), n_copies * box * D * 2);
+                        const uint32_t dst = ring + s * kTileBytes + c * box * 128;
+                        const int r = k0 + c * box;
+#pragma unroll
+                        for (int part = 0; part < kParts; ++part) {
+                            if (paged)
+                                tma_load(dst + part * (kTile * 128), map, part * 64, r & ((1 << a.bs_shift) - 1), g.h, block, full_bar(s));
+                            else
+                                tma_load(dst + part * (kTile * 128), map, part * 64, g.h, g.begin + r, 0, full_bar(s));
+                        }
+                    }
+                    __syncwarp();
                 }
+                if (n_copies == 0 && elect_one()) bar_arrive(full_bar(s));
+                __syncwarp();
                 ++it;
                 return true;
             };
@@ -620,7 +750,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (items > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (items - 1) & 1, failed));
             if (!ok) break;
             ++items;
-            if (lane == 0) {
+            if (elect_one()) {
                 const int tiles = g.two ? 2 : 1;
                 bar_expect(q_full, tiles * kParts * G * TQ * 128);
                 for (int r = 0; r < tiles; ++r)
@@ -647,71 +777,104 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (items > 0) bar_drain(q_full, (items - 1) & 1);
             for (uint32_t back = 1; back <= S && back <= it; ++back) bar_drain(full_bar((it - back) % S), ((it - back) / S) & 1);
         }
-    } else if (warp == kSoftmaxWarps + 1 && lane == 0) {
-        // ------------------------------------------------------------------ products: one thread
-        uint32_t it = 0, items = 0, pn0 = 0, pn1 = 0;  // pn: phases of a slot's weights
+    } else {
+        // ------------------------------------------------------------------ products: the warp waits, one lane issues
+        // stages in the order of their use, weights of a slot and queries: number (of a stage) and phase of the next
+        uint32_t stage = 0, stage_phase = 0, p_phase0 = 0, p_phase1 = 0, q_phase = 0;
         bool ok = true;
-        auto wait_stage = [&](uint32_t i) { return bar_wait(full_bar(i % S), (i / S) & 1, failed); };
-        auto scores = [&](int slot, int rows, uint32_t i) {
-            const uint32_t q = qbuf + rows * kTileBytes, k = ring + (i % S) * kTileBytes;
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, failed)); };
+        auto next_stage = [&]() {  // waits for it
+            const uint32_t s = stage;
+            wait(full_bar(s), stage_phase);
+            if (++stage == S) {
+                stage = 0;
+                stage_phase ^= 1;
+            }
+            return s;
+        };
+        const uint64_t qdesc = desc_k(qbuf), kdesc = desc_k(ring), vdesc = desc_mn(ring);
+        auto scores = [&](int slot, int row_tile, uint32_t s) {  // (by the elected lane, as all below)
+            const uint64_t q = qdesc + (uint64_t)(row_tile * (kTileBytes >> 4)), k = kdesc + (uint64_t)(s * (kTileBytes >> 4));
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk) {
-                const uint32_t off = (kk >> 2) * (kTile * 128) + (kk & 3) * 32;
-                mma_ss(s_col(slot), desc_k(q + off), desc_k(k + off), kIdescQK, kk > 0);
+                constexpr int kPart = (kTile * 128) >> 4;
+                mma_ss(s_col(slot), q + (kk >> 2) * kPart + (kk & 3) * 2, k + (kk >> 2) * kPart + (kk & 3) * 2, kIdescQK, kk > 0);
             }
             mma_commit(s_full(slot));
         };
+        // One slot's turn: its weights with the values of stage vs, in two halves, then the scores of its next key tile.
+        auto turn = [&](int slot, int row_tile, uint32_t vs, bool begun, bool last_use, bool more, uint32_t &ks, bool load_k, bool last_q) {
+            const uint32_t phase = slot ? p_phase1 : p_phase0;
+            if (slot)
+                p_phase1 ^= 1;
+            else
+                p_phase0 ^= 1;
+            wait(p_half(slot), phase);
+            if (!ok) return;
+            fence_after();
+            const uint64_t v = vdesc + (uint64_t)(vs * (kTileBytes >> 4));
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = 0; kk < kTile / 32; ++kk)
+                    mma_ts(o_col(slot), s_col(slot) + kk * 8, v + kk * (2048 >> 4), kIdescPV, begun || kk > 0);
+            }
+            __syncwarp();
+            if (load_k) ks = next_stage();
+            wait(p_full(slot), phase);
+            if (!ok) return;
+            fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int kk = kTile / 32; kk < kTile / 16; ++kk)
+                    mma_ts(o_col(slot), s_col(slot) + kk * 8, v + kk * (2048 >> 4), kIdescPV, 1);
+                if (more) {
+                    scores(slot, row_tile, ks);
+                    if (last_use) mma_commit(empty_bar(ks));
+                    if (last_q) mma_commit(q_empty);
+                } else {
+                    mma_commit(o_full(slot));
+                }
+                if (last_use) mma_commit(empty_bar(vs));
+            }
+            __syncwarp();
+        };
         while (ok && walk.next(a, TQ, g)) {
-            ok = bar_wait(q_full, items & 1, failed);
-            ++items;
+            wait(q_full, q_phase);
+            q_phase ^= 1;
             const int ahead = g.two ? 1 : 2;
-            for (int t = 0; ok && t < min(ahead, g.nt); ++t, ++it) {
-                ok = wait_stage(it);
+            for (int t = 0; ok && t < min(ahead, g.nt); ++t) {
+                const uint32_t s = next_stage();
                 if (!ok) break;
                 fence_after();
-                if (g.two) {
-                    scores(0, 0, it);
-                    scores(1, 1, it);
-                } else {
-                    scores(t, 0, it);
+                if (elect_one()) {
+                    if (g.two) {
+                        scores(0, 0, s);
+                        scores(1, 1, s);
+                    } else {
+                        scores(t, 0, s);
+                    }
+                    mma_commit(empty_bar(s));
+                    if (t == g.nt - 1) mma_commit(q_empty);
                 }
-                mma_commit(empty_bar(it % S));
-                if (t == g.nt - 1) mma_commit(q_empty);
+                __syncwarp();
             }
             for (int t = 0; ok && t < g.nt; ++t) {
-                const uint32_t vi = it++;
-                const bool more = t + ahead < g.nt;
-                const uint32_t ki = it;
-                if (more) ++it;
-                ok = wait_stage(vi);
-                for (int r = 0; ok && r < (g.two ? 2 : 1); ++r) {
-                    const int slot = g.two ? r : t & 1;
-                    ok = bar_wait(p_full(slot), (slot ? pn1++ : pn0++) & 1, failed);
-                    if (!ok) break;
-                    fence_after();
-                    const uint32_t v = ring + (vi % S) * kTileBytes;
-                    const bool begun = t >= (g.two ? 1 : 2);
-#pragma unroll
-                    for (int kk = 0; kk < kTile / 16; ++kk)
-                        mma_ts(o_col(slot), s_col(slot) + kk * 8, desc_mn(v + kk * 2048), kIdescPV, begun || kk > 0);
-                    if (!g.two || r == 1) mma_commit(empty_bar(vi % S));
-                    if (more) {
-                        if (r == 0) ok = wait_stage(ki);
-                        if (!ok) break;
-                        fence_after();
-                        scores(slot, g.two ? r : 0, ki);
-                        if (!g.two || r == 1) {
-                            mma_commit(empty_bar(ki % S));
-                            if (t + ahead == g.nt - 1) mma_commit(q_empty);
-                        }
-                    } else {
-                        mma_commit(o_full(slot));
-                    }
+                const uint32_t vs = next_stage();
+                const bool more = t + ahead < g.nt, last_q = t + ahead == g.nt - 1;
+                uint32_t ks = 0;
+                if (!ok) break;
+                if (g.two) {
+                    turn(0, 0, vs, t > 0, false, more, ks, more, false);
+                    if (ok) turn(1, 1, vs, t > 0, true, more, ks, false, last_q);
+                } else {
+                    turn(t & 1, 0, vs, t > 1, true, more, ks, more, last_q);
                 }
             }
         }
         if (*failed) {  // products already issued may still be writing tensor memory: it is freed when they have retired
-            mma_commit(drain);
+            __syncwarp();
+            if (elect_one()) mma_commit(drain);
+            __syncwarp();
             bar_drain(drain, 0);
         }
     }
