@@ -9,11 +9,13 @@
 //   one row tile (tokens, drafted chunks):  both slots have that row tile and take the key tiles in turn, so that one
 //                                           slot's softmax runs under the other's products; their sums meet at the end.
 //
-// attention_schedule_kernel  numbers all (item, key tile) units of the call and cuts the numbers into one equal run per
-//                            block, whatever the lengths are: no block waits for another, and an item may be shared.
-// attention_tc_kernel        a block's run of units: 8 softmax warps (two slots), a warp that fetches (TMA), a warp that
-//                            issues tcgen05.mma.  An item that a block has to itself is written out; a part of one goes
-//                            to the workspace as an unscaled sum with its reference and its sum of weights.
+// attention_tc_kernel        Every block first cuts the call's work into one equal run per block, whatever the lengths are:
+//                            it numbers the units of all items, a unit for each key tile and two for what an item costs
+//                            beside its key tiles, and looks up where its own run begins and ends.  No block waits for
+//                            another, and an item may be shared.  Then 8 softmax warps (two slots), a warp that fetches
+//                            (TMA) and a warp that issues tcgen05.mma go through the run.  An item that a block has to
+//                            itself is written out; a part of one goes to the workspace as an unscaled sum with its
+//                            reference and its sum of weights.
 // attention_combine_kernel   joins the parts of items that were shared, in the order of the blocks.
 //
 // Tensor memory: scores S0, S1 (128 columns each, fp32), outputs O0, O1 (D columns each, fp32).  The weights of a tile
@@ -36,16 +38,13 @@ constexpr int kFmaShare = 10;    // of 32 weights, how many are computed on the 
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
 
 // ---------------------------------------------------------------------------------------------- workspace
-struct Run {       // one block's units
-    int64_t first;  // number of its first unit
+struct Run {        // one block's key tiles
+    int64_t first;  // number of its first key tile among those of the call
     int32_t b, h, pair, tile;  // where that is
-    int32_t count;  // units
-    int32_t pad;
 };
 struct WorkspaceHead {
-    int32_t error;  // set when a bounded wait ran out: the call's outputs are then NaN
-    int32_t pad[63];
-    Run run[kMaxBlocks + 1];
+    Run run[kMaxBlocks + 1];     // the last begins behind the last key tile
+    int32_t failed[kMaxBlocks];  // set where a bounded wait ran out: the call's outputs are then NaN
 };
 // Partial sums: [block][2: a part that does not begin its item, one that does][2 * 128 rows], D sums each stored
 // [D][256] so that a warp's 32 rows are adjacent, then reference and sum of weights.
@@ -61,9 +60,6 @@ __device__ __forceinline__ float *part_base(void *ws, int block, int which, int 
 }
 
 // ---------------------------------------------------------------------------------------------- items
-struct Shape {
-    int G, TQ;  // query heads per key head, tokens of a row tile
-};
 __host__ __device__ __forceinline__ int pairs_of(int n, int TQ) { return (n + 2 * TQ - 1) / (2 * TQ); }
 // Key tiles of pair p: up to what its last row sees, and one where it sees nothing.
 __device__ __forceinline__ int tiles_of(int n, int len, int TQ, int p) {
@@ -71,113 +67,138 @@ __device__ __forceinline__ int tiles_of(int n, int len, int TQ, int p) {
     return lim <= kTile ? 1 : (lim + kTile - 1) / kTile;
 }
 
-// Sum over 0 <= i < n of floor((a i + b) / m), a, b >= 0 (Euclid's steps on a and m).
-__device__ __forceinline__ int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
-    int64_t s = 0;
+// Sum over 0 <= i < n of floor((a i + b) / 128), a, b >= 0: Euclid's steps on a and the divisor, the first of them by
+// shifts; what is left fits 32 bits.
+__device__ __forceinline__ int64_t floor_sum_128(uint32_t n, uint32_t a, int64_t b) {
+    const int64_t nn = n;
+    int64_t s = nn * (nn - 1) / 2 * (a >> 7) + nn * (b >> 7);
+    a &= 127;
+    int64_t y = (int64_t)a * n + (b & 127);
+    uint32_t m = a, x = 128;  // from here: sum over 0 <= i < y / 128 of floor((128 i + y % 128) / a), and so on
+    uint32_t c = (uint32_t)(y & 127);
+    n = (uint32_t)(y >> 7);
     while (n > 0) {
-        if (a >= m) {
-            s += n * (n - 1) / 2 * (a / m);
-            a %= m;
-        }
-        if (b >= m) {
-            s += n * (b / m);
-            b %= m;
-        }
-        const int64_t y = a * n + b;
-        if (y < m) break;
-        n = y / m;
-        b = y % m;
-        const int64_t t = a;
-        a = m;
+        const int64_t k = n;
+        s += k * (k - 1) / 2 * (x / m) + k * (c / m);
+        x %= m;
+        c %= m;
+        const uint64_t z = (uint64_t)x * n + c;
+        if (z < m) break;
+        n = (uint32_t)(z / m);
+        c = (uint32_t)(z % m);
+        const uint32_t t = x;
+        x = m;
         m = t;
     }
     return s;
 }
 // Key tiles of a sequence's first p pairs.
 __device__ int64_t tiles_before(int n, int len, int TQ, int p) {
-    const int whole = n / (2 * TQ), q = min(p, whole);  // pairs of 2 * TQ tokens
-    // pairs whose last row sees at most one tile of keys count 1 each: (i + 1) * 2 TQ <= 128 - (len - n)
-    const int64_t base = (int64_t)len - n, step = 2 * TQ;
-    const int64_t head = base >= kTile ? 0 : min((int64_t)q, (kTile - base) / step);
+    const int step = 2 * TQ, whole = n / step, q = min(p, whole);  // `whole` pairs of 2 * TQ tokens, then one of fewer
+    // pairs whose last row sees at most one tile of keys count 1 each: (i + 1) * step <= 128 - (len - n)
+    const int base = len - n;
+    const int head = base >= kTile ? 0 : (int)min((int64_t)q, (kTile - (int64_t)base) / step);
     int64_t s = head;
-    s += floor_sum(q - head, kTile, step, base + (head + 1) * step + kTile - 1);
+    if (q > head) s += floor_sum_128(q - head, step, base + (int64_t)(head + 1) * step + kTile - 1);
     if (p > whole) s += tiles_of(n, len, TQ, whole);
     return s;
 }
 
-// ---------------------------------------------------------------------------------------------- schedule
-constexpr int kScheduleThreads = 1024;
+// ---------------------------------------------------------------------------------------------- the cut
+// What an item costs beside its key tiles (fetching queries, the first and the last tile's latency, writing out), in units
+// of a key tile: measured at 6,500 to 7,800 cycles for 3,500 a key tile.  Blocks get at least kLeast units: fewer, and a
+// short call's parts cost more to join than they save.
+constexpr int kItemUnits = 2, kLeast = 4;
 
-// One block.  Thread t sums the units of a run of sequences, a scan numbers them, and then thread c finds where block c's
-// run begins: by bisection over the sequences, then over the pairs of one.
-__global__ void __launch_bounds__(kScheduleThreads) attention_schedule_kernel(const __grid_constant__ AttnArgs a, WorkspaceHead *ws) {
-    extern __shared__ int64_t before[];  // [B + 1] units of the sequences before b
-    __shared__ int64_t scratch[kScheduleThreads / 32];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;");
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
-    const int per = (a.B + kScheduleThreads - 1) / kScheduleThreads, lo = min(a.B, tid * per), hi = min(a.B, lo + per);
-    auto units_of = [&](int b) -> int64_t {
+// By all threads of the block: where runs `block` and `block + 1` begin, to out[0] and out[1].  `scratch` holds B
+// int64_t and B int32_t (192 KB of shared memory at the most).
+__device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int64_t *warp_units, int64_t *warp_items, Run *out) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, B = a.B;
+    int64_t *units = scratch;                                 // [B] of the sequences before b
+    int32_t *items = reinterpret_cast<int32_t *>(units + B);  // [B] items of one head of the sequences before b
+    const int per = (B + kThreads - 1) / kThreads, lo = min(B, tid * per), hi = min(B, lo + per);
+    int64_t usum = 0, isum = 0;
+    for (int b = lo; b < hi; ++b) {
+        units[b] = usum;
+        items[b] = (int32_t)isum;
         int begin, n, len;
         attn_sequence(a, b, begin, n, len);
-        return n == 0 ? 0 : tiles_before(n, len, TQ, pairs_of(n, TQ)) * a.kv_heads;
-    };
-    int64_t sum = 0;
-    for (int b = lo; b < hi; ++b) {
-        before[b] = sum;
-        sum += units_of(b);
+        const int pairs = pairs_of(n, TQ);
+        if (n > 0) {
+            const int64_t tiles = pairs == 1 ? tiles_of(n, len, TQ, 0) : tiles_before(n, len, TQ, pairs);
+            usum += (tiles + (int64_t)kItemUnits * pairs) * a.kv_heads;
+            isum += pairs;
+        }
     }
-    int64_t inc = sum;
+    int64_t uinc = usum, iinc = isum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t up = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += up;
-    }
-    if (lane == 31) scratch[warp] = inc;
-    __syncthreads();
-    int64_t base = inc - sum, total = 0;
-    for (int w = 0; w < kScheduleThreads / 32; ++w) {
-        if (w < warp) base += scratch[w];
-        total += scratch[w];
-    }
-    for (int b = lo; b < hi; ++b) before[b] += base;
-    if (tid == 0) before[a.B] = total;
-    __syncthreads();
-    if (tid == 0) ws->error = 0;
-    if (tid > kMaxBlocks) return;
-    const int blocks = (int)min((int64_t)kMaxBlocks, max(total, (int64_t)1));
-    const int64_t u = tid >= blocks ? total : total / blocks * tid + total % blocks * tid / blocks;
-    const int64_t next = tid + 1 >= blocks ? total : total / blocks * (tid + 1) + total % blocks * (tid + 1) / blocks;
-    Run r{u, 0, 0, 0, 0, (int32_t)(next - u), 0};
-    if (u < total) {
-        int x = 0, y = a.B - 1;  // the last sequence whose units begin at or before u: empty ones share their number
-        while (x < y) {
-            const int mid = (x + y + 1) >> 1;
-            if (before[mid] <= u)
-                x = mid;
-            else
-                y = mid - 1;
+        const int64_t u = __shfl_up_sync(0xffffffffu, uinc, o), i = __shfl_up_sync(0xffffffffu, iinc, o);
+        if (lane >= o) {
+            uinc += u;
+            iinc += i;
         }
-        int begin, n, len;
-        attn_sequence(a, x, begin, n, len);
-        const int pairs = pairs_of(n, TQ);
-        const int64_t per_head = tiles_before(n, len, TQ, pairs), in = u - before[x];
-        const int64_t rest = in % per_head;
-        int p = 0, q = pairs - 1;
-        while (p < q) {
-            const int mid = (p + q + 1) >> 1;
-            if (tiles_before(n, len, TQ, mid) <= rest)
-                p = mid;
-            else
-                q = mid - 1;
-        }
-        r.b = x;
-        r.h = (int)(in / per_head);
-        r.pair = p;
-        r.tile = (int)(rest - tiles_before(n, len, TQ, p));
     }
-    ws->run[tid] = r;
+    if (lane == 31) {
+        warp_units[warp] = uinc;
+        warp_items[warp] = iinc;
+    }
+    __syncthreads();
+    int64_t ubase = uinc - usum, ibase = iinc - isum, total = 0, all_items = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+        if (w < warp) {
+            ubase += warp_units[w];
+            ibase += warp_items[w];
+        }
+        total += warp_units[w];
+        all_items += warp_items[w];
+    }
+    for (int b = lo; b < hi; ++b) {
+        units[b] += ubase;
+        items[b] += (int32_t)ibase;
+    }
+    __syncthreads();
+    if (lane == 0 && warp < 2) {
+        const int blocks = (int)max((int64_t)1, min((int64_t)kMaxBlocks, total / kLeast)), c = blockIdx.x + warp;
+        Run r{total - (int64_t)kItemUnits * a.kv_heads * all_items, 0, 0, 0, 0};  // behind the last key tile
+        const int64_t u = c >= blocks ? total : total / blocks * c + total % blocks * c / blocks;
+        if (u < total) {
+            int x = 0, y = B - 1;  // the last sequence whose units begin at or before u: empty ones share their number
+            while (x < y) {
+                const int mid = (x + y + 1) >> 1;
+                if (units[mid] <= u)
+                    x = mid;
+                else
+                    y = mid - 1;
+            }
+            int begin, n, len;
+            attn_sequence(a, x, begin, n, len);
+            const int pairs = pairs_of(n, TQ);
+            const int64_t tiles = pairs == 1 ? tiles_of(n, len, TQ, 0) : tiles_before(n, len, TQ, pairs);
+            const int64_t per_head = tiles + (int64_t)kItemUnits * pairs, in = u - units[x];
+            const int h = (int)(in / per_head);
+            const int64_t rest = in - h * per_head;
+            int p = 0, q = pairs - 1;
+            while (p < q) {
+                const int mid = (p + q + 1) >> 1;
+                if (tiles_before(n, len, TQ, mid) + (int64_t)kItemUnits * mid <= rest)
+                    p = mid;
+                else
+                    q = mid - 1;
+            }
+            const int64_t head_tiles = p == 0 ? 0 : tiles_before(n, len, TQ, p);
+            // an item's own units come first: a cut within them leaves the whole item to the run behind it
+            const int64_t tile = max((int64_t)0, rest - head_tiles - (int64_t)kItemUnits * p - kItemUnits);
+            r.first = units[x] - (int64_t)kItemUnits * a.kv_heads * items[x] + h * tiles + head_tiles + tile;
+            r.b = x;
+            r.h = h;
+            r.pair = p;
+            r.tile = (int)tile;
+        }
+        out[warp] = r;
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // copies land in the scratch's place
+    __syncthreads();
 }
 
 // A block's run of units, item by item: the same walk in every role.
@@ -189,12 +210,12 @@ struct Segment {
 struct Walk {
     int b, h, pair, tile, left;
     int begin, n, len;
-    __device__ __forceinline__ void start(const AttnArgs &a, const Run &r) {
+    __device__ __forceinline__ void start(const AttnArgs &a, const Run &r, const Run &next) {
         b = r.b;
         h = r.h;
         pair = r.pair;
         tile = r.tile;
-        left = r.count;
+        left = (int)min(next.first - r.first, (int64_t)0x7fffffff);
         if (left > 0) attn_sequence(a, b, begin, n, len);
     }
     __device__ __forceinline__ bool next(const AttnArgs &a, int TQ, Segment &s) {
@@ -216,9 +237,12 @@ struct Walk {
             if (++h == a.kv_heads) {
                 h = 0;
                 do {
-                    ++b;
+                    if (++b >= a.B) {  // row starts that overlap may have been counted for more than there is
+                        left = 0;
+                        break;
+                    }
                     attn_sequence(a, b, begin, n, len);
-                } while (n == 0);  // units are left, so a sequence with rows follows
+                } while (n == 0);
             }
         }
         return true;
@@ -422,12 +446,23 @@ __device__ __forceinline__ void weights(const uint32_t *v, uint64_t scale, uint6
     }
 }
 
+// 32 bytes of a row.  A warp's lanes hold 32 rows, so a store touches 32 lines whatever its width: few and wide ones.
+__device__ __forceinline__ void store_row(void *p, const uint32_t (&w)[8], bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), PCG_W8(w, 0) : "memory");
+    } else {  // 16-byte alignment
+        reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- main kernel
 template <int D>
 struct Sizes {
     static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
     static constexpr int kStages = D == 128 ? 5 : 10;        // ring of key and value tiles: 160 KB
     static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;  // room to start on a 1024-byte boundary
+    static_assert((2 + kStages) * kTileBytes >= kAttnMaxB * 12, "the cut's scratch");
 };
 
 template <int D, bool BF16>
@@ -444,6 +479,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     constexpr float kLift = BF16 ? 0.f : 7.f;
 
     extern __shared__ unsigned char smem_raw[];
+    __shared__ int64_t warp_units[kThreads / 32], warp_items[kThreads / 32];
+    __shared__ Run run[2];
     __shared__ __align__(8) uint64_t bars[2 * S + 16];
     __shared__ float other_m[kTile], other_l[kTile];  // slot 1's, for the end of an item with one row tile
     __shared__ uint32_t tmem_slot;
@@ -484,8 +521,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
+    cut_work(a, TQ, reinterpret_cast<int64_t *>(smem_raw + (base - smem_u32(smem_raw))), warp_units, warp_items, run);
+    if (tid == 0) reinterpret_cast<WorkspaceHead *>(ws)->run[blockIdx.x] = run[0];
+    if (tid == 0 && blockIdx.x == kMaxBlocks - 1) reinterpret_cast<WorkspaceHead *>(ws)->run[kMaxBlocks] = run[1];
     Walk walk;
-    walk.start(a, reinterpret_cast<const WorkspaceHead *>(ws)->run[blockIdx.x]);
+    walk.start(a, run[0], run[1]);
     Segment g;
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax: thread = row of the slot's row tile
@@ -657,6 +697,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 // a row that sees no key is 0 (below); one that sees scores of -inf alone is NaN, as 0 / 0 is
                 const float inv = m == kNegInf ? __int_as_float(0x7fffffff) : 1.f / l;
                 char *out = (char *)a.out + (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2);
+                const bool wide = ((uintptr_t)a.out & 31) == 0;
                 const int prow = (g.two ? slot * kTile : 0) + row;
                 float *part = part_base(ws, blockIdx.x, g.t0 == 0 ? 1 : 0, D);
 #pragma unroll 1
@@ -676,13 +717,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     if (valid && whole) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            uint32_t w[4];
+                        for (int i = 0; i < 32; i += 16) {
+                            uint32_t w[8];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
+                            for (int j = 0; j < 8; ++j)
                                 w[j] = lim <= 0 ? 0u
                                                 : pack2<BF16>(__uint_as_float(o[i + 2 * j]) * inv, __uint_as_float(o[i + 2 * j + 1]) * inv);
-                            *reinterpret_cast<uint4 *>(out + (c + i) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+                            store_row(out + (c + i) * 2, w, wide);
                         }
                     } else if (valid) {
 #pragma unroll
@@ -880,32 +921,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     fence_before();
     __syncthreads();
-    if (tid == 0 && failed_flag) atomicMax(&reinterpret_cast<WorkspaceHead *>(ws)->error, 1);
+    if (tid == 0) reinterpret_cast<WorkspaceHead *>(ws)->failed[blockIdx.x] = failed_flag;
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
 }
 
 // ---------------------------------------------------------------------------------------------- combine
-// Block (c, y): the item that block c of the main kernel began and did not end, if there is one; 32 rows at a time,
-// thread = row (lane) and D / 8 head dimensions (warp).
-constexpr int kCombineThreads = 256, kCombineRows = 4;
+// Block (c, y, z): the item that block c of the main kernel began and did not end, if there is one; a quarter of the head
+// dimensions (y), every other 32 rows (z); thread = row (lane) and D / 32 dimensions (warp).  What bounds it is the latency
+// of the parts' loads, which do not depend on each other.
+constexpr int kCombineThreads = 256, kCombineDims = 4, kCombineRows = 2;
 
 template <int D, bool BF16>
 __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(const __grid_constant__ AttnArgs a, void *ws) {
+    constexpr int N = D / (8 * kCombineDims);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const WorkspaceHead *head = reinterpret_cast<const WorkspaceHead *>(ws);
-    const int tid = threadIdx.x, lane = tid & 31, dims = (tid >> 5) * (D / 8);
-    if (head->error) {  // a wait ran out: no row may pass for a result
+    const int tid = threadIdx.x, lane = tid & 31, dims = (blockIdx.y * 8 + (tid >> 5)) * N;
+    const int c = blockIdx.x;
+    const Run next = head->run[c + 1];
+    const int64_t begun = head->run[c].first, all = head->run[kMaxBlocks].first;
+    if (__syncthreads_or(tid < kMaxBlocks && head->failed[tid])) {  // no row may pass for a result
         const uint32_t nan2 = 0x7fff7fffu;  // NaN in both types
-        const int64_t vecs = (int64_t)a.rows * a.q_heads * (D / 8);
-        for (int64_t i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kCombineThreads + tid; i < vecs;
-             i += (int64_t)gridDim.x * gridDim.y * kCombineThreads)
+        const int64_t vecs = (int64_t)a.rows * a.q_heads * (D / 8), blocks = (int64_t)gridDim.x * gridDim.y * gridDim.z;
+        for (int64_t i = (((int64_t)blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + c) * kCombineThreads + tid; i < vecs;
+             i += blocks * kCombineThreads)
             reinterpret_cast<uint4 *>(a.out)[i] = make_uint4(nan2, nan2, nan2, nan2);
         return;
     }
-    const int c = blockIdx.x;
-    const Run next = head->run[c + 1];
-    if (next.tile == 0 || next.count == 0 || next.first - next.tile < head->run[c].first) return;
+    if (next.first >= all || next.tile == 0 || next.first - next.tile < begun) return;
     const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
     int begin, n, len;
     attn_sequence(a, next.b, begin, n, len);
@@ -914,34 +958,39 @@ __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(cons
     while (last + 1 < kMaxBlocks && head->run[last + 1].first < end) ++last;
     const int tokens = min(n - next.pair * 2 * TQ, 2 * TQ);
     const int rows = tokens > TQ ? kPartRows : kTile;
-    for (int r0 = blockIdx.y * 32; r0 < rows; r0 += 32 * kCombineRows) {
+    // the first part lies among its block's parts that begin an item, the others among those that do not
+    const float *first = part_base(ws, c, 1, D), *rest = part_base(ws, c + 1, 0, D);
+    constexpr int64_t kStride = 2 * (int64_t)part_floats<D>();
+    const int more = last - c;
+    for (int r0 = blockIdx.z * 32; r0 < rows; r0 += 32 * kCombineRows) {
         const int r = r0 + lane, in = r & (kTile - 1);
         const int tok = (r / kTile) * TQ + in / G;
         if (in / G >= TQ || tok >= tokens) continue;
-        float m = kNegInf;
-        for (int k = c; k <= last; ++k) m = fmaxf(m, part_base(ws, k, k == c, D)[(size_t)D * kPartRows + r]);
-        float l = 0.f, o[D / 8];
+        constexpr int64_t kM = (int64_t)D * kPartRows, kL = kM + kPartRows;
+        const float m0 = first[kM + r];
+        float m = m0;
+#pragma unroll 8
+        for (int k = 0; k < more; ++k) m = fmaxf(m, rest[k * kStride + kM + r]);
+        float f = m0 == kNegInf ? 0.f : m0 == m ? 1.f : ex2(m0 - m);
+        float l = first[kL + r] * f, o[N];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) o[i] = 0.f;
-        for (int k = c; k <= last; ++k) {
-            const float *p = part_base(ws, k, k == c, D);
-            const float mk = p[(size_t)D * kPartRows + r];
-            const float f = mk == kNegInf ? 0.f : mk == m ? 1.f : ex2(mk - m);
-            l += p[(size_t)(D + 1) * kPartRows + r] * f;
+        for (int i = 0; i < N; ++i) o[i] = first[(dims + i) * kPartRows + r] * f;
+#pragma unroll 4
+        for (int k = 0; k < more; ++k) {
+            const float *p = rest + k * kStride;
+            const float mk = p[kM + r];
+            f = mk == kNegInf ? 0.f : mk == m ? 1.f : ex2(mk - m);
+            l += p[kL + r] * f;
 #pragma unroll
-            for (int i = 0; i < D / 8; ++i) o[i] += p[(size_t)(dims + i) * kPartRows + r] * f;
+            for (int i = 0; i < N; ++i) o[i] += p[(dims + i) * kPartRows + r] * f;
         }
         const int t_row = next.pair * 2 * TQ + tok;
         const bool empty = len - n + t_row + 1 <= 0;
-        const float inv = 1.f / l;
-        char *out = (char *)a.out + ((((int64_t)begin + t_row) * a.q_heads + next.h * G + in % G) * D + dims) * 2;
+        const float inv = 1.f / l;  // 0 / 0 where every score was -inf
+        uint32_t *out = reinterpret_cast<uint32_t *>(
+            (char *)a.out + ((((int64_t)begin + t_row) * a.q_heads + next.h * G + in % G) * D + dims) * 2);
 #pragma unroll
-        for (int i = 0; i < D / 8; i += 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = empty ? 0u : pack2<BF16>(o[i + 2 * j] * inv, o[i + 2 * j + 1] * inv);
-            *reinterpret_cast<uint4 *>(out + i * 2) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int i = 0; i < N; i += 2) out[i / 2] = empty ? 0u : pack2<BF16>(o[i] * inv, o[i + 1] * inv);
     }
 }
 
@@ -992,15 +1041,10 @@ cudaError_t launch_behind(void (*kernel)(KArgs...), dim3 grid, int threads, size
 template <int D, bool BF16>
 cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, void *ws, cudaStream_t stream) {
     cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D>::kSmem);
-    const size_t smem = (size_t)(a.B + 1) * 8;
-    if (e == cudaSuccess && smem > 40 * 1024)
-        e = cudaFuncSetAttribute(attention_schedule_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kAttnMaxB + 1) * 8);
-    if (e == cudaSuccess)
-        e = launch_behind(attention_schedule_kernel, dim3(1), kScheduleThreads, smem, stream, a, (WorkspaceHead *)ws);
     if (e == cudaSuccess)
         e = launch_behind(attention_tc_kernel<D, BF16>, dim3(kMaxBlocks), kThreads, (size_t)Sizes<D>::kSmem, stream, a, q, k, v, ws);
     if (e == cudaSuccess)
-        e = launch_behind(attention_combine_kernel<D, BF16>, dim3(kMaxBlocks, kCombineRows), kCombineThreads, 0, stream, a, ws);
+        e = launch_behind(attention_combine_kernel<D, BF16>, dim3(kMaxBlocks, kCombineDims, kCombineRows), kCombineThreads, 0, stream, a, ws);
     return e;
 }
 
