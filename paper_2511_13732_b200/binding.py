@@ -9,10 +9,16 @@ exception is raised.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Optional
 
 import numpy as np
+
+try:
+    import torch
+except ImportError:  # the entry points that take numpy arrays do without it
+    torch = None
 
 from . import build as _build
 
@@ -430,48 +436,53 @@ class Asg:
 
 
 # ---- the paged key/value cache of a decoding round ---------------------------------------------------------
+# These calls are made once a layer and round, on small tensors: their checks read each attribute once and allocate as
+# little as they can, since the host's time is what a small call costs.
 def _need(ok: bool, text: str):
     if not ok:
         raise ValueError(text)
 
 
-def _check_here(*tensors):
-    """CUDA tensors of the current device: the library launches there."""
-    import torch
-
-    here = None
-    for t in tensors:
-        if t is None:
-            continue
-        if here is None and t.is_cuda:
-            here = torch.cuda.current_device()
-        if here is None or t.get_device() != here:
-            raise ValueError(f"expected CUDA tensors of the current device, got one on {t.device}")
+def _device(t) -> int:
+    """The device of a call: its first tensor's, which has to be the current one (the library launches there)."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"expected CUDA tensors of the current device, got one on {t.device}")
+    return t.get_device()
 
 
-def _check_ints(n: int, *tensors):
-    import torch
-
-    for t in tensors:
-        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous()):
-            raise ValueError(f"expected a contiguous int32 tensor [{n}], got {t.dtype} {tuple(t.shape)}")
-
-
-def _row_stride(t, name: str) -> int:
-    """Elements between the tokens of [rows, heads, d] whose heads are dense (a slice of a fused projection is)."""
-    _need(t.dim() == 3, f"{name} must be [rows, heads, head_dim]")
-    n, h, d = t.shape
-    s = t.stride()
-    _need((s[2] == 1 or d == 1) and (s[1] == d or h == 1), f"{name}: a token's heads must be dense")
-    return s[0] if n > 1 else h * d
+def _int_ptr(t, shape, dev: int) -> int:
+    """Address of a contiguous int32 tensor of this shape on device `dev`."""
+    if t.dtype is not torch.int32 or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"expected a contiguous int32 tensor {tuple(shape)} on the current device, got {t.dtype} {tuple(t.shape)} "
+                         f"on {t.device}")
+    return t.data_ptr()
 
 
-def _cache_struct(k_cache, v_cache) -> _Cache:
-    _need(k_cache.dim() == 4 and k_cache.shape == v_cache.shape and k_cache.dtype == v_cache.dtype
-          and k_cache.is_contiguous() and v_cache.is_contiguous(),
-          "k_cache and v_cache must be contiguous [n_blocks, kv_heads, block_size, head_dim] of one type")
-    n, h, bs, d = k_cache.shape
-    return _Cache(n, bs, h, d, dtype_code(k_cache), k_cache.data_ptr(), v_cache.data_ptr())
+def _stream_of(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+
+
+def _packed(t, name: str, dtype, dev: int):
+    """(shape, elements between tokens) of [rows, heads, d] whose heads are dense (a slice of a fused projection is)."""
+    shape = t.shape
+    if len(shape) != 3 or t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be [rows, heads, head_dim], of the call's type and device")
+    (n, h, d), s = shape, t.stride()
+    if (s[2] != 1 and d != 1) or (s[1] != d and h != 1):
+        raise ValueError(f"{name}: a token's heads must be dense")
+    return shape, s[0] if n > 1 else h * d
+
+
+_DTYPES = {} if torch is None else {torch.bfloat16: PCG_BF16, torch.float16: PCG_F16}
+
+
+def _cache_struct(k_cache, v_cache, dev: int) -> _Cache:
+    shape = k_cache.shape
+    _need(len(shape) == 4 and v_cache.shape == shape and v_cache.dtype is k_cache.dtype and k_cache.is_contiguous()
+          and v_cache.is_contiguous() and k_cache.get_device() == dev and v_cache.get_device() == dev,
+          "k_cache and v_cache must be contiguous [n_blocks, kv_heads, block_size, head_dim] of one type, on the current device")
+    return _Cache(shape[0], shape[2], shape[1], shape[3], _DTYPES.get(k_cache.dtype) or dtype_code(k_cache), k_cache.data_ptr(),
+                  v_cache.data_ptr())
 
 
 def pcg_cache_plan(cached_len, new_len, held, block_table, free_ring, ring_state, block_size: int, rows: int,
@@ -481,62 +492,60 @@ def pcg_cache_plan(cached_len, new_len, held, block_table, free_ring, ring_state
     ``accept_len`` is what ``pcg_verify`` returned for the last round (None: every cached token stays).  Writes new
     entries of ``block_table`` [B, max_blocks] and released blocks of ``free_ring`` in place; everything else comes
     back in a ``CachePlan`` (``out`` optionally supplies it; its tensors may not be those of the inputs)."""
-    import torch
-
+    dev = _device(cached_len)
     B = cached_len.shape[0]
-    _check_ints(B, cached_len, new_len, held, accept_len)
-    _check_ints(2, ring_state)
-    _check_ints(free_ring.shape[0], free_ring)
-    _need(block_table.dim() == 2 and block_table.shape[0] == B and block_table.dtype == torch.int32
-          and block_table.is_contiguous(), "block_table must be a contiguous int32 tensor [B, max_blocks]")
+    one = (B,)
+    _need(block_table.dim() == 2 and free_ring.dim() == 1, "block_table must be [B, max_blocks], free_ring [ring_size]")
+    max_blocks, ring_size = block_table.shape[1], free_ring.shape[0]
+    args = (B, _int_ptr(cached_len, one, dev), None if accept_len is None else _int_ptr(accept_len, one, dev),
+            _int_ptr(new_len, one, dev), _int_ptr(held, one, dev), block_size, max_blocks,
+            _int_ptr(block_table, (B, max_blocks), dev), _int_ptr(free_ring, (ring_size,), dev), ring_size,
+            _int_ptr(ring_state, (2,), dev), rows)
+    sizes = (B, B, B, B + 1, rows, rows, 2, B)
     if out is None:
-        sizes = (B, B, B, B + 1, rows, rows, 2, B)
-        out = CachePlan(*torch.empty(sum(sizes), dtype=torch.int32, device=cached_len.device).split(sizes))
+        buf = cached_len.new_empty(5 * B + 2 * rows + 3)
+        p = buf.data_ptr()
+        ptrs = []
+        for n in sizes:
+            ptrs.append(p)
+            p += 4 * n
+        out = CachePlan(*torch.split_with_sizes(buf, sizes))
     else:
-        _check_ints(B, out.cached_len, out.kv_len, out.held, out.flags)
-        _check_ints(B + 1, out.row_start)
-        _check_ints(rows, out.slots, out.positions)
-        _check_ints(2, out.ring_state)
-    _check_here(cached_len, new_len, held, accept_len, block_table, free_ring, ring_state, *out)
-    _check(load().pcg_cache_plan(B, cached_len.data_ptr(), None if accept_len is None else accept_len.data_ptr(),
-                                 new_len.data_ptr(), held.data_ptr(), block_size, block_table.shape[1],
-                                 block_table.data_ptr(), free_ring.data_ptr(), free_ring.shape[0], ring_state.data_ptr(),
-                                 rows, *(None if t is None else t.data_ptr() for t in out), _stream_ptr(stream)))
+        ptrs = [None if t is None else _int_ptr(t, (n,), dev) for t, n in zip(out, sizes)]
+    _check((_lib or load()).pcg_cache_plan(*args, *ptrs, _stream_of(stream, dev)))
     return out
 
 
 def pcg_cache_append(k, v, slots, k_cache, v_cache, stream=None):
     """``pcg_cache_append``: the keys and values [rows, kv_heads, head_dim] of new tokens into the cache's slots."""
-    cache = _cache_struct(k_cache, v_cache)
-    rows = k.shape[0]
-    ks, vs = _row_stride(k, "k"), _row_stride(v, "v")
-    _need(k.shape == v.shape and k.shape[1:] == (cache.kv_heads, cache.head_dim) and k.dtype == v.dtype == k_cache.dtype,
-          "k and v must be [rows, kv_heads, head_dim] of the cache's type")
-    _check_ints(rows, slots)
-    _check_here(k, v, slots, k_cache, v_cache)
-    _check(load().pcg_cache_append(k.data_ptr(), ks, v.data_ptr(), vs, rows, slots.data_ptr(), ctypes.byref(cache),
-                                   _stream_ptr(stream)))
+    dev = _device(k)
+    cache = _cache_struct(k_cache, v_cache, dev)
+    shape, ks = _packed(k, "k", k_cache.dtype, dev)
+    vshape, vs = _packed(v, "v", k_cache.dtype, dev)
+    _need(shape == vshape and shape[1] == cache.kv_heads and shape[2] == cache.head_dim,
+          "k and v must be [rows, kv_heads, head_dim] of the cache")
+    _check((_lib or load()).pcg_cache_append(k.data_ptr(), ks, v.data_ptr(), vs, shape[0], _int_ptr(slots, shape[:1], dev),
+                                             ctypes.byref(cache), _stream_of(stream, dev)))
     return k_cache, v_cache
 
 
+@functools.lru_cache(maxsize=256)
 def pcg_attention_workspace_bytes(B: int, q_heads: int, kv_heads: int, head_dim: int, dtype: int) -> int:
     return int(load().pcg_attention_workspace_bytes(B, q_heads, kv_heads, head_dim, dtype))
 
 
-def _attention_buffers(q, row_start, kv_heads, out, workspace):
-    import torch
-
-    rows, q_heads, d = q.shape
-    B = row_start.shape[0] - 1
-    _check_ints(max(B, 0) + 1, row_start)
+def _attention_buffers(q, shape, out, workspace, B, kv_heads, dtype, dev):
     if out is None:
-        out = torch.empty((rows, q_heads, d), dtype=q.dtype, device=q.device)
+        out = q.new_empty(shape)
     else:
-        _need(out.shape == q.shape and out.dtype == q.dtype and out.is_contiguous(), "out must be contiguous, of q's shape and type")
+        _need(out.shape == shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == dev,
+              "out must be contiguous, of q's shape, type and device")
     if workspace is None:
-        need = pcg_attention_workspace_bytes(B, q_heads, kv_heads, d, dtype_code(q))
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    return B, out, workspace
+        need = pcg_attention_workspace_bytes(B, shape[1], kv_heads, shape[2], dtype)
+        workspace = q.new_empty(need, dtype=torch.uint8)
+    else:
+        _need(workspace.get_device() == dev and workspace.is_contiguous(), "workspace must be contiguous, on the current device")
+    return out, workspace
 
 
 def pcg_cache_attention(q, row_start, kv_len, block_table, k_cache, v_cache, scale: Optional[float] = None, out=None,
@@ -546,33 +555,34 @@ def pcg_cache_attention(q, row_start, kv_len, block_table, k_cache, v_cache, sca
 
     ``scale`` defaults to 1 / sqrt(head_dim).  ``workspace`` is a uint8 CUDA tensor of at least
     ``pcg_attention_workspace_bytes`` bytes (allocated here if omitted)."""
-    import torch
-
-    cache = _cache_struct(k_cache, v_cache)
-    stride = _row_stride(q, "q")
-    _need(q.shape[2] == cache.head_dim and q.dtype == k_cache.dtype, "q must have the cache's head_dim and type")
-    B, out, workspace = _attention_buffers(q, row_start, cache.kv_heads, out, workspace)
-    _check_ints(B, kv_len)
-    _need(block_table.dim() == 2 and block_table.shape[0] == B and block_table.dtype == torch.int32
-          and block_table.is_contiguous(), "block_table must be a contiguous int32 tensor [B, max_blocks]")
-    _check_here(q, row_start, kv_len, block_table, k_cache, v_cache, out, workspace)
-    _check(load().pcg_cache_attention(q.data_ptr(), stride, q.shape[0], q.shape[1], row_start.data_ptr(), kv_len.data_ptr(),
-                                      block_table.data_ptr(), B, block_table.shape[1], ctypes.byref(cache),
-                                      q.shape[2] ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    dev = _device(q)
+    cache = _cache_struct(k_cache, v_cache, dev)
+    shape, stride = _packed(q, "q", k_cache.dtype, dev)
+    _need(shape[2] == cache.head_dim and block_table.dim() == 2 and row_start.dim() == 1,
+          "q must have the cache's head_dim, block_table be [B, max_blocks], row_start [B + 1]")
+    B, max_blocks = block_table.shape
+    out, workspace = _attention_buffers(q, shape, out, workspace, B, cache.kv_heads, cache.dtype, dev)
+    _check((_lib or load()).pcg_cache_attention(
+        q.data_ptr(), stride, shape[0], shape[1], _int_ptr(row_start, (B + 1,), dev), _int_ptr(kv_len, (B,), dev),
+        _int_ptr(block_table, (B, max_blocks), dev), B, max_blocks, ctypes.byref(cache),
+        shape[2] ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
+        workspace.numel() * workspace.element_size(), _stream_of(stream, dev)))
     return out
 
 
 def pcg_prompt_attention(q, k, v, row_start, scale: Optional[float] = None, out=None, workspace=None, stream=None):
     """``pcg_prompt_attention``: causal attention of whole prompts packed one after the other; q [rows, q_heads,
     head_dim], k and v [rows, kv_heads, head_dim] (slices of a fused projection will do), row_start [B + 1]."""
-    qs, ks, vs = _row_stride(q, "q"), _row_stride(k, "k"), _row_stride(v, "v")
-    _need(k.shape == v.shape and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2] and q.dtype == k.dtype == v.dtype,
-          "k and v must be [rows, kv_heads, head_dim] with q's rows, head_dim and type")
-    B, out, workspace = _attention_buffers(q, row_start, k.shape[1], out, workspace)
-    _check_here(q, k, v, row_start, out, workspace)
-    _check(load().pcg_prompt_attention(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dtype_code(q), q.shape[0],
-                                       q.shape[1], k.shape[1], q.shape[2], row_start.data_ptr(), B,
-                                       q.shape[2] ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
-                                       workspace.numel() * workspace.element_size(), _stream_ptr(stream)))
+    dev = _device(q)
+    shape, qs = _packed(q, "q", q.dtype, dev)
+    kshape, ks = _packed(k, "k", q.dtype, dev)
+    vshape, vs = _packed(v, "v", q.dtype, dev)
+    _need(kshape == vshape and kshape[0] == shape[0] and kshape[2] == shape[2] and row_start.dim() == 1 and row_start.shape[0] > 0,
+          "k and v must be [rows, kv_heads, head_dim] with q's rows and head_dim, row_start [B + 1]")
+    B, dtype = row_start.shape[0] - 1, _DTYPES.get(q.dtype) or dtype_code(q)
+    out, workspace = _attention_buffers(q, shape, out, workspace, B, kshape[1], dtype, dev)
+    _check((_lib or load()).pcg_prompt_attention(
+        q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dtype, shape[0], shape[1], kshape[1], shape[2],
+        _int_ptr(row_start, (B + 1,), dev), B, shape[2] ** -0.5 if scale is None else scale, out.data_ptr(),
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(stream, dev)))
     return out

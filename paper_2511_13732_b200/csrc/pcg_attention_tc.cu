@@ -26,6 +26,8 @@
 #include <cuda.h>  // CUtensorMap and its enums only; the encoder is fetched through the runtime, not linked
 #include <cuda_bf16.h>
 
+#include <atomic>
+
 #include "pcg_attention.cuh"
 
 namespace pcg {
@@ -34,7 +36,6 @@ constexpr int kTile = 128;       // rows of a row tile = lanes of tensor memory;
 constexpr int kMaxBlocks = 148;  // blocks of the main kernel: one per SM of a B200 (more or fewer SMs only change the pace)
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
-constexpr int kFmaShare = 10;    // of 32 weights, how many are computed on the FMA pipes
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
 
 // ---------------------------------------------------------------------------------------------- workspace
@@ -402,46 +403,18 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
     return r;
 }
 
-// 2^x of two values on the FMA pipes, for x <= 16 and finite, or -inf (which gives 2^-126): the special-function unit makes
-// 16 a clock and SM, which is half of what the tensor cores could use, so that some of a tile's weights come from here.
-// Cody and Waite's reduction, x = n + f with n = round(x) by adding 1.5 * 2^23, and a polynomial of degree 4 for 2^f on
-// [-1/2, 1/2], fitted by Remez' exchange to the least relative error: 2.7e-6 in fp32.
-__device__ __forceinline__ uint64_t exp2_fma(uint64_t x) {
-    constexpr float kRound = 12582912.f;
-    float a, b;
-    unpair(x, a, b);
-    x = pair(fmaxf(a, -126.f), fmaxf(b, -126.f));
-    const uint64_t r = add2(x, pair(kRound, kRound));
-    const uint64_t n = add2(r, pair(-kRound, -kRound));
-    const uint64_t f = fma2(n, pair(-1.f, -1.f), x);
-    uint64_t y = fma2(f, pair(0.009570102207362652f, 0.009570102207362652f), pair(0.05591785907745361f, 0.05591785907745361f));
-    y = fma2(f, y, pair(0.240247443318367f, 0.240247443318367f));
-    y = fma2(f, y, pair(0.6931217908859253f, 0.6931217908859253f));
-    y = fma2(f, y, pair(0.9999992847442627f, 0.9999992847442627f));
-    float ra, rb, ya, yb;
-    unpair(r, ra, rb);
-    unpair(y, ya, yb);
-    return pair(__uint_as_float((__float_as_uint(ra) << 23) + __float_as_uint(ya)),
-                __uint_as_float((__float_as_uint(rb) << 23) + __float_as_uint(yb)));
-}
-
-// 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs.  kFmaShare of them by exp2_fma.
+// 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs.  All by the special-function unit: with
+// 6, 10, 13 or 16 of 32 computed by a polynomial on the FMA pipes a prompt of 8192 tokens took 2 to 9 % longer, since a
+// tile's time is the latency of its steps rather than the unit's rate.
 template <bool BF16>
 __device__ __forceinline__ void weights(const uint32_t *v, uint64_t scale, uint64_t shift, uint64_t (&sum)[4], uint32_t *p) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        uint64_t x = fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale, shift);
         float a, b;
-        if ((i * kFmaShare) % 32 < kFmaShare) {
-            x = exp2_fma(x);
-            unpair(x, a, b);
-        } else {
-            unpair(x, a, b);
-            a = ex2(a);
-            b = ex2(b);
-            x = pair(a, b);
-        }
-        sum[i & 3] = add2(sum[i & 3], x);
+        unpair(fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale, shift), a, b);
+        a = ex2(a);
+        b = ex2(b);
+        sum[i & 3] = add2(sum[i & 3], pair(a, b));
         p[i] = pack2<BF16>(a, b);
     }
 }
@@ -620,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         }
                         m = mnew;
                     }
-                    // a row that has met no score above -inf yet weighs everything 0 (or 2^-126: its sums are dropped)
+                    // a row that has met no score above -inf yet weighs everything 0
                     const float by = (m == kNegInf ? 0.f : -m) + kLift;
                     const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), by2 = pair(by, by);
                     uint64_t sum[4] = {0, 0, 0, 0};
@@ -694,8 +667,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     m = mx;
                 }
                 const bool whole = g.t0 == 0 && g.nt == g.tiles;
-                // a row that sees no key is 0 (below); one that sees scores of -inf alone is NaN, as 0 / 0 is
-                const float inv = m == kNegInf ? __int_as_float(0x7fffffff) : 1.f / l;
+                // a row that sees no key is 0 (below); one that sees scores of -inf alone is 0 / 0 = NaN
+                const float inv = 1.f / l;
                 char *out = (char *)a.out + (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2);
                 const bool wide = ((uintptr_t)a.out & 31) == 0;
                 const int prow = (g.two ? slot * kTile : 0) + row;
@@ -1040,7 +1013,13 @@ cudaError_t launch_behind(void (*kernel)(KArgs...), dim3 grid, int threads, size
 
 template <int D, bool BF16>
 cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &k, const CUtensorMap &v, void *ws, cudaStream_t stream) {
-    cudaError_t e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D>::kSmem);
+    static std::atomic<uint64_t> prepared{0};  // devices whose kernel has been given its shared memory
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (dev > 63 || !(prepared.load(std::memory_order_relaxed) >> dev & 1))) {
+        e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D>::kSmem);
+        if (e == cudaSuccess && dev <= 63) prepared.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
     if (e == cudaSuccess)
         e = launch_behind(attention_tc_kernel<D, BF16>, dim3(kMaxBlocks), kThreads, (size_t)Sizes<D>::kSmem, stream, a, q, k, v, ws);
     if (e == cudaSuccess)
