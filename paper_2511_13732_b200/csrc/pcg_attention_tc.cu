@@ -3,15 +3,17 @@
 // The rows of one key head -- G = q_heads / kv_heads query heads for each of a sequence's new tokens -- are packed
 // token by token into tiles of 128 rows (TQ = 128 / G tokens), so that a key or value is fetched once for the heads that
 // share it and a drafted chunk's few tokens fill as much of a tile as there is.  An ITEM is a (sequence, key head, pair of
-// row tiles); it meets its keys 128 at a time (a KEY TILE).  A block works on an item with two SLOTS, each a warpgroup
-// with its own scores and its own output accumulator in tensor memory:
-//   two row tiles (chunks of prompts):      slot s has row tile s, and every key tile goes to both;
-//   one row tile (tokens, drafted chunks):  both slots have that row tile and take the key tiles in turn, so that one
-//                                           slot's softmax runs under the other's products; their sums meet at the end.
-//
+// row tiles).  A block works on an item with two SLOTS, each a warpgroup with its own scores and its own output accumulator
+// in tensor memory:
+//   two row tiles (chunks of prompts):      key tiles of 128 keys; slot s has row tile s, and every key tile goes to both.
+//                                           Bound by the products, and by the softmax between them.
+//   one row tile (tokens, drafted chunks):  key tiles of 64 keys; both slots have that row tile and take the key tiles in
+//                                           turn, and their sums meet at the end.  Bound by HBM: a stage of the ring waits
+//                                           for its tile's softmax, so that half as large a tile leaves more of the ring
+//                                           for tiles that are on their way.
 // attention_tc_kernel        Every block first cuts the call's work into one equal run per block, whatever the lengths are:
-//                            it numbers the units of all items, a unit for each key tile and two for what an item costs
-//                            beside its key tiles, and looks up where its own run begins and ends.  No block waits for
+//                            it numbers the units of all items, one for each 64 keys and four for what an item costs
+//                            beside its keys, and looks up where its own run begins and ends.  No block waits for
 //                            another, and an item may be shared.  Then 8 softmax warps (two slots), a warp that fetches
 //                            (TMA) and a warp that issues tcgen05.mma go through the run.  An item that a block has to
 //                            itself is written out; a part of one goes to the workspace as an unscaled sum with its
@@ -32,7 +34,8 @@
 
 namespace pcg {
 
-constexpr int kTile = 128;       // rows of a row tile = lanes of tensor memory; keys of a key tile
+constexpr int kTile = 128;       // rows of a row tile = lanes of tensor memory; keys of a key tile of an item with two
+constexpr int kHalf = 64;        // keys of a key tile of an item with one row tile; rows of one copy at the most
 constexpr int kMaxBlocks = 148;  // blocks of the main kernel: one per SM of a B200 (more or fewer SMs only change the pace)
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
@@ -40,11 +43,11 @@ constexpr float kSlack = 8.f;    // the reference may lag the maximum by a facto
 
 // ---------------------------------------------------------------------------------------------- workspace
 struct Run {        // one block's key tiles
-    int64_t first;  // number of its first key tile among those of the call
-    int32_t b, h, pair, tile;  // where that is
+    int64_t first;  // number of its first 64 keys among those of the call
+    int32_t b, h, pair, tile;  // where that is (tile: in 64 keys)
 };
 struct WorkspaceHead {
-    Run run[kMaxBlocks + 1];     // the last begins behind the last key tile
+    Run run[kMaxBlocks + 1];     // the last begins behind the last keys
     int32_t failed[kMaxBlocks];  // set where a bounded wait ran out: the call's outputs are then NaN
 };
 // Partial sums: [block][2: a part that does not begin its item, one that does][2 * 128 rows], D sums each stored
@@ -62,10 +65,11 @@ __device__ __forceinline__ float *part_base(void *ws, int block, int which, int 
 
 // ---------------------------------------------------------------------------------------------- items
 __host__ __device__ __forceinline__ int pairs_of(int n, int TQ) { return (n + 2 * TQ - 1) / (2 * TQ); }
-// Key tiles of pair p: up to what its last row sees, and one where it sees nothing.
+// Keys of pair p in units of 64: up to what its last row sees, in whole key tiles, and one of them where it sees nothing.
 __device__ __forceinline__ int tiles_of(int n, int len, int TQ, int p) {
-    const int lim = len - n + min((p + 1) * 2 * TQ, n);
-    return lim <= kTile ? 1 : (lim + kTile - 1) / kTile;
+    const int tokens = min(n - p * 2 * TQ, 2 * TQ), lim = len - n + p * 2 * TQ + tokens;
+    if (tokens > TQ) return lim <= kTile ? 2 : (lim + kTile - 1) / kTile * 2;
+    return lim <= kHalf ? 1 : (lim + kHalf - 1) / kHalf;
 }
 
 // Sum over 0 <= i < n of floor((a i + b) / 128), a, b >= 0: Euclid's steps on a and the divisor, the first of them by
@@ -93,7 +97,7 @@ __device__ __forceinline__ int64_t floor_sum_128(uint32_t n, uint32_t a, int64_t
     }
     return s;
 }
-// Key tiles of a sequence's first p pairs.
+// The same of a sequence's first p pairs together.
 __device__ int64_t tiles_before(int n, int len, int TQ, int p) {
     const int step = 2 * TQ, whole = n / step, q = min(p, whole);  // `whole` pairs of 2 * TQ tokens, then one of fewer
     // pairs whose last row sees at most one tile of keys count 1 each: (i + 1) * step <= 128 - (len - n)
@@ -101,15 +105,16 @@ __device__ int64_t tiles_before(int n, int len, int TQ, int p) {
     const int head = base >= kTile ? 0 : (int)min((int64_t)q, (kTile - (int64_t)base) / step);
     int64_t s = head;
     if (q > head) s += floor_sum_128(q - head, step, base + (int64_t)(head + 1) * step + kTile - 1);
+    s *= 2;
     if (p > whole) s += tiles_of(n, len, TQ, whole);
     return s;
 }
 
 // ---------------------------------------------------------------------------------------------- the cut
-// What an item costs beside its key tiles (fetching queries, the first and the last tile's latency, writing out), in units
-// of a key tile: measured at 6,500 to 7,800 cycles for 3,500 a key tile.  Blocks get at least kLeast units: fewer, and a
+// What an item costs beside its keys (fetching queries, the first and the last tile's latency, writing out), in units of 64
+// keys: measured at 6,500 to 7,800 cycles for 3,500 a key tile of 128.  Blocks get at least kLeast units: fewer, and a
 // short call's parts cost more to join than they save.
-constexpr int kItemUnits = 2, kLeast = 4;
+constexpr int kItemUnits = 4, kLeast = 8;
 
 // By all threads of the block: where runs `block` and `block + 1` begin, to out[0] and out[1].  `scratch` holds B
 // int64_t and B int32_t (192 KB of shared memory at the most).
@@ -159,9 +164,9 @@ __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int64_t *w
         items[b] += (int32_t)ibase;
     }
     __syncthreads();
-    if (lane == 0 && warp < 2) {
+    if (warp < 2) {  // a warp for each of the two
         const int blocks = (int)max((int64_t)1, min((int64_t)kMaxBlocks, total / kLeast)), c = blockIdx.x + warp;
-        Run r{total - (int64_t)kItemUnits * a.kv_heads * all_items, 0, 0, 0, 0};  // behind the last key tile
+        Run r{total - (int64_t)kItemUnits * a.kv_heads * all_items, 0, 0, 0, 0};  // behind the last keys
         const int64_t u = c >= blocks ? total : total / blocks * c + total % blocks * c / blocks;
         if (u < total) {
             int x = 0, y = B - 1;  // the last sequence whose units begin at or before u: empty ones share their number
@@ -179,24 +184,28 @@ __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int64_t *w
             const int64_t per_head = tiles + (int64_t)kItemUnits * pairs, in = u - units[x];
             const int h = (int)(in / per_head);
             const int64_t rest = in - h * per_head;
-            int p = 0, q = pairs - 1;
-            while (p < q) {
-                const int mid = (p + q + 1) >> 1;
-                if (tiles_before(n, len, TQ, mid) + (int64_t)kItemUnits * mid <= rest)
-                    p = mid;
-                else
-                    q = mid - 1;
+            // the pair: of [p, p + count) in steps of a 32nd, by the lanes
+            int p = 0, count = pairs;
+            int64_t head_tiles = 0;
+            while (count > 1) {
+                const int step = (count + 31) / 32, mine = p + lane * step;
+                const int64_t before = lane * step < count && mine > 0 ? tiles_before(n, len, TQ, mine) : 0;
+                const bool below = lane * step < count && before + (int64_t)kItemUnits * mine <= rest;
+                const int top = 31 - __clz(__ballot_sync(0xffffffffu, below));  // lane 0's always is
+                head_tiles = __shfl_sync(0xffffffffu, before, top);
+                count = min(step, count - top * step);
+                p += top * step;
             }
-            const int64_t head_tiles = p == 0 ? 0 : tiles_before(n, len, TQ, p);
             // an item's own units come first: a cut within them leaves the whole item to the run behind it
-            const int64_t tile = max((int64_t)0, rest - head_tiles - (int64_t)kItemUnits * p - kItemUnits);
+            int64_t tile = max((int64_t)0, rest - head_tiles - (int64_t)kItemUnits * p - kItemUnits);
+            if (n - p * 2 * TQ > TQ) tile &= ~(int64_t)1;  // a whole key tile
             r.first = units[x] - (int64_t)kItemUnits * a.kv_heads * items[x] + h * tiles + head_tiles + tile;
             r.b = x;
             r.h = h;
             r.pair = p;
             r.tile = (int)tile;
         }
-        out[warp] = r;
+        if (lane == 0) out[warp] = r;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // copies land in the scratch's place
     __syncthreads();
@@ -205,8 +214,9 @@ __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int64_t *w
 // A block's run of units, item by item: the same walk in every role.
 struct Segment {
     int b, h, pair, begin, n, len;
-    int tiles, t0, nt;  // key tiles of the item, the first of this part, how many
-    bool two;           // two row tiles
+    int t0, nt;   // the first key tile of this part, how many
+    bool whole;   // the part is the item
+    bool two;     // two row tiles, key tiles of 128 keys; else of 64
 };
 struct Walk {
     int b, h, pair, tile, left;
@@ -227,11 +237,12 @@ struct Walk {
         s.begin = begin;
         s.n = n;
         s.len = len;
-        s.tiles = tiles_of(n, len, TQ, pair);
-        s.t0 = tile;
-        s.nt = min(left, s.tiles - tile);
         s.two = n - pair * 2 * TQ > TQ;
-        left -= s.nt;
+        const int all = tiles_of(n, len, TQ, pair), nt = min(left, all - tile);
+        s.whole = nt == all;
+        s.t0 = s.two ? tile >> 1 : tile;
+        s.nt = s.two ? max(nt >> 1, 1) : nt;
+        left -= nt;
         tile = 0;
         if (left > 0 && ++pair == pairs_of(n, TQ)) {
             pair = 0;
@@ -308,10 +319,10 @@ __device__ __forceinline__ uint64_t desc_k(uint32_t addr) {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 // MN-major (values: rows are keys, the product's inner index; 64 head dimensions a row): blocks of 64 head dimensions
-// 128 * 128 bytes apart (leading offset), groups of 8 keys 1024 bytes apart (stride offset).
-__device__ __forceinline__ uint64_t desc_mn(uint32_t addr) {
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)((kTile * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
-           (1ull << 46) | (2ull << 61);
+// `keys` * 128 bytes apart (leading offset), groups of 8 keys 1024 bytes apart (stride offset).
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, int keys) {
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | ((uint64_t)((keys * 128) >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -433,7 +444,8 @@ __device__ __forceinline__ void store_row(void *p, const uint32_t (&w)[8], bool 
 template <int D>
 struct Sizes {
     static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
-    static constexpr int kStages = D == 128 ? 5 : 10;        // ring of key and value tiles: 160 KB
+    // Ring, 160 KB: a stage holds 128 keys or their values, or 64 keys and then their values, each as D / 64 parts.
+    static constexpr int kStages = D == 128 ? 5 : 10;
     static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;  // room to start on a 1024-byte boundary
     static_assert((2 + kStages) * kTileBytes >= kAttnMaxB * 12, "the cut's scratch");
 };
@@ -446,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // instruction descriptors: D = fp32, A and B of one 16-bit type, M = 128; N = 128 keys, B K-major; N = D, B MN-major
     constexpr uint32_t kType = BF16 ? (1u << 7) | (1u << 10) : 0u;
     constexpr uint32_t kIdescQK = (1u << 4) | kType | ((kTile >> 3) << 17) | ((kTile >> 4) << 24);
+    constexpr uint32_t kIdescQKHalf = (1u << 4) | kType | ((kHalf >> 3) << 17) | ((kTile >> 4) << 24);  // N = 64 keys
     constexpr uint32_t kIdescPV = (1u << 4) | kType | (1u << 16) | ((D >> 3) << 17) | ((kTile >> 4) << 24);
     // float16's weights are kept 2^7 higher than the reference says, out of the range where they lose bits: 2^8 above the
     // reference is then 2^15 at most.  The sums carry the same factor, so it cancels.
@@ -485,6 +498,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
     }
+    if (tid < 3 * 32 && lane == 0)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(warp == 0 ? &qmap : warp == 1 ? &kmap : &vmap)) : "memory");
     fence_before();
     __syncthreads();
     fence_after();
@@ -521,21 +536,21 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ok = __all_sync(0xffffffffu, bar_wait(s_full(slot), sn & 1, failed));
                 if (!ok) break;
                 fence_after();
-                const int k0 = (g.t0 + t) * kTile;
-                if (t == g.nt - 1 && k0 + kTile > g.len && (!g.two || slot == 0)) {
+                const int keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
+                if (t == g.nt - 1 && k0 + keys > g.len && (!g.two || slot == 0)) {
                     // Values behind the sequence's last token may hold anything, and 0 * NaN is NaN: they are zeroed
                     // where they lie.  This stage is the last of the part; the slot's weights are announced after it, and
                     // slot 1's product comes behind slot 0's.
-                    const uint32_t i = loads + 2 * g.nt - 1;
+                    const uint32_t i = loads + (g.two ? 2 * g.nt : g.nt) - 1;
                     ok = __all_sync(0xffffffffu, bar_wait(full_bar(i % S), (i / S) & 1, failed));
                     if (!ok) break;
-                    if (k0 + row >= g.len) {
-                        const uint32_t at = ring + (i % S) * kTileBytes + row * 128;
-#pragma unroll
+                    if (row < keys && k0 + row >= g.len) {
+                        const uint32_t at = ring + (i % S) * kTileBytes + (g.two ? 0 : kTileBytes / 2) + row * 128;
+#pragma unroll 1
                         for (int part = 0; part < kParts; ++part)
 #pragma unroll
                             for (int c = 0; c < 8; ++c)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + part * (kTile * 128) + c * 16), "r"(0u)
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + part * (keys * 128) + c * 16), "r"(0u)
                                              : "memory");
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -543,34 +558,37 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (warp_valid) {
                     uint32_t v[64];
                     float top[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
-                    const bool masked = __any_sync(0xffffffffu, lim < k0 + kTile);
+                    const bool masked = __any_sync(0xffffffffu, lim < k0 + keys);
                     const int seen = lim - k0;
                     auto mask = [&](int from) {
 #pragma unroll
                         for (int c = 0; c < 64; ++c)
                             if (from + c >= seen) v[c] = __float_as_uint(kNegInf);
                     };
-                    {
+                    tmem_ld32(sc, v);
+                    tmem_ld32(sc + 32, v + 32);
+                    if (g.two) {
                         uint32_t u[64];
-                        tmem_ld32(sc, v);
-                        tmem_ld32(sc + 32, v + 32);
                         tmem_ld32(sc + 64, u);
                         tmem_ld32(sc + 96, u + 32);
                         tmem_wait_ld();
-                        tmem_loaded<64>(v);
                         tmem_loaded<64>(u);
                         if (masked) {
-                            mask(0);
 #pragma unroll
                             for (int c = 0; c < 64; ++c)
                                 if (64 + c >= seen) u[c] = __float_as_uint(kNegInf);
                         }
 #pragma unroll
-                        for (int c = 0; c < 64; c += 2) {
-                            top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                        for (int c = 0; c < 64; c += 2)
                             top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(u[c]), __uint_as_float(u[c + 1]));
-                        }
+                    } else {
+                        tmem_wait_ld();
                     }
+                    tmem_loaded<64>(v);
+                    if (masked) mask(0);
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2)
+                        top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
                     const float mt = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * a.scale_log2;
                     bad = bad || !(mt < -kNegInf);
                     // also when the first score above -inf is met; a row's reference depends on its own scores alone, and
@@ -602,7 +620,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // loop of two turns keeps the code in the instruction cache, which 128 scores in line do not fit.  (The
                     // first half's weights lie where its own scores were.)
 #pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < (g.two ? 2 : 1); ++h) {
                         uint32_t p[32];
                         if (h) {
                             tmem_wait_ld();
@@ -610,12 +628,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (masked) mask(64);
                         }
                         weights<BF16>(v, scale2, by2, sum, p);
-                        if (!h) tmem_ld32(sc + 64, v);
+                        if (!h && g.two) tmem_ld32(sc + 64, v);
                         weights<BF16>(v + 32, scale2, by2, sum, p + 16);
-                        if (!h) tmem_ld32(sc + 96, v + 32);
+                        if (!h && g.two) tmem_ld32(sc + 96, v + 32);
                         tmem_st32(sc + h * 32, p);
                         tmem_wait_st();
-                        if (!h) {
+                        if (!h && g.two) {
                             fence_before();
                             __syncwarp();
                             if (lane == 0) bar_arrive(p_half(slot));
@@ -624,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     float s0, s1;
                     unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
                     l += s0 + s1;
-                } else {
+                } else if (g.two) {
                     __syncwarp();
                     if (lane == 0) bar_arrive(p_half(slot));
                 }
@@ -634,7 +652,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (bad) l = __int_as_float(0x7fffffff);  // a score of +inf or NaN
             if (!ok) break;
-            loads += 2 * g.nt;
+            loads += g.two ? 2 * g.nt : g.nt;
             // ---- end of the part
             const bool mine = first < g.nt;                    // this slot has had a key tile
             const bool shared = !g.two && g.nt > 1;            // both have, of one row tile
@@ -666,7 +684,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                     l = l * f0 + l1 * f1;
                     m = mx;
                 }
-                const bool whole = g.t0 == 0 && g.nt == g.tiles;
                 // a row that sees no key is 0 (below); one that sees scores of -inf alone is 0 / 0 = NaN
                 const float inv = 1.f / l;
                 char *out = (char *)a.out + (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2);
@@ -688,7 +705,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (int i = 0; i < 32; ++i)
                             o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
                     }
-                    if (valid && whole) {
+                    if (valid && g.whole) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 16) {
                             uint32_t w[8];
@@ -704,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     __syncwarp();  // the next columns are read by the whole warp
                 }
-                if (valid && !whole) {
+                if (valid && !g.whole) {
                     part[(size_t)D * kPartRows + prow] = m;
                     part[(size_t)(D + 1) * kPartRows + prow] = l;
                 }
@@ -718,48 +735,58 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else if (warp == kSoftmaxWarps) {
         // ------------------------------------------------------------------ fetch: a lane per page looks its block up, one issues
         const bool paged = a.kv_len != nullptr;
-        const int box = paged ? min(1 << a.bs_shift, kTile) : kTile;  // rows of one copy
-        const int copies = kTile / box;
+        const int box = paged ? min(1 << a.bs_shift, kHalf) : kHalf;  // rows of one copy
         uint32_t it = 0, stage = 0, stage_phase = 1, items = 0;  // a stage's first fill waits for nothing: parity 1 has passed
         bool ok = true;
-        while (ok && walk.next(a, TQ, g)) {
-            auto page_of = [&](int t) -> int32_t {  // the block of key tile t's rows from lane * box on
-                const int p = (g.t0 + t) * kTile + lane * box;
-                if (!paged || lane >= copies || t >= g.nt || p >= g.len) return -1;
-                const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
-                return block < 0 || block >= a.n_blocks ? a.n_blocks : block;  // behind the tensor: reads zeros
-            };
-            auto fetch = [&](const CUtensorMap *map, int t, int32_t page) -> bool {
-                const uint32_t s = stage;
-                if (!__all_sync(0xffffffffu, bar_wait(empty_bar(s), stage_phase, failed))) return false;
-                if (++stage == S) {
-                    stage = 0;
-                    stage_phase ^= 1;
-                }
-                const int k0 = (g.t0 + t) * kTile;
-                // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
-                const int n_copies = paged ? min(copies, (max(g.len - k0, 0) + box - 1) / box) : 1;
-                for (int c = 0; c < n_copies; ++c) {
-                    const int32_t block = __shfl_sync(0xffffffffu, page, c);
-                    if (elect_one()) {
-                        if (c == 0) bar_expect(full_bar(s), n_copies * box * D * 2);
-                        const uint32_t dst = ring + s * kTileBytes + c * box * 128;
-                        const int r = k0 + c * box;
+        auto page_of = [&](const Segment &g, int t) -> int32_t {  // the block of key tile t's rows from lane * box on
+            const int p = (g.t0 + t) * (g.two ? kTile : kHalf) + lane * box;
+            if (!paged || lane >= 8 || t >= g.nt || p >= g.len) return -1;
+            const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
+            return block < 0 || block >= a.n_blocks ? a.n_blocks : block;  // behind the tensor: reads zeros
+        };
+        // The next stage, once it has been read: `keys` rows of one of the tensors, or of both, one behind the other.
+        auto fetch = [&](const CUtensorMap *map, const CUtensorMap *second, int t, int32_t page) {
+            const uint32_t s = stage;
+            ok = ok && __all_sync(0xffffffffu, bar_wait(empty_bar(s), stage_phase, failed));
+            if (!ok) return;
+            if (++stage == S) {
+                stage = 0;
+                stage_phase ^= 1;
+            }
+            const int keys = second ? kHalf : kTile, k0 = (g.t0 + t) * keys;
+            // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
+            const int copies = min(keys / box, (max(g.len - k0, 0) + box - 1) / box);
+            int32_t block[8];
 #pragma unroll
-                        for (int part = 0; part < kParts; ++part) {
-                            if (paged)
-                                tma_load(dst + part * (kTile * 128), map, part * 64, r & ((1 << a.bs_shift) - 1), g.h, block, full_bar(s));
-                            else
-                                tma_load(dst + part * (kTile * 128), map, part * 64, g.h, g.begin + r, 0, full_bar(s));
-                        }
+            for (int c = 0; c < 8; ++c) block[c] = paged ? __shfl_sync(0xffffffffu, page, c) : 0;
+            if (elect_one()) {
+                bar_expect(full_bar(s), copies * box * (second ? 2 : 1) * D * 2);
+                const uint32_t dst = ring + s * kTileBytes;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    if (c >= copies) break;
+                    const int r = k0 + c * box;
+                    const int c1 = paged ? r & ((1 << a.bs_shift) - 1) : g.h, c2 = paged ? g.h : g.begin + r;
+#pragma unroll
+                    for (int part = 0; part < kParts; ++part) {
+                        tma_load(dst + part * (keys * 128) + c * box * 128, map, part * 64, c1, c2, block[c], full_bar(s));
+                        if (second)
+                            tma_load(dst + kTileBytes / 2 + part * (keys * 128) + c * box * 128, second, part * 64, c1, c2, block[c], full_bar(s));
                     }
-                    __syncwarp();
                 }
-                if (n_copies == 0 && elect_one()) bar_arrive(full_bar(s));
-                __syncwarp();
-                ++it;
-                return true;
-            };
+            }
+            __syncwarp();
+            ++it;
+        };
+        bool have = walk.next(a, TQ, g);
+        int32_t page0 = -1, page1 = -1, page2 = -1;  // blocks of the tiles t .. t + 2
+        auto first_pages = [&]() {
+            page0 = page_of(g, 0);
+            page1 = page_of(g, 1);
+            page2 = page_of(g, 2);
+        };
+        if (have) first_pages();
+        while (ok && have) {
             // the queries: G heads of TQ tokens at a time, which is the row tile's order
             if (items > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (items - 1) & 1, failed));
             if (!ok) break;
@@ -773,18 +800,34 @@ __global__ void __launch_bounds__(kThreads, 1)
                                  g.begin + (g.pair * 2 + r) * TQ, q_full);
             }
             __syncwarp();
-            // keys lead by the number of slots that a key tile does not go to both of
-            const int ahead = g.two ? 1 : 2;
-            int32_t page0 = page_of(0), page1 = page_of(1), page2 = page_of(2);  // blocks of the tiles t .. t + 2
-            ok = fetch(&kmap, 0, page0);
-            if (ok && ahead == 2 && g.nt > 1) ok = fetch(&kmap, 1, page1);
-            for (int t = 0; ok && t < g.nt; ++t) {
-                const int32_t page3 = page_of(t + 3);  // its latency passes under the waits
-                ok = fetch(&vmap, t, page0);
-                if (ok && t + ahead < g.nt) ok = fetch(&kmap, t + ahead, ahead == 2 ? page2 : page1);
-                page0 = page1;
-                page1 = page2;
-                page2 = page3;
+            if (g.two) {
+                fetch(&kmap, nullptr, 0, page0);
+                for (int t = 0; ok && t < g.nt; ++t) {
+                    const int32_t page3 = page_of(g, t + 3);  // its latency passes under the waits
+                    fetch(&vmap, nullptr, t, page0);
+                    if (t + 1 < g.nt) fetch(&kmap, nullptr, t + 1, page1);
+                    page0 = page1;
+                    page1 = page2;
+                    page2 = page3;
+                }
+                have = walk.next(a, TQ, g);
+                if (have) first_pages();
+            } else {
+                // the next item's lengths and first blocks are looked up while this one's tiles are on their way
+                fetch(&kmap, &vmap, 0, page0);
+                Segment next;
+                have = walk.next(a, TQ, next);
+                const int32_t next0 = have ? page_of(next, 0) : -1, next1 = have ? page_of(next, 1) : -1, next2 = have ? page_of(next, 2) : -1;
+                for (int t = 1; ok && t < g.nt; ++t) {
+                    const int32_t page3 = page_of(g, t + 2);
+                    fetch(&kmap, &vmap, t, page1);
+                    page1 = page2;
+                    page2 = page3;
+                }
+                g = next;
+                page0 = next0;
+                page1 = next1;
+                page2 = next2;
             }
         }
         if (*failed) {  // giving up: copies already asked for may still be landing
@@ -794,7 +837,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         // ------------------------------------------------------------------ products: the warp waits, one lane issues
         // stages in the order of their use, weights of a slot and queries: number (of a stage) and phase of the next
-        uint32_t stage = 0, stage_phase = 0, p_phase0 = 0, p_phase1 = 0, q_phase = 0;
+        uint32_t stage = 0, stage_phase = 0, p_phase0 = 0, p_phase1 = 0, h_phase0 = 0, h_phase1 = 0, q_phase = 0;
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, failed)); };
         auto next_stage = [&]() {  // waits for it
@@ -806,82 +849,125 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             return s;
         };
-        const uint64_t qdesc = desc_k(qbuf), kdesc = desc_k(ring), vdesc = desc_mn(ring);
-        auto scores = [&](int slot, int row_tile, uint32_t s) {  // (by the elected lane, as all below)
-            const uint64_t q = qdesc + (uint64_t)(row_tile * (kTileBytes >> 4)), k = kdesc + (uint64_t)(s * (kTileBytes >> 4));
+        const uint64_t qdesc = desc_k(qbuf), kdesc = desc_k(ring);
+        const uint64_t vdesc = desc_mn(ring, kTile), vdesc_half = desc_mn(ring + kTileBytes / 2, kHalf);
+        constexpr uint32_t kStep = kTileBytes >> 4;
+        // All by the elected lane.  A slot's scores of 128 or 64 keys; its weights of 16 * steps keys from column p on with
+        // their values.
+        auto scores = [&](int slot, uint64_t q, uint32_t s) {
+            constexpr int kPart = (kTile * 128) >> 4;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk) {
-                constexpr int kPart = (kTile * 128) >> 4;
-                mma_ss(s_col(slot), q + (kk >> 2) * kPart + (kk & 3) * 2, k + (kk >> 2) * kPart + (kk & 3) * 2, kIdescQK, kk > 0);
-            }
+            for (int kk = 0; kk < D / 16; ++kk)
+                mma_ss(s_col(slot), q + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPart + (kk & 3) * 2, kIdescQK, kk > 0);
             mma_commit(s_full(slot));
         };
-        // One slot's turn: its weights with the values of stage vs, in two halves, then the scores of its next key tile.
-        auto turn = [&](int slot, int row_tile, uint32_t vs, bool begun, bool last_use, bool more, uint32_t &ks, bool load_k, bool last_q) {
-            const uint32_t phase = slot ? p_phase1 : p_phase0;
-            if (slot)
+        auto scores_half = [&](int slot, uint32_t s) {
+            constexpr int kPart = (kTile * 128) >> 4, kPartK = (kHalf * 128) >> 4;
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+                mma_ss(s_col(slot), qdesc + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPartK + (kk & 3) * 2, kIdescQKHalf,
+                       kk > 0);
+            mma_commit(s_full(slot));
+        };
+        auto outputs = [&](int slot, int col, uint64_t v, bool begun) {
+#pragma unroll
+            for (int kk = 0; kk < kHalf / 16; ++kk)
+                mma_ts(o_col(slot), s_col(slot) + col + kk * 8, v + kk * (2048 >> 4), kIdescPV, begun || kk > 0);
+        };
+        // Two row tiles, one slot's turn: its weights with the values of stage vs, in two halves, then the scores of its next
+        // key tile.
+        auto turn = [&](int slot, uint32_t vs, bool begun, bool more, uint32_t &ks, bool load_k, bool last_q) {
+            const uint32_t phase = slot ? p_phase1 : p_phase0, half = slot ? h_phase1 : h_phase0;
+            if (slot) {
                 p_phase1 ^= 1;
-            else
+                h_phase1 ^= 1;
+            } else {
                 p_phase0 ^= 1;
-            wait(p_half(slot), phase);
+                h_phase0 ^= 1;
+            }
+            wait(p_half(slot), half);
             if (!ok) return;
             fence_after();
-            const uint64_t v = vdesc + (uint64_t)(vs * (kTileBytes >> 4));
-            if (elect_one()) {
-#pragma unroll
-                for (int kk = 0; kk < kTile / 32; ++kk)
-                    mma_ts(o_col(slot), s_col(slot) + kk * 8, v + kk * (2048 >> 4), kIdescPV, begun || kk > 0);
-            }
+            const uint64_t v = vdesc + vs * kStep;
+            if (elect_one()) outputs(slot, 0, v, begun);
             __syncwarp();
             if (load_k) ks = next_stage();
             wait(p_full(slot), phase);
             if (!ok) return;
             fence_after();
             if (elect_one()) {
-#pragma unroll
-                for (int kk = kTile / 32; kk < kTile / 16; ++kk)
-                    mma_ts(o_col(slot), s_col(slot) + kk * 8, v + kk * (2048 >> 4), kIdescPV, 1);
+                outputs(slot, 32, v + 4 * (2048 >> 4), true);
                 if (more) {
-                    scores(slot, row_tile, ks);
-                    if (last_use) mma_commit(empty_bar(ks));
+                    scores(slot, qdesc + slot * kStep, ks);
+                    if (slot) mma_commit(empty_bar(ks));
                     if (last_q) mma_commit(q_empty);
                 } else {
                     mma_commit(o_full(slot));
                 }
-                if (last_use) mma_commit(empty_bar(vs));
+                if (slot) mma_commit(empty_bar(vs));
             }
             __syncwarp();
         };
         while (ok && walk.next(a, TQ, g)) {
             wait(q_full, q_phase);
             q_phase ^= 1;
-            const int ahead = g.two ? 1 : 2;
-            for (int t = 0; ok && t < min(ahead, g.nt); ++t) {
+            if (g.two) {
                 const uint32_t s = next_stage();
                 if (!ok) break;
                 fence_after();
                 if (elect_one()) {
-                    if (g.two) {
-                        scores(0, 0, s);
-                        scores(1, 1, s);
-                    } else {
-                        scores(t, 0, s);
-                    }
+                    scores(0, qdesc, s);
+                    scores(1, qdesc + kStep, s);
                     mma_commit(empty_bar(s));
-                    if (t == g.nt - 1) mma_commit(q_empty);
+                    if (g.nt == 1) mma_commit(q_empty);
                 }
                 __syncwarp();
-            }
-            for (int t = 0; ok && t < g.nt; ++t) {
-                const uint32_t vs = next_stage();
-                const bool more = t + ahead < g.nt, last_q = t + ahead == g.nt - 1;
-                uint32_t ks = 0;
-                if (!ok) break;
-                if (g.two) {
-                    turn(0, 0, vs, t > 0, false, more, ks, more, false);
-                    if (ok) turn(1, 1, vs, t > 0, true, more, ks, false, last_q);
-                } else {
-                    turn(t & 1, 0, vs, t > 1, true, more, ks, more, last_q);
+                for (int t = 0; ok && t < g.nt; ++t) {
+                    const uint32_t vs = next_stage();
+                    const bool more = t + 1 < g.nt;
+                    uint32_t ks = 0;
+                    if (!ok) break;
+                    turn(0, vs, t > 0, more, ks, more, false);
+                    if (ok) turn(1, vs, t > 0, more, ks, false, t + 2 == g.nt);
+                }
+            } else {
+                uint32_t mine[2] = {0, 0};  // the stages of the slots' key tiles
+                for (int t = 0; ok && t < g.nt + 2; ++t) {
+                    // tile t - 2's weights with its values; then tile t's scores, in the same slot
+                    const int slot = t & 1;
+                    if (t >= 2) {
+                        const uint32_t phase = slot ? p_phase1 : p_phase0;
+                        wait(p_full(slot), phase);
+                        if (slot)
+                            p_phase1 ^= 1;
+                        else
+                            p_phase0 ^= 1;
+                        if (!ok) break;
+                        fence_after();
+                        const uint32_t s = slot ? mine[1] : mine[0];
+                        if (elect_one()) {
+                            outputs(slot, 0, vdesc_half + s * kStep, t >= 4);
+                            mma_commit(empty_bar(s));
+                            if (t >= g.nt) mma_commit(o_full(slot));
+                        }
+                        __syncwarp();
+                    } else if (t >= g.nt) {
+                        continue;  // one key tile: the other slot has none
+                    }
+                    if (t < g.nt) {
+                        const uint32_t s = next_stage();
+                        if (!ok) break;
+                        fence_after();
+                        if (slot)
+                            mine[1] = s;
+                        else
+                            mine[0] = s;
+                        if (elect_one()) {
+                            scores_half(slot, s);
+                            if (t == g.nt - 1) mma_commit(q_empty);
+                        }
+                        __syncwarp();
+                    }
                 }
             }
         }
@@ -1045,13 +1131,13 @@ pcg_status attention_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, voi
     CUresult r = encode(&q, bf16, a.q, {d, G, heads, rows}, {d * 2, G * d * 2, (cuuint64_t)a.q_stride * 2}, {64u, g, 1u, tokens});
     if (a.kv_len) {
         const cuuint64_t bs = 1ull << a.bs_shift, blocks = a.n_blocks;
-        const cuuint32_t box = bs < kTile ? (cuuint32_t)bs : kTile;
+        const cuuint32_t box = bs < kHalf ? (cuuint32_t)bs : kHalf;
         if (r == CUDA_SUCCESS) r = encode(&k, bf16, a.k, {d, bs, heads, blocks}, {d * 2, bs * d * 2, heads * bs * d * 2}, {64u, box, 1u, 1u});
         if (r == CUDA_SUCCESS) r = encode(&v, bf16, a.v, {d, bs, heads, blocks}, {d * 2, bs * d * 2, heads * bs * d * 2}, {64u, box, 1u, 1u});
     } else {
         const cuuint64_t ks = (cuuint64_t)a.k_stride * 2, vs = (cuuint64_t)a.v_stride * 2;
-        if (r == CUDA_SUCCESS) r = encode(&k, bf16, a.k, {d, heads, rows, 1}, {d * 2, ks, rows * ks}, {64u, 1u, kTile, 1u});
-        if (r == CUDA_SUCCESS) r = encode(&v, bf16, a.v, {d, heads, rows, 1}, {d * 2, vs, rows * vs}, {64u, 1u, kTile, 1u});
+        if (r == CUDA_SUCCESS) r = encode(&k, bf16, a.k, {d, heads, rows, 1}, {d * 2, ks, rows * ks}, {64u, 1u, kHalf, 1u});
+        if (r == CUDA_SUCCESS) r = encode(&v, bf16, a.v, {d, heads, rows, 1}, {d * 2, vs, rows * vs}, {64u, 1u, kHalf, 1u});
     }
     if (r != CUDA_SUCCESS) {
         set_error("%s: cuTensorMapEncodeTiled failed (%d)", who, (int)r);
