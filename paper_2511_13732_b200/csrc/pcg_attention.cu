@@ -29,8 +29,7 @@ struct Narrow<f16_t> {
 // ---------------------------------------------------------------------------------------------- any type and head size
 // One block per (row, query head): its eight warps take keys 32 at a time in turn, a lane scores one key (16-byte loads,
 // the query in shared memory), and the warp sums the 32 weighted values with lane = head dimension.  The warps'
-// running sums meet in shared memory at the end.  Serves float32 and the head dimensions that the tensor-core kernel is
-// not built for.  Blocks of one sequence and head group re-read its keys out of L2.
+// running sums meet in shared memory at the end.  Serves the head dimensions that the other kernels are not built for.  Blocks of one sequence and head group re-read its keys out of L2.
 constexpr int kSimpleThreads = 256;
 
 template <typename T, int DPL>  // DPL: values per lane, 32 * DPL >= d
@@ -161,7 +160,8 @@ pcg_status run_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, vo
     }
     pcg_status st = check_here(who, a.out);
     if (st != PCG_OK) return st;
-    if (attention_tc_takes(a.d, dtype)) return attention_tc(who, a, dtype, workspace, stream);
+    if (attention_shares(a.d))
+        return dtype == PCG_F32 ? attention_f32(who, a, workspace, stream) : attention_tc(who, a, dtype, workspace, stream);
     PCG_DISPATCH_DTYPE(dtype, launch_simple<LogitT>(a, stream));
     cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
@@ -194,7 +194,7 @@ using namespace pcg;
 
 extern "C" size_t pcg_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                                                 pcg_dtype dtype) {
-    return attention_tc_takes(head_dim, dtype) ? attention_tc_workspace_bytes(B, head_dim) : 256;
+    return attention_shares(head_dim) ? attention_work_bytes(head_dim) : 256;
 }
 
 extern "C" pcg_status pcg_cache_attention(const void *q, int64_t q_stride, int32_t rows, int32_t q_heads,

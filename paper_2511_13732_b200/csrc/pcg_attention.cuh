@@ -17,10 +17,12 @@ struct AttnArgs {
 
 constexpr int kAttnMaxB = 16384, kAttnMaxGroup = 128;
 
-// Whether the tensor-core kernels take these sizes.
-inline bool attention_tc_takes(int d, pcg_dtype dtype) { return dtype != PCG_F32 && (d == 64 || d == 128); }
-size_t attention_tc_workspace_bytes(int32_t B, int32_t d);
+// The kernels that share their work out among all SMs take head dimensions 64 and 128: the 16-bit types on the tensor
+// cores, float32 on the FMA pipes.  Both need attention_work_bytes(d) of workspace.
+inline bool attention_shares(int d) { return d == 64 || d == 128; }
+size_t attention_work_bytes(int32_t d);
 pcg_status attention_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream);
+pcg_status attention_f32(const char *who, const AttnArgs &a, void *workspace, cudaStream_t stream);
 
 #ifdef __CUDACC__
 
