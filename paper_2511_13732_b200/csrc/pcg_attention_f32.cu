@@ -83,27 +83,37 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
                                     (int64_t)(g.h * G + ((r0 + r) & (kTile - 1)) % G) * D + c * 4;
                 copy16(&sh.q[r][c * 4], from, t >= 0);
             }
+            // Thread t copies vector t % V of rows t / V, t / V + 256 / V, ...; the blocks of those rows are looked up one tile
+            // ahead of the copies.
+            constexpr int kCopies = kF32Keys * V / kF32Threads;
+            int32_t block[kCopies];
+            auto look_up = [&](int k0) {
+#pragma unroll
+                for (int j = 0; j < kCopies; ++j) {
+                    const int pos = k0 + tid / V + j * (kF32Threads / V);
+                    block[j] = a.kv_len && pos < k_stop ? a.block_table[(int64_t)g.b * a.max_blocks + (pos >> a.bs_shift)] : 0;
+                }
+            };
             auto fetch = [&](int k0, int buf) {
-                for (int i = tid; i < kF32Keys * V; i += kF32Threads) {
-                    const int r = i / V, c = i % V, pos = k0 + r;
+#pragma unroll
+                for (int j = 0; j < kCopies; ++j) {
+                    const int r = tid / V + j * (kF32Threads / V), c = tid % V, pos = k0 + r;
                     bool there = pos < k_stop;
                     int64_t ko = 0, vo = 0;
-                    if (there) {
-                        if (a.kv_len) {
-                            const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (pos >> a.bs_shift)];
-                            there = block >= 0 && block < a.n_blocks;
-                            if (there)
-                                ko = vo = ((((int64_t)block * a.kv_heads + g.h) << a.bs_shift) + (pos & ((1 << a.bs_shift) - 1))) * D;
-                        } else {
-                            ko = ((int64_t)g.begin + pos) * a.k_stride + (int64_t)g.h * D;
-                            vo = ((int64_t)g.begin + pos) * a.v_stride + (int64_t)g.h * D;
-                        }
+                    if (a.kv_len) {
+                        there = there && block[j] >= 0 && block[j] < a.n_blocks;
+                        if (there) ko = vo = ((((int64_t)block[j] * a.kv_heads + g.h) << a.bs_shift) + (pos & ((1 << a.bs_shift) - 1))) * D;
+                    } else if (there) {
+                        ko = ((int64_t)g.begin + pos) * a.k_stride + (int64_t)g.h * D;
+                        vo = ((int64_t)g.begin + pos) * a.v_stride + (int64_t)g.h * D;
                     }
                     copy16(&sh.k[buf][r][c * 4], (const float *)a.k + ko + c * 4, there);
                     copy16(&sh.v[buf][r][c * 4], (const float *)a.v + vo + c * 4, there);
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
+                look_up(k0 + kF32Keys);
             };
+            look_up(k_begin);
             float m[4], l[4], o[4][4 * N];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {

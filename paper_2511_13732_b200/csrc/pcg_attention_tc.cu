@@ -198,7 +198,7 @@ __device__ __forceinline__ void weights(const uint32_t *v, uint64_t scale, uint6
     }
 }
 
-// 32 bytes of a row.  A warp's lanes hold 32 rows, so a store touches 32 lines whatever its width: few and wide ones.
+// 32 bytes of a row (the lanes' rows are apart: whole sectors at least).
 __device__ __forceinline__ void store_row(void *p, const uint32_t (&w)[8], bool wide) {
     if (wide) {
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), PCG_W8(w, 0) : "memory");
@@ -214,7 +214,7 @@ struct Sizes {
     static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
     // Ring, 160 KB: a stage holds 128 keys or their values, or 64 keys and then their values, each as D / 64 parts.
     static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr int kSmem = (2 + kStages) * kTileBytes + 1024;  // room to start on a 1024-byte boundary
+    static constexpr int kSmem = (2 + kStages) * kTileBytes;  // 224 KB; 3 KB are left for all else
     static_assert((2 + kStages) * kTileBytes >= kAttnMaxB * 12, "the cut's scratch");
 };
 
@@ -232,35 +232,35 @@ __global__ void __launch_bounds__(kThreads, 1)
     // reference is then 2^15 at most.  The sums carry the same factor, so it cancels.
     constexpr float kLift = BF16 ? 0.f : 7.f;
 
-    extern __shared__ unsigned char smem_raw[];
+    extern __shared__ __align__(1024) unsigned char smem_raw[];  // swizzled tiles start on 1024-byte boundaries
     __shared__ int64_t warp_units[kThreads / 32], warp_items[kThreads / 32];
     __shared__ Run run[2];
-    __shared__ __align__(8) uint64_t bars[2 * S + 16];
-    __shared__ float other_m[kTile], other_l[kTile];  // slot 1's, for the end of an item with one row tile
+    __shared__ __align__(8) uint64_t bars[2 * S + 15];
+    __shared__ float slot_m[2][kTile], slot_l[2][kTile];  // for the end of an item with one row tile
     __shared__ uint32_t tmem_slot;
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, bar0 = smem_u32(bars);
-    const uint32_t qbuf = base, ring = base + 2 * kTileBytes;
+    const uint32_t qbuf = smem_u32(smem_raw), ring = qbuf + 2 * kTileBytes, bar0 = smem_u32(bars);
     auto full_bar = [&](int s) { return bar0 + 8u * s; };         // a stage has landed
     auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };  // a stage has been read
     const uint32_t q_full = bar0 + 8u * (2 * S), q_empty = q_full + 8, drain = q_full + 16;
     auto s_full = [&](int s) { return q_full + 24u + 8u * s; };   // a slot's scores are complete
     auto p_full = [&](int s) { return q_full + 40u + 8u * s; };   // ... its weights are in place
     auto o_full = [&](int s) { return q_full + 56u + 8u * s; };   // ... its last product is complete
+    auto written = [&](int s) { return q_full + 104u + 8u * s; };  // a slot's outputs of an item are out of its stage
     auto p_half = [&](int s) { return q_full + 88u + 8u * s; };   // ... those of the first 64 keys
-    const uint32_t merge_full = q_full + 72, merge_done = q_full + 80;  // slot 1's reference and sum are handed over, read
+    const uint32_t merge_full = q_full + 72, merge_done = q_full + 80;  // both slots' references and sums are there, read
 
     if (tid == 0) {
-        for (int i = 0; i < 2 * S + 13; ++i) {
+        for (int i = 0; i < 2 * S + 15; ++i) {
             // by warps: the weights of a slot (4), the hand-over (4 and 4); by one thread or the hardware: all others
             const uint32_t bar = bar0 + 8u * i;
-            const uint32_t count = bar == p_full(0) || bar == p_full(1) || bar == p_half(0) || bar == p_half(1) || bar == merge_full || bar == merge_done ? 4 : 1;
+            const uint32_t count = bar == p_full(0) || bar == p_full(1) || bar >= p_half(0) ? 4 : bar >= merge_full ? 8 : 1;
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        failed_flag = 0;
+        failed_flag = (qbuf & 1023u) != 0;  // never: the array is declared so
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512));
@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
-    cut_work(a, TQ, reinterpret_cast<int64_t *>(smem_raw + (base - smem_u32(smem_raw))), warp_units, warp_items, run);
+    cut_work(a, TQ, reinterpret_cast<int64_t *>(smem_raw), warp_units, warp_items, run);
     if (tid == 0) reinterpret_cast<WorkspaceHead *>(ws)->run[blockIdx.x] = run[0];
     if (tid == 0 && blockIdx.x == kMaxBlocks - 1) reinterpret_cast<WorkspaceHead *>(ws)->run[kMaxBlocks] = run[1];
     Walk walk;
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t sc = s_col(slot) + lanes, oc = o_col(slot) + lanes;
         const int tok = row / G, head = row - tok * G;
-        uint32_t sn = 0, on = 0, on_other = 0, mn = 0;  // phases met so far
+        uint32_t sn = 0, on = 0, on_other = 0, mn = 0, wn = 0;  // phases met so far
         uint32_t loads = 0;                             // stages filled so far
         bool ok = true;
         while (ok && walk.next(a, TQ, g)) {
@@ -326,12 +326,35 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (warp_valid) {
                     uint32_t v[64];
                     float top[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
-                    const bool masked = __any_sync(0xffffffffu, lim < k0 + keys);
-                    const int seen = lim - k0;
-                    auto mask = [&](int from) {
+                    if (__any_sync(0xffffffffu, lim < k0 + keys)) {
+                        // Scores of keys that a row does not see become -inf where they lie, 16 columns at a time: first those
+                        // that some of the warp's rows see, then those that none does.  (In line, over all columns, this took
+                        // 2,000 cycles: code that runs once an item comes at some 6 cycles an instruction, being out of the
+                        // instruction cache.  So does all else that an item has once, hence the small loops below.)
+                        const int seen = max(lim - k0, 0);
+                        int c = __reduce_min_sync(0xffffffffu, seen) & ~15;
+                        const int none = __reduce_max_sync(0xffffffffu, valid ? seen : 0);
+                        uint32_t x[16];
+#pragma unroll 1
+                        for (; c < none && c < keys; c += 16) {
+                            tmem_ld16(sc + c, x);
+                            tmem_wait_ld();
+                            tmem_loaded<16>(x);
 #pragma unroll
-                        for (int c = 0; c < 64; ++c)
-                            if (from + c >= seen) v[c] = __float_as_uint(kNegInf);
+                            for (int i = 0; i < 16; ++i)
+                                if (c + i >= seen) x[i] = __float_as_uint(kNegInf);
+                            tmem_st16(sc + c, x);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(kNegInf);
+#pragma unroll 1
+                        for (; c < keys; c += 16) tmem_st16(sc + c, x);
+                        tmem_wait_st();
+                    }
+                    auto take_max = [&](const uint32_t (&x)[64]) {
+#pragma unroll
+                        for (int c = 0; c < 64; c += 2)
+                            top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
                     };
                     tmem_ld32(sc, v);
                     tmem_ld32(sc + 32, v + 32);
@@ -341,22 +364,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                         tmem_ld32(sc + 96, u + 32);
                         tmem_wait_ld();
                         tmem_loaded<64>(u);
-                        if (masked) {
-#pragma unroll
-                            for (int c = 0; c < 64; ++c)
-                                if (64 + c >= seen) u[c] = __float_as_uint(kNegInf);
-                        }
-#pragma unroll
-                        for (int c = 0; c < 64; c += 2)
-                            top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(u[c]), __uint_as_float(u[c + 1]));
+                        take_max(u);
                     } else {
                         tmem_wait_ld();
                     }
                     tmem_loaded<64>(v);
-                    if (masked) mask(0);
-#pragma unroll
-                    for (int c = 0; c < 64; c += 2)
-                        top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                    take_max(v);
                     const float mt = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * a.scale_log2;
                     bad = bad || !(mt < -kNegInf);
                     // also when the first score above -inf is met; a row's reference depends on its own scores alone, and
@@ -393,7 +406,6 @@ __global__ void __launch_bounds__(kThreads, 1)
                         if (h) {
                             tmem_wait_ld();
                             tmem_loaded<64>(v);
-                            if (masked) mask(64);
                         }
                         weights<BF16>(v, scale2, by2, sum, p);
                         if (!h && g.two) tmem_ld32(sc + 64, v);
@@ -426,78 +438,128 @@ __global__ void __launch_bounds__(kThreads, 1)
             const bool shared = !g.two && g.nt > 1;            // both have, of one row tile
             if (mine) ok = __all_sync(0xffffffffu, bar_wait(o_full(slot), on++ & 1, failed));
             if (!ok) break;
-            if (shared) {
-                if (slot == 1) {
-                    other_m[row] = m;
-                    other_l[row] = l;
-                    __syncwarp();
-                    if (lane == 0) bar_arrive(merge_full);
-                    ok = __all_sync(0xffffffffu, bar_wait(merge_done, mn++ & 1, failed));  // slot 0 has read this slot's sums
-                    continue;
-                }
-                ok = __all_sync(0xffffffffu, bar_wait(o_full(1), on_other++ & 1, failed)) &&
-                     __all_sync(0xffffffffu, bar_wait(merge_full, mn++ & 1, failed));
+            if (shared) {  // the slots join their sums, each for one half of the head dimensions
+                slot_m[slot][row] = m;
+                slot_l[slot][row] = l;
+                __syncwarp();
+                if (lane == 0) bar_arrive(merge_full);
+                ok = __all_sync(0xffffffffu, bar_wait(merge_full, mn & 1, failed)) &&
+                     __all_sync(0xffffffffu, bar_wait(o_full(slot ^ 1), on_other++ & 1, failed));
                 if (!ok) break;
-            } else if (g.two) {
+            } else if (g.two || !mine) {
                 ++on_other;
             }
-            if (!mine) continue;
-            fence_after();
-            if (warp_valid) {
-                float f0 = 1.f, f1 = 0.f;
-                if (shared) {
-                    const float m1 = other_m[row], l1 = other_l[row], mx = fmaxf(m, m1);
-                    f0 = m == mx ? 1.f : ex2(m - mx);  // equal, or both -inf: nothing to scale
-                    f1 = m1 == mx ? 1.f : ex2(m1 - mx);
-                    l = l * f0 + l1 * f1;
-                    m = mx;
-                }
-                // a row that sees no key is 0 (below); one that sees scores of -inf alone is 0 / 0 = NaN
-                const float inv = 1.f / l;
-                char *out = (char *)a.out + (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2);
-                const bool wide = ((uintptr_t)a.out & 31) == 0;
-                const int prow = (g.two ? slot * kTile : 0) + row;
-                float *part = part_base(ws, blockIdx.x, g.t0 == 0 ? 1 : 0, D);
-#pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(oc + c, o);
-                    tmem_wait_ld();
-                    tmem_loaded<32>(o);
+            // With two row tiles, outputs are staged in the item's last two stages of the ring (slot 0 in the keys', slot 1 in
+            // the values'), which the products leave to the softmax to release: all that read them is complete.
+            const uint32_t last = (loads - (slot == 0 ? 2 : 1)) % S, staged = ring + last * kTileBytes;
+            if (mine) {
+                fence_after();
+                if (warp_valid) {
+                    float f0 = 1.f, f1 = 0.f;
                     if (shared) {
-                        uint32_t o1[32];
-                        tmem_ld32(o_col(1) + lanes + c, o1);
-                        tmem_wait_ld();
-                        tmem_loaded<32>(o1);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+                        const float m1 = slot_m[slot ^ 1][row], l1 = slot_l[slot ^ 1][row], mx = fmaxf(m, m1);
+                        f0 = m == mx ? 1.f : ex2(m - mx);  // equal, or both -inf: nothing to scale
+                        f1 = m1 == mx ? 1.f : ex2(m1 - mx);
+                        l = l * f0 + l1 * f1;
+                        m = mx;
                     }
-                    if (valid && g.whole) {
+                    // a row that sees no key is 0 (below); one that sees scores of -inf alone is 0 / 0 = NaN
+                    if (g.whole) {
+                        const float inv = 1.f / l;
+                        f0 *= inv;
+                        f1 *= inv;
+                    }
+                    const int prow = (g.two ? slot * kTile : 0) + row;
+                    float *part = part_base(ws, blockIdx.x, g.t0 == 0 ? 1 : 0, D);
+                    const uint32_t stage_row = staged + row * (D * 2);
+                    const int64_t offset = valid ? (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2) : -1;
+                    const bool wide = ((uintptr_t)a.out & 31) == 0;
+#pragma unroll 1
+                    for (int c = shared && slot ? D / 2 : 0; c < (shared && !slot ? D / 2 : D); c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(oc + c, o);
+                        if (shared) {
+                            uint32_t o1[16];
+                            tmem_ld16(o_col(slot ^ 1) + lanes + c, o1);
+                            tmem_wait_ld();
+                            tmem_loaded<16>(o);
+                            tmem_loaded<16>(o1);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 16) {
+                            for (int i = 0; i < 16; ++i)
+                                o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+                        } else {
+                            tmem_wait_ld();
+                            tmem_loaded<16>(o);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0);
+                        }
+                        if (g.whole) {
                             uint32_t w[8];
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
-                                w[j] = lim <= 0 ? 0u
-                                                : pack2<BF16>(__uint_as_float(o[i + 2 * j]) * inv, __uint_as_float(o[i + 2 * j + 1]) * inv);
-                            store_row(out + (c + i) * 2, w, wide);
-                        }
-                    } else if (valid) {
+                                w[j] = lim <= 0 ? 0u : pack2<BF16>(__uint_as_float(o[2 * j]), __uint_as_float(o[2 * j + 1]));
+                            if (g.two) {
+                                // 16-byte chunks of the row, permuted by its number: a warp's lanes meet all banks alike
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) part[(size_t)(c + i) * kPartRows + prow] = __uint_as_float(o[i]);
+                                for (int i = 0; i < 2; ++i)
+                                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage_row + (((c >> 3) + i) ^ (row & 7)) * 16),
+                                                 "r"(w[4 * i]), "r"(w[4 * i + 1]), "r"(w[4 * i + 2]), "r"(w[4 * i + 3])
+                                                 : "memory");
+                            } else if (valid) {  // few rows: straight to memory
+                                store_row((char *)a.out + offset + c * 2, w, wide);
+                            }
+                        } else if (valid) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) part[(size_t)(c + i) * kPartRows + prow] = __uint_as_float(o[i]);
+                        }
+                        __syncwarp();  // the next columns are read by the whole warp
                     }
-                    __syncwarp();  // the next columns are read by the whole warp
+                    if (valid && !g.whole && !(shared && slot)) {
+                        part[(size_t)D * kPartRows + prow] = m;
+                        part[(size_t)(D + 1) * kPartRows + prow] = l;
+                    }
+                    if (g.whole && g.two) {
+                        // whole rows to memory, 32 / (D / 8) at a time: a row a lane would touch 32 lines a store, which took
+                        // 4,400 cycles a tile of head dimension 128
+                        constexpr int kChunks = D / 8, kRowsAtOnce = 32 / kChunks;
+                        const int rows = 32 - __clz(__ballot_sync(0xffffffffu, valid));  // valid rows come first
+                        const int chunk = lane % kChunks;
+                        const uint32_t stage_warp = staged + (warp & 3) * 32 * (D * 2);
+#pragma unroll 1
+                        for (int r0 = 0; r0 < rows; r0 += 4 * kRowsAtOnce) {
+                            uint32_t w[4][4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int r = (r0 + k * kRowsAtOnce + lane / kChunks) & 31;
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                             : "=r"(w[k][0]), "=r"(w[k][1]), "=r"(w[k][2]), "=r"(w[k][3])
+                                             : "r"(stage_warp + r * (D * 2) + (chunk ^ (r & 7)) * 16)
+                                             : "memory");
+                            }
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int r = r0 + k * kRowsAtOnce + lane / kChunks;
+                                const int64_t to = __shfl_sync(0xffffffffu, offset, r & 31);
+                                if (r < rows && to >= 0)
+                                    *reinterpret_cast<uint4 *>((char *)a.out + to + chunk * 16) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+                            }
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // copies land there next
+                    }
                 }
-                if (valid && !g.whole) {
-                    part[(size_t)D * kPartRows + prow] = m;
-                    part[(size_t)(D + 1) * kPartRows + prow] = l;
-                }
-            }
-            fence_before();
-            if (shared) {
+                fence_before();
                 __syncwarp();
-                if (lane == 0) bar_arrive(merge_done);
+                if (g.two) {
+                    if (lane == 0) bar_arrive(written(slot));
+                    if ((warp & 3) == 0) {  // the stage is free when all four warps are through
+                        ok = __all_sync(0xffffffffu, bar_wait(written(slot), wn & 1, failed));
+                        if (ok && lane == 0) bar_arrive(empty_bar(last));
+                    }
+                    ++wn;
+                } else if (shared) {  // the other slot has read this one's sums
+                    if (lane == 0) bar_arrive(merge_done);
+                    ok = __all_sync(0xffffffffu, bar_wait(merge_done, mn++ & 1, failed));
+                }
             }
         }
     } else if (warp == kSoftmaxWarps) {
@@ -605,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     } else {
         // ------------------------------------------------------------------ products: the warp waits, one lane issues
         // stages in the order of their use, weights of a slot and queries: number (of a stage) and phase of the next
-        uint32_t stage = 0, stage_phase = 0, p_phase0 = 0, p_phase1 = 0, h_phase0 = 0, h_phase1 = 0, q_phase = 0;
+        uint32_t stage = 0, stage_phase = 0, h_phase = 0, p_phase0 = 0, p_phase1 = 0, q_phase = 0;
         bool ok = true;
         auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, failed)); };
         auto next_stage = [&]() {  // waits for it
@@ -642,40 +704,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int kk = 0; kk < kHalf / 16; ++kk)
                 mma_ts(o_col(slot), s_col(slot) + col + kk * 8, v + kk * (2048 >> 4), kIdescPV, begun || kk > 0);
         };
-        // Two row tiles, one slot's turn: its weights with the values of stage vs, in two halves, then the scores of its next
-        // key tile.
-        auto turn = [&](int slot, uint32_t vs, bool begun, bool more, uint32_t &ks, bool load_k, bool last_q) {
-            const uint32_t phase = slot ? p_phase1 : p_phase0, half = slot ? h_phase1 : h_phase0;
-            if (slot) {
-                p_phase1 ^= 1;
-                h_phase1 ^= 1;
-            } else {
-                p_phase0 ^= 1;
-                h_phase0 ^= 1;
-            }
-            wait(p_half(slot), half);
-            if (!ok) return;
-            fence_after();
-            const uint64_t v = vdesc + vs * kStep;
-            if (elect_one()) outputs(slot, 0, v, begun);
-            __syncwarp();
-            if (load_k) ks = next_stage();
-            wait(p_full(slot), phase);
-            if (!ok) return;
-            fence_after();
-            if (elect_one()) {
-                outputs(slot, 32, v + 4 * (2048 >> 4), true);
-                if (more) {
-                    scores(slot, qdesc + slot * kStep, ks);
-                    if (slot) mma_commit(empty_bar(ks));
-                    if (last_q) mma_commit(q_empty);
-                } else {
-                    mma_commit(o_full(slot));
-                }
-                if (slot) mma_commit(empty_bar(vs));
-            }
-            __syncwarp();
-        };
         while (ok && walk.next(a, TQ, g)) {
             wait(q_full, q_phase);
             q_phase ^= 1;
@@ -683,20 +711,44 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const uint32_t s = next_stage();
                 if (!ok) break;
                 fence_after();
-                if (elect_one()) {
-                    scores(0, qdesc, s);
-                    scores(1, qdesc + kStep, s);
-                    mma_commit(empty_bar(s));
-                    if (g.nt == 1) mma_commit(q_empty);
-                }
+                for (int slot = 0; slot < 2; ++slot)
+                    if (elect_one()) scores(slot, qdesc + slot * kStep, s);
+                if (elect_one()) mma_commit(g.nt == 1 ? q_empty : empty_bar(s));  // (the last keys' stage is the softmax's)
                 __syncwarp();
                 for (int t = 0; ok && t < g.nt; ++t) {
                     const uint32_t vs = next_stage();
                     const bool more = t + 1 < g.nt;
                     uint32_t ks = 0;
                     if (!ok) break;
-                    turn(0, vs, t > 0, more, ks, more, false);
-                    if (ok) turn(1, vs, t > 0, more, ks, false, t + 2 == g.nt);
+                    // each slot in turn: its weights with the values of stage vs, in two halves, then the scores of its next
+                    // key tile
+#pragma unroll
+                    for (int slot = 0; slot < 2; ++slot) {
+                        wait(p_half(slot), h_phase);
+                        if (!ok) break;
+                        fence_after();
+                        const uint64_t v = vdesc + vs * kStep;
+                        if (elect_one()) outputs(slot, 0, v, t > 0);
+                        __syncwarp();
+                        if (more && slot == 0) ks = next_stage();
+                        wait(p_full(slot), slot ? p_phase1 : p_phase0);
+                        if (!ok) break;
+                        fence_after();
+                        if (elect_one()) {
+                            outputs(slot, 32, v + 4 * (2048 >> 4), true);
+                            if (more) {
+                                scores(slot, qdesc + slot * kStep, ks);
+                                if (slot) mma_commit(t + 2 == g.nt ? q_empty : empty_bar(ks));
+                            } else {
+                                mma_commit(o_full(slot));
+                            }
+                            if (slot && more) mma_commit(empty_bar(vs));
+                        }
+                        __syncwarp();
+                    }
+                    h_phase ^= 1;
+                    p_phase0 ^= 1;
+                    p_phase1 ^= 1;
                 }
             } else {
                 uint32_t mine[2] = {0, 0};  // the stages of the slots' key tiles
@@ -704,8 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     // tile t - 2's weights with its values; then tile t's scores, in the same slot
                     const int slot = t & 1;
                     if (t >= 2) {
-                        const uint32_t phase = slot ? p_phase1 : p_phase0;
-                        wait(p_full(slot), phase);
+                        wait(p_full(slot), slot ? p_phase1 : p_phase0);
                         if (slot)
                             p_phase1 ^= 1;
                         else

@@ -43,10 +43,21 @@ __device__ __forceinline__ int tiles_of(int n, int len, int TQ, int p) {
     return lim <= kHalf ? 1 : (lim + kHalf - 1) / kHalf;
 }
 
-// Sum over 0 <= i < n of floor((a i + b) / 128), a, b >= 0: Euclid's steps on a and the divisor, the first of them by
-// shifts; what is left fits 32 bits.
+// Sum over 0 <= i < n of floor((a i + b) / 128), a, b >= 0.  a a power of two, as it is where the query heads a key head
+// are: floor((i + floor(b / a)) / (128 / a)), in closed form.  Else Euclid's steps on a and the divisor, the first of
+// them by shifts; what is left fits 32 bits.
 __device__ __forceinline__ int64_t floor_sum_128(uint32_t n, uint32_t a, int64_t b) {
     const int64_t nn = n;
+    if ((a & (a - 1)) == 0) {
+        if (a >= 128) return nn * (nn - 1) / 2 * (a >> 7) + nn * (b >> 7);
+        const int k = 7 - (31 - __clz(a));  // 128 / a = 2^k
+        auto upto = [&](int64_t x) {  // sum over 0 <= j < x of floor(j / 2^k)
+            const int64_t q = x >> k, r = x & ((1 << k) - 1);
+            return ((q * (q - 1) / 2) << k) + r * q;
+        };
+        const int64_t c = b >> (7 - k);
+        return upto(nn + c) - upto(c);
+    }
     int64_t s = nn * (nn - 1) / 2 * (a >> 7) + nn * (b >> 7);
     a &= 127;
     int64_t y = (int64_t)a * n + (b & 127);
@@ -85,7 +96,7 @@ inline __device__ int64_t tiles_before(int n, int len, int TQ, int p) {
 // What an item costs beside its keys (fetching queries, the first and the last tile's latency, writing out), in units of 64
 // keys: measured at 6,500 to 7,800 cycles for 3,500 a key tile of 128.  Blocks get at least kLeast units: fewer, and a
 // short call's parts cost more to join than they save.
-constexpr int kItemUnits = 4, kLeast = 8;
+constexpr int kItemUnits = 4, kLeast = 4;
 
 // By all threads of the block: where runs `block` and `block + 1` begin, to out[0] and out[1].  `scratch` holds B
 // int64_t and B int32_t (192 KB of shared memory at the most).
@@ -138,7 +149,11 @@ inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int
     if (warp < 2) {  // a warp for each of the two
         const int blocks = (int)max((int64_t)1, min((int64_t)kMaxBlocks, total / kLeast)), c = blockIdx.x + warp;
         Run r{total - (int64_t)kItemUnits * a.kv_heads * all_items, 0, 0, 0, 0};  // behind the last keys
-        const int64_t u = c >= blocks ? total : total / blocks * c + total % blocks * c / blocks;
+        // (64-bit divisions are calls; below 2^31 units, 32 bits do)
+        const bool small = total <= 0x7fffffff;
+        const int64_t each = small ? (int64_t)((uint32_t)total / (uint32_t)blocks) : total / blocks;
+        const uint32_t left = (uint32_t)(total - each * blocks);
+        const int64_t u = c >= blocks ? total : each * c + left * (uint32_t)c / (uint32_t)blocks;
         if (u < total) {
             int x = 0, y = B - 1;  // the last sequence whose units begin at or before u: empty ones share their number
             while (x < y) {
@@ -153,7 +168,7 @@ inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int
             const int pairs = pairs_of(n, TQ);
             const int64_t tiles = pairs == 1 ? tiles_of(n, len, TQ, 0) : tiles_before(n, len, TQ, pairs);
             const int64_t per_head = tiles + (int64_t)kItemUnits * pairs, in = u - units[x];
-            const int h = (int)(in / per_head);
+            const int h = small ? (int)((uint32_t)in / (uint32_t)per_head) : (int)(in / per_head);
             const int64_t rest = in - h * per_head;
             // the pair: of [p, p + count) in steps of a 32nd, by the lanes
             int p = 0, count = pairs;
