@@ -1,0 +1,103 @@
+"""Decoding rounds: the paged cache of a batch of sequences, from one verification to the next.
+
+A round feeds every sequence a chunk of new tokens (its last token and K drafted ones, or a prompt), attends from them
+over what is cached, and ends with the verification of the drafts, whose accept lengths decide what stays cached::
+
+    state = DecodeRounds(B, layers, n_blocks, block_size, kv_heads, head_dim, max_blocks)
+    plan = state.begin(prompt_lens, rows)            # rows: the host's bound for the sum of the lengths
+    for layer in range(layers):
+        o = state.attend(layer, q, k, v)             # appends k and v to the cache, attends over it
+    state.keep_all()                                 # a prompt is kept whole
+    while ...:
+        plan = state.begin(chunk_lens, rows)         # lengths, blocks and slots follow from the accept lengths on the GPU
+        for layer in range(layers):
+            o = state.attend(layer, q, k, v)
+        accept_len, tokens, groups, flags = state.verify(target_logits, draft_logits, draft_tokens, handle, uniforms)
+
+Nothing here waits for the GPU: lengths stay there from round to round.  The arithmetic is the library's
+(``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cache_attention``, ``pcg_prompt_attention``, ``pcg_verify``).
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import binding
+
+
+class DecodeRounds:
+    """Cache, block tables and lengths of ``B`` sequences (rows of a batch; a finished one's row is free for another).
+
+    ``n_blocks`` blocks of ``block_size`` tokens are shared by all sequences and all layers' caches alike; a sequence
+    holds ``max_blocks`` at most."""
+
+    def __init__(self, B: int, layers: int, n_blocks: int, block_size: int, kv_heads: int, head_dim: int, max_blocks: int,
+                 dtype=torch.bfloat16, device="cuda"):
+        if min(B, layers, n_blocks, max_blocks) < 1:
+            raise ValueError("B, layers, n_blocks and max_blocks must be at least 1")
+
+        def ints(*shape, fill=0):
+            return torch.full(shape, fill, dtype=torch.int32, device=device)
+
+        shape = (layers, n_blocks, kv_heads, block_size, head_dim)
+        self.k_cache = torch.empty(shape, dtype=dtype, device=device)
+        self.v_cache = torch.empty(shape, dtype=dtype, device=device)
+        self.block_size, self.B = block_size, B
+        self.block_table = ints(B, max_blocks, fill=-1)
+        self.free_ring = torch.arange(n_blocks, dtype=torch.int32, device=device)
+        self.ring_state = torch.tensor([0, n_blocks], dtype=torch.int32, device=device)
+        self.cached_len, self.held = ints(B), ints(B)
+        self.accept_len = ints(B, fill=-1)  # of the last round; -1: none of its tokens stays
+        self.new_len = None
+        self.plan: Optional[binding.CachePlan] = None
+        self._workspace = None
+
+    def begin(self, new_len, rows: int, stream=None) -> binding.CachePlan:
+        """Plans a round of ``new_len`` [B] new tokens a sequence (int32, on the device; negative: the sequence has
+        finished and its blocks are free again), packed into ``rows`` rows at the most.  ``plan.row_start`` and
+        ``plan.positions`` say which row is which token; a sequence with ``plan.flags`` set has no part in the round."""
+        if self.plan is not None:
+            raise RuntimeError("the last round has not ended: verify() or keep_all()")
+        plan = binding.pcg_cache_plan(self.cached_len, new_len, self.held, self.block_table, self.free_ring, self.ring_state,
+                                      self.block_size, rows, accept_len=self.accept_len, stream=stream)
+        self.plan, self.new_len = plan, new_len
+        self.cached_len, self.held, self.ring_state = plan.cached_len, plan.held, plan.ring_state
+        return plan
+
+    def attend(self, layer: int, q, k, v, scale: Optional[float] = None, fresh: bool = False, out=None, stream=None):
+        """One layer's attention of the round's rows: q [rows, q_heads, head_dim], k and v [rows, kv_heads, head_dim].
+
+        Writes k and v to the cache first.  ``fresh`` says that no sequence has anything cached, and every one of the
+        round's was given its blocks: the rows' own keys and values are then read instead of the cache."""
+        if self.plan is None:
+            raise RuntimeError("no round has begun")
+        plan, kc, vc = self.plan, self.k_cache[layer], self.v_cache[layer]
+        if self._workspace is None:
+            need = binding.pcg_attention_workspace_bytes(self.B, q.shape[1], k.shape[1], q.shape[2], binding.dtype_code(q))
+            self._workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        binding.pcg_cache_append(k, v, plan.slots, kc, vc, stream=stream)
+        if fresh:
+            return binding.pcg_prompt_attention(q, k, v, plan.row_start, scale=scale, out=out, workspace=self._workspace, stream=stream)
+        return binding.pcg_cache_attention(q, plan.row_start, plan.kv_len, self.block_table, kc, vc, scale=scale, out=out,
+                                           workspace=self._workspace, stream=stream)
+
+    def verify(self, target_logits, draft_logits, draft_tokens, groups, uniforms, temperature: float = 1.0, **kw):
+        """``pcg_verify`` of the round's drafts; of the chunk, its first token and the accepted drafts stay cached."""
+        if self.plan is None:
+            raise RuntimeError("no round has begun")
+        result = binding.pcg_verify(target_logits, draft_logits, draft_tokens, groups, uniforms, temperature, **kw)
+        self._end(result[0])
+        return result
+
+    def keep_all(self):
+        """Ends a round without drafts (a prompt, or a chunk of one): all of its tokens stay cached."""
+        if self.plan is None:
+            raise RuntimeError("no round has begun")
+        self._end(self.new_len - 1)
+
+    def _end(self, accept_len):
+        # a flagged sequence had no slots, a finished one has no tokens: nothing of the round stays
+        none = (self.plan.flags != 0) | (self.new_len < 1)
+        self.accept_len = torch.where(none, -1, accept_len).to(torch.int32)
+        self.plan = None
