@@ -210,7 +210,7 @@ extern "C" pcg_status pcg_cache_attention(const void *q, int64_t q_stride, int32
     }
     const AttnArgs a{q, cache->k, cache->v, out, row_start, kv_len, block_table, q_stride, 0, 0, rows, B, q_heads,
                      cache->kv_heads, cache->head_dim, max_blocks, cache->n_blocks, __builtin_ctz(cache->block_size),
-                     scale * 1.4426950408889634f};
+                     scale * 1.4426950408889634f, 0};
     st = check_attention(who, a, cache->dtype, scale);
     if (st != PCG_OK || rows == 0 || B == 0) return st;
     if (!kv_len || !block_table) {
@@ -232,7 +232,7 @@ extern "C" pcg_status pcg_prompt_attention(const void *q, int64_t q_stride, cons
         return PCG_ERR_INVALID_ARG;
     }
     const AttnArgs a{q, k, v, out, row_start, nullptr, nullptr, q_stride, k_stride, v_stride, rows, B, q_heads, kv_heads,
-                     head_dim, 0, 0, 0, scale * 1.4426950408889634f};
+                     head_dim, 0, 0, 0, scale * 1.4426950408889634f, 0};
     pcg_status st = check_attention(who, a, dtype, scale);
     if (st != PCG_OK || rows == 0 || B == 0) return st;
     st = check_rows(who, "k", k, k_stride, kv_heads, head_dim, dtype);

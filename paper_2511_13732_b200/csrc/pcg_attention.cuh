@@ -13,6 +13,7 @@ struct AttnArgs {
     int32_t rows, B, q_heads, kv_heads, d;
     int32_t max_blocks, n_blocks, bs_shift;
     float scale_log2;
+    int32_t few_tokens;  // (tensor cores) tokens of one copy of an item with one row tile
 };
 
 constexpr int kAttnMaxB = 16384, kAttnMaxGroup = 128;
