@@ -316,3 +316,95 @@ def test_two_streams_with_their_own_workspaces():
     for s, got in zip(sets, outs):
         s.check(got[0])
         assert all(torch.equal(got[0], x) for x in got)
+
+
+# ---- what the documentation allows and a model seldom does -----------------------------------------------------------
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128, 40])
+def test_outputs_and_queries_on_any_16_byte_boundary(dtype, d):
+    s = Paged([(300, 5), (70, 1), (0, 150)], 8, 2, d, 32, dtype, seed=50)
+    want = s.run()
+    step = 16 // want.element_size()
+    room = torch.zeros(want.numel() + 2 * step, dtype=dtype, device="cuda")
+    out = room[step: step + want.numel()].view(want.shape)
+    wide = torch.zeros((s.q.shape[0], s.q.shape[1] * d + step), dtype=dtype, device="cuda")  # rows 16 bytes apart from dense
+    q = wide[:, step:].unflatten(1, (s.q.shape[1], d))
+    q.copy_(s.q)
+    s.q = q
+    assert torch.equal(s.run(out=out), want)
+    assert not room[:step].any() and not room[step + want.numel():].any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_lengths_beyond_the_table_are_cut(dtype):
+    import cache_ref
+
+    s = Paged([(100, 5), (40, 3)], 4, 2, 64, 16, dtype, seed=51)
+    width = s.table.shape[1] * 16
+    s.kv_len = _ints([2 ** 31 - 1, width + 1])
+    got = s.run()
+    for b, n in ((0, 5), (1, 3)):
+        k, v = torch.zeros((width, 2, 64), dtype=dtype, device="cuda"), torch.zeros((width, 2, 64), dtype=dtype, device="cuda")
+        blocks = s.table[b].tolist()
+        used = [j for j in range(len(blocks)) if 0 <= blocks[j] < s.kc.shape[0]]
+        s.kc.nan_to_num_(0.0), s.vc.nan_to_num_(0.0)
+        for j in used:
+            k[16 * j: 16 * j + 16], v[16 * j: 16 * j + 16] = s.kc[blocks[j]].transpose(0, 1), s.vc[blocks[j]].transpose(0, 1)
+        rows = slice(0, 5) if b == 0 else slice(5, 8)
+        got = s.run()
+        cache_ref.check(got[rows], cache_ref.attention(s.q[rows], k, v, [width - n + i + 1 for i in range(n)], 0.125), dtype, 64, width)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_batch(dtype, d):
+    """16384 sequences of one token: each row is its own value; the next size is refused."""
+    from paper_2511_13732_b200 import binding
+
+    B = 16384
+    q, k, v = (torch.randn((B, h, d), device="cuda").to(dtype) for h in (4, 2, 2))
+    start = torch.arange(B + 1, dtype=torch.int32, device="cuda")
+    got = binding.pcg_prompt_attention(q, k, v, start)
+    assert torch.equal(got, v.repeat_interleave(2, 1))
+    kc, vc = (torch.zeros((B, 2, 16, d), dtype=dtype, device="cuda") for _ in range(2))
+    table = torch.randperm(B, device="cuda").to(torch.int32)[:, None].contiguous()
+    binding.pcg_cache_append(k, v, table[:, 0] * 16, kc, vc)
+    got = binding.pcg_cache_attention(q, start, torch.ones(B, dtype=torch.int32, device="cuda"), table, kc, vc)
+    assert torch.equal(got, v.repeat_interleave(2, 1))
+    with pytest.raises(binding.PcgError):
+        binding.pcg_prompt_attention(q, k, v, torch.arange(B + 2, dtype=torch.int32, device="cuda").clamp(max=B))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d", [64, 128])
+def test_mixed_batches_of_tokens_chunks_and_prompts(dtype, d):
+    """Items with one row tile and with two in one call, in any order: the ring's stages mean different things to them."""
+    rng = random.Random(d)
+    for seed in range(6):
+        lens = [(rng.choice([0, 3, 63, 64, 65, 500, 1300]), rng.choice([0, 1, 1, 2, 5, 17, 31, 32, 33, 64, 65, 96, 200, 400]))
+                for _ in range(rng.randint(1, 40))]
+        s = Paged(lens, 8, 2, d, rng.choice([16, 64, 256]), dtype, seed=60 + seed)
+        s.check(s.run())
+
+
+@pytest.mark.parametrize("heads", [(128, 1), (100, 1), (64, 2), (6, 2), (5, 1), (96, 3)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_and_odd_heads_a_key_head(heads, dtype):
+    s = Paged([(70, 1), (10, 4), (0, 9), (300, 2)], *heads, 64, 16, dtype, seed=70)
+    s.check(s.run())
+
+
+def test_calls_that_share_a_workspace_in_one_stream():
+    """Back to back, of different sizes and types, without a wait between them."""
+    from paper_2511_13732_b200 import binding
+
+    sets = [Paged([(900, 5), (20, 1)], 8, 2, 128, 32, torch.bfloat16, seed=80), Paged([(0, 400), (50, 3)], 8, 2, 64, 16, torch.float16, seed=81),
+            Paged([(333, 17)] * 5, 8, 2, 64, 16, torch.float32, seed=82)]
+    ws = torch.empty(max(binding.pcg_attention_workspace_bytes(9, 8, 2, d, 0) for d in (64, 128)), dtype=torch.uint8, device="cuda")
+    want = [s.run() for s in sets]
+    torch.cuda.synchronize()
+    outs = [[s.run(workspace=ws) for s in sets] for _ in range(8)]
+    torch.cuda.synchronize()
+    for s, w, got in zip(sets, want, zip(*outs)):
+        s.check(w)
+        assert all(torch.equal(w, x) for x in got)

@@ -188,3 +188,43 @@ def test_append_reaches_offsets_past_32_bits():
     binding.pcg_cache_append(k, v, _ints(slots), kc, vc)
     for r, s in enumerate(slots):
         assert torch.equal(kc[s // bs, :, s % bs], k[r]) and torch.equal(vc[s // bs, :, s % bs], v[r])
+
+
+def test_plan_and_append_on_another_stream():
+    from paper_2511_13732_b200 import binding
+    import cache_ref
+
+    side = torch.cuda.Stream()
+    st = _state(50, 16, random.Random(6))
+    rows = sum(max(n, 0) for n in st["new_len"])
+    want, table, _ = cache_ref.plan(rows=rows, **st)
+    d = {k: (v if k == "block_size" else _ints(v)) for k, v in st.items()}
+    kc, vc = (torch.zeros((len(st["free_ring"]), 2, 16, 64), device="cuda") for _ in range(2))
+    k = torch.randn((rows, 2, 64), device="cuda")
+    torch.cuda.synchronize()
+    p = binding.pcg_cache_plan(d["cached_len"], d["new_len"], d["held"], d["block_table"], d["free_ring"], d["ring_state"], 16, rows,
+                               accept_len=d["accept_len"], stream=side)
+    binding.pcg_cache_append(k, -k, p.slots, kc, vc, stream=side)
+    side.synchronize()
+    assert p.slots.tolist() == want["slots"] and d["block_table"].tolist() == table
+    for r, s in enumerate(want["slots"]):
+        if s >= 0:
+            assert torch.equal(kc[s // 16, :, s % 16], k[r]) and torch.equal(vc[s // 16, :, s % 16], -k[r])
+
+
+def test_plan_into_given_tensors_without_flags_and_positions():
+    from paper_2511_13732_b200 import binding
+    import cache_ref
+
+    st = _state(9, 32, random.Random(8))
+    rows = sum(max(n, 0) for n in st["new_len"])
+    want = cache_ref.plan(rows=rows, **st)[0]
+    d = {k: (v if k == "block_size" else _ints(v)) for k, v in st.items()}
+    e = lambda n: torch.full((n,), -9, dtype=torch.int32, device="cuda")  # noqa: E731
+    out = binding.CachePlan(e(9), e(9), e(9), e(10), e(rows), None, e(2), None)
+    got = binding.pcg_cache_plan(d["cached_len"], d["new_len"], d["held"], d["block_table"], d["free_ring"], d["ring_state"], 32, rows,
+                                 accept_len=d["accept_len"], out=out)
+    assert got is out and got.slots.tolist() == want["slots"] and got.held.tolist() == want["held"]
+    with pytest.raises(binding.PcgError):  # outputs that are inputs
+        binding.pcg_cache_plan(d["cached_len"], d["new_len"], d["held"], d["block_table"], d["free_ring"], d["ring_state"], 32, rows,
+                               accept_len=d["accept_len"], out=out._replace(held=d["held"]))
