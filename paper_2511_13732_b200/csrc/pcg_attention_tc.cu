@@ -54,13 +54,21 @@ __device__ __forceinline__ bool bar_poll(uint32_t bar, uint32_t parity) {
         : "memory");
     return done != 0;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed) {
+__device__ __forceinline__ bool bar_wait_hot(uint32_t bar, uint32_t parity, volatile int *failed) {
     for (uint32_t i = 0; i < kPolls; ++i) {
         if (bar_poll(bar, parity)) return true;
         if (*failed) return false;
     }
     *failed = 1;
     return false;
+}
+// The same with the loop out of line: there are some twenty waits, and with a loop in each the kernel's code misses the
+// instruction cache more often (256 drafted chunks: 265 us, so 247).  The products for head dimension 128 keep theirs.
+__device__ __noinline__ bool bar_wait_on(uint32_t bar, uint32_t parity, volatile int *failed) {
+    return bar_wait_hot(bar, parity, failed);
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed) {
+    return bar_poll(bar, parity) || bar_wait_on(bar, parity, failed);
 }
 // The same without a look at the failure flag: what is in flight is waited for after a failure too.
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
@@ -584,240 +592,237 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
             return block < 0 || block >= a.n_blocks ? a.n_blocks : block;  // behind the tensor: reads zeros
         };
-        // The next stage, once it has been read: `keys` rows of one of the tensors, or of both, one behind the other.
-        auto fetch = [&](const CUtensorMap *map, const CUtensorMap *second, int t, int32_t page) {
-            const uint32_t s = stage;
-            ok = ok && __all_sync(0xffffffffu, bar_wait(empty_bar(s), stage_phase, failed));
-            if (!ok) return;
-            if (++stage == S) {
-                stage = 0;
-                stage_phase ^= 1;
-            }
-            const int keys = second ? kHalf : kTile, k0 = (g.t0 + t) * keys;
-            // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
-            const int copies = min(keys / box, (max(g.len - k0, 0) + box - 1) / box);
-            int32_t block[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c) block[c] = paged ? __shfl_sync(0xffffffffu, page, c) : 0;
-            if (elect_one()) {
-                bar_expect(full_bar(s), copies * box * (second ? 2 : 1) * D * 2);
-                const uint32_t dst = ring + s * kTileBytes;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    if (c >= copies) break;
-                    const int r = k0 + c * box;
-                    const int c1 = paged ? r & ((1 << a.bs_shift) - 1) : g.h, c2 = paged ? g.h : g.begin + r;
-#pragma unroll
-                    for (int part = 0; part < kParts; ++part) {
-                        tma_load(dst + part * (keys * 128) + c * box * 128, map, part * 64, c1, c2, block[c], full_bar(s));
-                        if (second)
-                            tma_load(dst + kTileBytes / 2 + part * (keys * 128) + c * box * 128, second, part * 64, c1, c2, block[c], full_bar(s));
-                    }
-                }
-            }
-            __syncwarp();
-            ++it;
-        };
         bool have = walk.next(a, TQ, g);
         int32_t page0 = -1, page1 = -1, page2 = -1;  // blocks of the tiles t .. t + 2
-        auto first_pages = [&]() {
+        if (have) {
             page0 = page_of(g, 0);
             page1 = page_of(g, 1);
             page2 = page_of(g, 2);
-        };
-        if (have) first_pages();
+        }
         while (ok && have) {
             // the queries: G heads of TQ tokens at a time, which is the row tile's order
             if (items > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (items - 1) & 1, failed));
             if (!ok) break;
             ++items;
             if (elect_one()) {
-                if (g.two) {
-                    bar_expect(q_full, 2 * kParts * G * TQ * 128);
-                    for (int r = 0; r < 2; ++r)
-                        for (int part = 0; part < kParts; ++part)
-                            tma_load(qbuf + r * kTileBytes + part * (kTile * 128), &qmap, part * 64, 0, g.h,
-                                     g.begin + (g.pair * 2 + r) * TQ, q_full);
-                } else {  // its tokens, few_tokens() at a time
-                    const uint32_t tokens = g.n - g.pair * 2 * TQ, copies = (tokens + few - 1) / few;
-                    const bool all = copies * few_rows > kTile;  // the last copy would end behind the tile: all in one
-                    const uint32_t step = all ? kTile : few_rows;
-                    bar_expect(q_full, (all ? G * TQ : copies * few_rows) * kParts * 128);
+                // two row tiles, or the tokens of one, `few` at a time; all in one where the last copy would end behind the tile
+                const uint32_t tokens = g.n - g.pair * 2 * TQ, few_copies = (tokens + few - 1) / few;
+                const bool all = g.two || few_copies * few_rows > kTile;
+                const uint32_t rows = all ? G * TQ : few_rows, step = g.two ? kTile : few_rows, copies = g.two ? 2 : all ? 1 : few_copies;
+                bar_expect(q_full, copies * rows * kParts * 128);
 #pragma unroll 1
-                    for (uint32_t c = 0; c < (all ? 1 : copies); ++c)
+                for (uint32_t c = 0; c < copies; ++c)
 #pragma unroll
-                        for (int part = 0; part < kParts; ++part)
-                            tma_load(qbuf + part * (kTile * 128) + c * step * 128, all ? &qmap : &qmap_few, part * 64, 0, g.h,
-                                     g.begin + g.pair * 2 * TQ + c * few, q_full);
-                }
+                    for (int part = 0; part < kParts; ++part)  // (the second row tile's parts lie behind the first's)
+                        tma_load(qbuf + part * (kTile * 128) + c * step * 128 * (g.two ? kParts : 1), all ? &qmap : &qmap_few, part * 64, 0,
+                                 g.h, g.begin + g.pair * 2 * TQ + c * (all ? TQ : few), q_full);
             }
             __syncwarp();
-            if (g.two) {
-                fetch(&kmap, nullptr, 0, page0);
-                for (int t = 0; ok && t < g.nt; ++t) {
-                    const int32_t page3 = page_of(g, t + 3);  // its latency passes under the waits
-                    fetch(&vmap, nullptr, t, page0);
-                    if (t + 1 < g.nt) fetch(&kmap, nullptr, t + 1, page1);
+            // Two row tiles: the keys of tile 0, its values, the keys of tile 1, and so on, a stage each.  One: the keys and
+            // values of a tile in one stage.
+            Segment next;
+            int32_t next0 = -1, next1 = -1, next2 = -1;
+            const int loads = g.two ? 2 * g.nt : g.nt;
+#pragma unroll 1
+            for (int j = 0; j < loads; ++j) {
+                const int t = g.two ? j >> 1 : j, keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
+                const uint32_t s = stage;
+                ok = __all_sync(0xffffffffu, bar_wait(empty_bar(s), stage_phase, failed));
+                if (!ok) break;
+                if (++stage == S) {
+                    stage = 0;
+                    stage_phase ^= 1;
+                }
+                ++it;
+                // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
+                const int copies = min(keys / box, (max(g.len - k0, 0) + box - 1) / box);
+                if (elect_one()) bar_expect(full_bar(s), copies * box * (g.two ? 1 : 2) * D * 2);
+                __syncwarp();
+                const CUtensorMap *map = g.two && (j & 1) ? &vmap : &kmap;
+#pragma unroll 1
+                for (int c = 0; c < copies; ++c) {
+                    const int32_t block = paged ? __shfl_sync(0xffffffffu, page0, c) : 0;
+                    if (elect_one()) {
+                        const uint32_t dst = ring + s * kTileBytes + c * box * 128;
+                        const int r = k0 + c * box;
+                        const int c1 = paged ? r & ((1 << a.bs_shift) - 1) : g.h, c2 = paged ? g.h : g.begin + r;
+#pragma unroll
+                        for (int part = 0; part < kParts; ++part) {
+                            tma_load(dst + part * (keys * 128), map, part * 64, c1, c2, block, full_bar(s));
+                            if (!g.two) tma_load(dst + kTileBytes / 2 + part * (keys * 128), &vmap, part * 64, c1, c2, block, full_bar(s));
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (j == 0) {  // the next item's lengths and first blocks, looked up while this one's tiles are on their way
+                    have = walk.next(a, TQ, next);
+                    if (have) {
+                        next0 = page_of(next, 0);
+                        next1 = page_of(next, 1);
+                        next2 = page_of(next, 2);
+                    }
+                }
+                if (!g.two || (j & 1)) {
                     page0 = page1;
                     page1 = page2;
-                    page2 = page3;
+                    page2 = page_of(g, t + 3);  // its latency passes under the waits
                 }
-                have = walk.next(a, TQ, g);
-                if (have) first_pages();
-            } else {
-                // the next item's lengths and first blocks are looked up while this one's tiles are on their way
-                fetch(&kmap, &vmap, 0, page0);
-                Segment next;
-                have = walk.next(a, TQ, next);
-                const int32_t next0 = have ? page_of(next, 0) : -1, next1 = have ? page_of(next, 1) : -1, next2 = have ? page_of(next, 2) : -1;
-                for (int t = 1; ok && t < g.nt; ++t) {
-                    const int32_t page3 = page_of(g, t + 2);
-                    fetch(&kmap, &vmap, t, page1);
-                    page1 = page2;
-                    page2 = page3;
-                }
-                g = next;
-                page0 = next0;
-                page1 = next1;
-                page2 = next2;
             }
+            g = next;
+            page0 = next0;
+            page1 = next1;
+            page2 = next2;
         }
         if (*failed) {  // giving up: copies already asked for may still be landing
             if (items > 0) bar_drain(q_full, (items - 1) & 1);
             for (uint32_t back = 1; back <= S && back <= it; ++back) bar_drain(full_bar((it - back) % S), ((it - back) / S) & 1);
         }
     } else {
-        // ------------------------------------------------------------------ products: the warp waits, one lane issues
-        // stages in the order of their use, weights of a slot and queries: number (of a stage) and phase of the next
-        uint32_t stage = 0, stage_phase = 0, h_phase = 0, p_phase0 = 0, p_phase1 = 0, q_phase = 0;
-        bool ok = true;
-        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, failed)); };
-        auto next_stage = [&]() {  // waits for it
-            const uint32_t s = stage;
-            wait(full_bar(s), stage_phase);
-            if (++stage == S) {
-                stage = 0;
-                stage_phase ^= 1;
-            }
-            return s;
+        // ------------------------------------------------------------------ products
+        // Head dimension 128: one lane, elected once, waits and issues, which costs the fewest instructions between two
+        // products (a prompt of 8192: 525 us with the warp waiting and a lane elected for each issue, 512 so).  64: the warp
+        // waits (16 prompts of up to 1500: 101 us with one lane, 95 so: its code is the smaller).
+        constexpr bool kOneLane = D == 128;
+        auto issuing = [&]() { return kOneLane || elect_one(); };
+        auto together = [&]() {
+            if (!kOneLane) __syncwarp();
         };
-        const uint64_t qdesc = desc_k(qbuf), kdesc = desc_k(ring);
-        const uint64_t vdesc = desc_mn(ring, kTile), vdesc_half = desc_mn(ring + kTileBytes / 2, kHalf);
-        constexpr uint32_t kStep = kTileBytes >> 4;
-        // All by the elected lane.  A slot's scores of 128 or 64 keys; its weights of 16 * steps keys from column p on with
-        // their values.
-        auto scores = [&](int slot, uint64_t q, uint32_t s) {
-            constexpr int kPart = (kTile * 128) >> 4;
+        if (!kOneLane || elect_one()) {
+            // stages in the order of their use, weights of a slot and queries: number (of a stage) and phase of the next
+            uint32_t stage = 0, stage_phase = 0, h_phase = 0, p_phase0 = 0, p_phase1 = 0, q_phase = 0;
+            bool ok = true;
+            auto wait = [&](uint32_t bar, uint32_t parity) {
+                if (kOneLane)
+                    ok = ok && bar_wait_hot(bar, parity, failed);
+                else
+                    ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, failed));
+            };
+            auto next_stage = [&]() {  // waits for it
+                const uint32_t s = stage;
+                wait(full_bar(s), stage_phase);
+                if (++stage == S) {
+                    stage = 0;
+                    stage_phase ^= 1;
+                }
+                return s;
+            };
+            const uint64_t qdesc = desc_k(qbuf), kdesc = desc_k(ring);
+            const uint64_t vdesc = desc_mn(ring, kTile), vdesc_half = desc_mn(ring + kTileBytes / 2, kHalf);
+            constexpr uint32_t kStep = kTileBytes >> 4;
+            // All by the elected lane.  A slot's scores of 128 or 64 keys; 64 keys' weights, from column col on, with their values.
+            auto scores = [&](int slot, uint64_t q, uint32_t s) {
+                constexpr int kPart = (kTile * 128) >> 4;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-                mma_ss(s_col(slot), q + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPart + (kk & 3) * 2, kIdescQK, kk > 0);
-            mma_commit(s_full(slot));
-        };
-        auto scores_half = [&](int slot, uint32_t s) {
-            constexpr int kPart = (kTile * 128) >> 4, kPartK = (kHalf * 128) >> 4;
+                for (int kk = 0; kk < D / 16; ++kk)
+                    mma_ss(s_col(slot), q + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPart + (kk & 3) * 2, kIdescQK, kk > 0);
+                mma_commit(s_full(slot));
+            };
+            auto scores_half = [&](int slot, uint32_t s) {
+                constexpr int kPart = (kTile * 128) >> 4, kPartK = (kHalf * 128) >> 4;
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-                mma_ss(s_col(slot), qdesc + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPartK + (kk & 3) * 2, kIdescQKHalf,
-                       kk > 0);
-            mma_commit(s_full(slot));
-        };
-        auto outputs = [&](int slot, int col, uint64_t v, bool begun) {
+                for (int kk = 0; kk < D / 16; ++kk)
+                    mma_ss(s_col(slot), qdesc + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPartK + (kk & 3) * 2, kIdescQKHalf,
+                           kk > 0);
+                mma_commit(s_full(slot));
+            };
+            auto outputs = [&](int slot, int col, uint64_t v, bool begun) {
 #pragma unroll
-            for (int kk = 0; kk < kHalf / 16; ++kk)
-                mma_ts(o_col(slot), s_col(slot) + col + kk * 8, v + kk * (2048 >> 4), kIdescPV, begun || kk > 0);
-        };
-        while (ok && walk.next(a, TQ, g)) {
-            wait(q_full, q_phase);
-            q_phase ^= 1;
-            if (g.two) {
-                const uint32_t s = next_stage();
-                if (!ok) break;
-                fence_after();
-                for (int slot = 0; slot < 2; ++slot)
-                    if (elect_one()) scores(slot, qdesc + slot * kStep, s);
-                if (elect_one()) mma_commit(g.nt == 1 ? q_empty : empty_bar(s));  // (the last keys' stage is the softmax's)
-                __syncwarp();
-                for (int t = 0; ok && t < g.nt; ++t) {
-                    const uint32_t vs = next_stage();
-                    const bool more = t + 1 < g.nt;
-                    uint32_t ks = 0;
+                for (int kk = 0; kk < kHalf / 16; ++kk)
+                    mma_ts(o_col(slot), s_col(slot) + col + kk * 8, v + kk * (2048 >> 4), kIdescPV, begun || kk > 0);
+            };
+            while (ok && walk.next(a, TQ, g)) {
+                wait(q_full, q_phase);
+                q_phase ^= 1;
+                if (g.two) {
+                    const uint32_t s = next_stage();
                     if (!ok) break;
-                    // each slot in turn: its weights with the values of stage vs, in two halves, then the scores of its next
-                    // key tile
+                    fence_after();
+                    for (int slot = 0; slot < 2; ++slot)
+                        if (issuing()) scores(slot, qdesc + slot * kStep, s);
+                    if (issuing()) mma_commit(g.nt == 1 ? q_empty : empty_bar(s));  // (the last keys' stage is the softmax's)
+                    together();
+                    for (int t = 0; ok && t < g.nt; ++t) {
+                        const uint32_t vs = next_stage();
+                        const bool more = t + 1 < g.nt;
+                        uint32_t ks = 0;
+                        if (!ok) break;
+                        // each slot in turn: its weights with the values of stage vs, in two halves, then the scores of its next
+                        // key tile
 #pragma unroll
-                    for (int slot = 0; slot < 2; ++slot) {
-                        wait(p_half(slot), h_phase);
-                        if (!ok) break;
-                        fence_after();
-                        const uint64_t v = vdesc + vs * kStep;
-                        if (elect_one()) outputs(slot, 0, v, t > 0);
-                        __syncwarp();
-                        if (more && slot == 0) ks = next_stage();
-                        wait(p_full(slot), slot ? p_phase1 : p_phase0);
-                        if (!ok) break;
-                        fence_after();
-                        if (elect_one()) {
-                            outputs(slot, 32, v + 4 * (2048 >> 4), true);
-                            if (more) {
-                                scores(slot, qdesc + slot * kStep, ks);
-                                if (slot) mma_commit(t + 2 == g.nt ? q_empty : empty_bar(ks));
-                            } else {
-                                mma_commit(o_full(slot));
+                        for (int slot = 0; slot < 2; ++slot) {
+                            wait(p_half(slot), h_phase);
+                            if (!ok) break;
+                            fence_after();
+                            const uint64_t v = vdesc + vs * kStep;
+                            if (issuing()) outputs(slot, 0, v, t > 0);
+                            together();
+                            if (more && slot == 0) ks = next_stage();
+                            wait(p_full(slot), slot ? p_phase1 : p_phase0);
+                            if (!ok) break;
+                            fence_after();
+                            if (issuing()) {
+                                outputs(slot, 32, v + 4 * (2048 >> 4), true);
+                                if (more) {
+                                    scores(slot, qdesc + slot * kStep, ks);
+                                    if (slot) mma_commit(t + 2 == g.nt ? q_empty : empty_bar(ks));
+                                } else {
+                                    mma_commit(o_full(slot));
+                                }
+                                if (slot && more) mma_commit(empty_bar(vs));
                             }
-                            if (slot && more) mma_commit(empty_bar(vs));
+                            together();
                         }
-                        __syncwarp();
+                        h_phase ^= 1;
+                        p_phase0 ^= 1;
+                        p_phase1 ^= 1;
                     }
-                    h_phase ^= 1;
-                    p_phase0 ^= 1;
-                    p_phase1 ^= 1;
-                }
-            } else {
-                uint32_t mine[2] = {0, 0};  // the stages of the slots' key tiles
-                for (int t = 0; ok && t < g.nt + 2; ++t) {
-                    // tile t - 2's weights with its values; then tile t's scores, in the same slot
-                    const int slot = t & 1;
-                    if (t >= 2) {
-                        wait(p_full(slot), slot ? p_phase1 : p_phase0);
-                        if (slot)
-                            p_phase1 ^= 1;
-                        else
-                            p_phase0 ^= 1;
-                        if (!ok) break;
-                        fence_after();
-                        const uint32_t s = slot ? mine[1] : mine[0];
-                        if (elect_one()) {
-                            outputs(slot, 0, vdesc_half + s * kStep, t >= 4);
-                            mma_commit(empty_bar(s));
-                            if (t >= g.nt) mma_commit(o_full(slot));
+                } else {
+                    uint32_t mine[2] = {0, 0};  // the stages of the slots' key tiles
+                    for (int t = 0; ok && t < g.nt + 2; ++t) {
+                        // tile t - 2's weights with its values; then tile t's scores, in the same slot
+                        const int slot = t & 1;
+                        if (t >= 2) {
+                            wait(p_full(slot), slot ? p_phase1 : p_phase0);
+                            if (slot)
+                                p_phase1 ^= 1;
+                            else
+                                p_phase0 ^= 1;
+                            if (!ok) break;
+                            fence_after();
+                            const uint32_t s = slot ? mine[1] : mine[0];
+                            if (issuing()) {
+                                outputs(slot, 0, vdesc_half + s * kStep, t >= 4);
+                                mma_commit(empty_bar(s));
+                                if (t >= g.nt) mma_commit(o_full(slot));
+                            }
+                            together();
+                        } else if (t >= g.nt) {
+                            continue;  // one key tile: the other slot has none
                         }
-                        __syncwarp();
-                    } else if (t >= g.nt) {
-                        continue;  // one key tile: the other slot has none
-                    }
-                    if (t < g.nt) {
-                        const uint32_t s = next_stage();
-                        if (!ok) break;
-                        fence_after();
-                        if (slot)
-                            mine[1] = s;
-                        else
-                            mine[0] = s;
-                        if (elect_one()) {
-                            scores_half(slot, s);
-                            if (t == g.nt - 1) mma_commit(q_empty);
+                        if (t < g.nt) {
+                            const uint32_t s = next_stage();
+                            if (!ok) break;
+                            fence_after();
+                            if (slot)
+                                mine[1] = s;
+                            else
+                                mine[0] = s;
+                            if (issuing()) {
+                                scores_half(slot, s);
+                                if (t == g.nt - 1) mma_commit(q_empty);
+                            }
+                            together();
                         }
-                        __syncwarp();
                     }
                 }
             }
-        }
-        if (*failed) {  // products already issued may still be writing tensor memory: it is freed when they have retired
-            __syncwarp();
-            if (elect_one()) mma_commit(drain);
-            __syncwarp();
-            bar_drain(drain, 0);
-        }
+            if (*failed) {  // products already issued may still be writing tensor memory: it is freed when they have retired
+                together();
+                if (issuing()) mma_commit(drain);
+                together();
+                bar_drain(drain, 0);
+            }
+            }
     }
     fence_before();
     __syncthreads();
