@@ -627,6 +627,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = 0; j < loads; ++j) {
                 const int t = g.two ? j >> 1 : j, keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
                 const uint32_t s = stage;
+                const int32_t page3 = page_of(g, t + 3);  // its latency passes under the wait
                 ok = __all_sync(0xffffffffu, bar_wait(empty_bar(s), stage_phase, failed));
                 if (!ok) break;
                 if (++stage == S) {
@@ -636,24 +637,33 @@ __global__ void __launch_bounds__(kThreads, 1)
                 ++it;
                 // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
                 const int copies = min(keys / box, (max(g.len - k0, 0) + box - 1) / box);
-                if (elect_one()) bar_expect(full_bar(s), copies * box * (g.two ? 1 : 2) * D * 2);
-                __syncwarp();
                 const CUtensorMap *map = g.two && (j & 1) ? &vmap : &kmap;
+                const uint32_t bar = full_bar(s);
+                int c0 = 0;
 #pragma unroll 1
-                for (int c = 0; c < copies; ++c) {
-                    const int32_t block = paged ? __shfl_sync(0xffffffffu, page0, c) : 0;
-                    if (elect_one()) {
-                        const uint32_t dst = ring + s * kTileBytes + c * box * 128;
-                        const int r = k0 + c * box;
-                        const int c1 = paged ? r & ((1 << a.bs_shift) - 1) : g.h, c2 = paged ? g.h : g.begin + r;
+                do {  // (four at a time: small blocks' copies are paced by their issue)
+                    int32_t block[4];
 #pragma unroll
-                        for (int part = 0; part < kParts; ++part) {
-                            tma_load(dst + part * (keys * 128), map, part * 64, c1, c2, block, full_bar(s));
-                            if (!g.two) tma_load(dst + kTileBytes / 2 + part * (keys * 128), &vmap, part * 64, c1, c2, block, full_bar(s));
+                    for (int c = 0; c < 4; ++c) block[c] = paged ? __shfl_sync(0xffffffffu, page0, c0 + c) : 0;
+                    if (elect_one()) {
+                        if (c0 == 0) bar_expect(bar, copies * box * (g.two ? 1 : 2) * D * 2);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            if (c0 + c >= copies) break;
+                            const uint32_t dst = ring + s * kTileBytes + (c0 + c) * box * 128;
+                            const int r = k0 + (c0 + c) * box;
+                            const int c1 = paged ? r & ((1 << a.bs_shift) - 1) : g.h, c2 = paged ? g.h : g.begin + r;
+#pragma unroll
+                            for (int part = 0; part < kParts; ++part) {
+                                tma_load(dst + part * (keys * 128), map, part * 64, c1, c2, block[c], bar);
+                                if (!g.two)
+                                    tma_load(dst + kTileBytes / 2 + part * (keys * 128), &vmap, part * 64, c1, c2, block[c], bar);
+                            }
                         }
                     }
                     __syncwarp();
-                }
+                    c0 += 4;
+                } while (c0 < copies);
                 if (j == 0) {  // the next item's lengths and first blocks, looked up while this one's tiles are on their way
                     have = walk.next(a, TQ, next);
                     if (have) {
@@ -665,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (!g.two || (j & 1)) {
                     page0 = page1;
                     page1 = page2;
-                    page2 = page_of(g, t + 3);  // its latency passes under the waits
+                    page2 = page3;
                 }
             }
             g = next;
