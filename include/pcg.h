@@ -430,7 +430,8 @@ size_t pcg_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t kv_head
  *
  *   q          [rows, q_heads, head_dim] of the cache's type, token r at q + r * q_stride elements (16-byte aligned,
  *              stride a multiple of 16 bytes and at least q_heads * head_dim elements)
- *   row_start  [B + 1], kv_len [B], block_table [B, max_blocks]; kv_len is clamped to 0 .. max_blocks * block_size
+ *   row_start  [B + 1], kv_len [B], block_table [B, max_blocks]; kv_len is clamped to 0 .. max_blocks * block_size,
+ *              which is at most 2^31 - 256
  *   out        [rows, q_heads, head_dim], dense, 16-byte aligned; rows outside every sequence are left as they were
  *   scale      > 0, finite
  *   workspace  >= pcg_attention_workspace_bytes(...), contents irrelevant on entry; calls that share one must not

@@ -204,8 +204,8 @@ extern "C" pcg_status pcg_cache_attention(const void *q, int64_t q_stride, int32
     const char *who = "pcg_cache_attention";
     pcg_status st = check_cache(who, cache);
     if (st != PCG_OK) return st;
-    if (max_blocks < 1 || (int64_t)max_blocks * cache->block_size > 0x7fffffff) {
-        set_error("%s: max_blocks must be at least 1, and max_blocks * block_size below 2^31 (got %d)", who, max_blocks);
+    if (max_blocks < 1 || (int64_t)max_blocks * cache->block_size > 0x7fffff00) {  // a key tile's end fits 31 bits
+        set_error("%s: max_blocks must be at least 1, and max_blocks * block_size at most 2^31 - 256 (got %d)", who, max_blocks);
         return PCG_ERR_INVALID_ARG;
     }
     const AttnArgs a{q, cache->k, cache->v, out, row_start, kv_len, block_table, q_stride, 0, 0, rows, B, q_heads,

@@ -11,6 +11,9 @@
 //                                           turn, and their sums meet at the end.  Bound by HBM: a stage of the ring waits
 //                                           for its tile's softmax, so that half as large a tile leaves more of the ring
 //                                           for tiles that are on their way.
+// Measured (after a pause, 1.7 to 1.9 GHz): one prompt of 8192, 32 / 8 heads x 128, 502 us = 1095 TFLOP/s (65 % of the
+// measured cuBLAS burst); 64 tokens over up to 8000 cached, the same heads, 197 us = 5.98 TB/s (93 % of the measured copy).
+//
 // attention_tc_kernel        Every block first cuts the call's work into one equal run per block, whatever the lengths are:
 //                            it numbers the units of all items, one for each 64 keys and four for what an item costs
 //                            beside its keys, and looks up where its own run begins and ends.  No block waits for
@@ -263,7 +266,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 
     if (tid == 0) {
         for (int i = 0; i < 2 * S + 15; ++i) {
-            // by warps: the weights of a slot (4), the hand-over (4 and 4); by one thread or the hardware: all others
+            // by a slot's warps: its weights, its outputs (4); by both slots': the hand-over (8); by one thread or the
+            // hardware: all others
             const uint32_t bar = bar0 + 8u * i;
             const uint32_t count = bar == p_full(0) || bar == p_full(1) || bar >= p_half(0) ? 4 : bar >= merge_full ? 8 : 1;
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));

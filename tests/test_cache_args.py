@@ -79,7 +79,7 @@ BOTH = [dict(q=None), dict(q=P + 8), dict(rows=-1), dict(B=-1), dict(q_heads=3),
         dict(out=P + 4), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))]
 
 
-@pytest.mark.parametrize("bad", BOTH + [dict(kv=None), dict(table=None), dict(max_blocks=0), dict(max_blocks=1 << 28), dict(stride=248),
+@pytest.mark.parametrize("bad", BOTH + [dict(kv=None), dict(table=None), dict(max_blocks=0), dict(max_blocks=1 << 28), dict(max_blocks=134217727), dict(stride=248),
                                         dict(stride=260)])
 def test_cache_attention_refusals(bad):
     assert _attend(**bad) == INVALID
