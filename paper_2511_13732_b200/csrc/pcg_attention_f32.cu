@@ -1,7 +1,7 @@
 // Attention in float32 on the FMA pipes, head dimensions 64 and 128: the work is shared out as for the tensor cores
-// (pcg_attention_work.cuh), a block's run is gone through 64 rows by 64 keys at a time.
+// (pcg_attention_work.cuh), a block's run is gone through 64 or 32 rows by 64 keys at a time.
 //
-// Thread (ty, tx) of 16 x 16 has rows 4 ty .. 4 ty + 3: their scores with keys tx, tx + 16, tx + 32, tx + 48, and their
+// Thread (ty, tx) of 16 x 16 has rows R ty .. R ty + R - 1, R = 4 or 2: their scores with keys tx, tx + 16, tx + 32, tx + 48, and their
 // outputs in dimensions 4 tx .. (and 64 + 4 tx ..).  Operands come out of shared memory as 16-byte vectors, sixteen products
 // for two of them; keys and values of the next 64 keys arrive (cp.async) while these are worked on.  Warps whose rows are all
 // padding, as most are for a drafted chunk's few rows, skip the arithmetic.
@@ -9,6 +9,7 @@
 // to 700 tokens, 12 / 4 heads x 64: 28 us for 14 MB; a block per row and head took 109).
 #include <atomic>
 #include <cstddef>
+#include <type_traits>
 
 #include "pcg_attention_work.cuh"
 
@@ -57,28 +58,27 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
         const int k_begin = g.t0 * keys, k_end = min((g.t0 + g.nt) * keys, g.len);
         const int tokens = min(g.n - g.pair * 2 * TQ, 2 * TQ);
         float *part = part_base(ws, blockIdx.x, g.t0 == 0 ? 1 : 0, D);
-        // the rows of both row tiles, 64 at a time: row r of tile r / 128 has token (r / 128) TQ + (r % 128) / G
-        for (int r0 = 0; r0 < (g.two ? 2 * kTile : kTile); r0 += kF32Rows) {
-            const int in0 = r0 & (kTile - 1);
-            if (in0 / G >= TQ || (r0 / kTile) * TQ + in0 / G >= tokens) continue;  // padding from its first row on
+        // Row r of tile r / 128 has token (r / 128) TQ + (r % 128) / G.  16 * R rows from r0 on, R of them a thread.
+        auto work = [&](auto rows_each, int r0) {
+            constexpr int R = decltype(rows_each)::value, kRows = 16 * R;
             auto token_of = [&](int r) {  // of the row in its sequence, or -1
                 const int in = r & (kTile - 1), tok = (r / kTile) * TQ + in / G;
                 return in / G >= TQ || tok >= tokens ? -1 : g.pair * 2 * TQ + tok;
             };
-            int lim[4];
+            int lim[R];
             bool any = false;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = token_of(r0 + 4 * ty + i);
+            for (int i = 0; i < R; ++i) {
+                const int t = token_of(r0 + R * ty + i);
                 lim[i] = t < 0 ? 0 : g.len - g.n + t + 1;
                 any = any || t >= 0;
             }
             any = __any_sync(0xffffffffu, any);
-            // what the 64 rows' last one sees
-            int last = token_of(r0 + kF32Rows - 1);
+            // what the last of these rows sees
+            int last = token_of(r0 + kRows - 1);
             if (last < 0) last = r0 < kTile && tokens > TQ ? g.pair * 2 * TQ + TQ - 1 : g.pair * 2 * TQ + tokens - 1;
             const int k_stop = min(k_end, g.len - g.n + last + 1);
-            for (int i = tid; i < kF32Rows * V; i += kF32Threads) {
+            for (int i = tid; i < kRows * V; i += kF32Threads) {
                 const int r = i / V, c = i % V, t = token_of(r0 + r);
                 const float *from = (const float *)a.q + ((int64_t)g.begin + max(t, 0)) * a.q_stride +
                                     (int64_t)(g.h * G + ((r0 + r) & (kTile - 1)) % G) * D + c * 4;
@@ -115,9 +115,9 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
                 look_up(k0 + kF32Keys);
             };
             look_up(k_begin);
-            float m[4], l[4], o[4][4 * N];
+            float m[R], l[R], o[R][4 * N];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < R; ++i) {
                 m[i] = kNegInf;
                 l[i] = 0.f;
 #pragma unroll
@@ -130,20 +130,20 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
                 __syncthreads();
                 if (any) {
-                    float s[4][4];
+                    float s[R][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int i = 0; i < R; ++i)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 4
                     for (int c = 0; c < D; c += 4) {
-                        float4 x[4], y[4];
+                        float4 x[R], y[4];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4 *>(&sh.q[4 * ty + i][c]);
+                        for (int i = 0; i < R; ++i) x[i] = *reinterpret_cast<const float4 *>(&sh.q[R * ty + i][c]);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4 *>(&sh.k[buf][tx + 16 * j][c]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
+                        for (int i = 0; i < R; ++i)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 s[i][j] = fmaf(x[i].x, y[j].x, s[i][j]);
@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
                             }
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < R; ++i) {
                         float top = kNegInf;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -174,22 +174,22 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
                             // masked places and scores of -inf weigh 0, whatever the reference is
                             const float w = s[i][j] == kNegInf ? 0.f : exp2f(s[i][j] - m[i]);
                             l[i] += w;
-                            sh.p[4 * ty + i][tx + 16 * j] = w;
+                            sh.p[R * ty + i][tx + 16 * j] = w;
                         }
                     }
                     __syncwarp();  // a row's weights come from 16 lanes of this warp
 #pragma unroll 2
                     for (int c = 0; c < kF32Keys; c += 4) {
-                        float4 w[4];
+                        float4 w[R];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4 *>(&sh.p[4 * ty + i][c]);
+                        for (int i = 0; i < R; ++i) w[i] = *reinterpret_cast<const float4 *>(&sh.p[R * ty + i][c]);
 #pragma unroll
                         for (int n = 0; n < N; ++n)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const float4 y = *reinterpret_cast<const float4 *>(&sh.v[buf][c + e][64 * n + 4 * tx]);
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) {
+                                for (int i = 0; i < R; ++i) {
                                     const float x = e == 0 ? w[i].x : e == 1 ? w[i].y : e == 2 ? w[i].z : w[i].w;
                                     o[i][4 * n] = fmaf(x, y.x, o[i][4 * n]);
                                     o[i][4 * n + 1] = fmaf(x, y.y, o[i][4 * n + 1]);
@@ -203,10 +203,10 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
             }
             asm volatile("cp.async.wait_group 0;" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < R; ++i) {
 #pragma unroll
                 for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
-                const int r = r0 + 4 * ty + i, t = token_of(r);
+                const int r = r0 + R * ty + i, t = token_of(r);
                 if (t < 0) continue;
                 if (g.whole) {
                     const float inv = 1.f / l[i];  // 0 / 0 where every score was -inf
@@ -226,6 +226,21 @@ __global__ void __launch_bounds__(kF32Threads, 1) attention_f32_kernel(const __g
                 }
             }
             __syncthreads();  // the queries are read
+                };
+        // 64 rows at a time, and 32 where no more are left: with four rows a thread, more than half of the warps would have
+        // nothing to do (four, then two rows a thread: 15 rows over 300 tokens 20.9 -> 18.1 us, 16 x 68 over 1500 354 -> 322;
+        // 16 x 27 over up to 700, where each way most warps work or wait on one another, 28.4 -> 29.3)
+        for (int tile = 0; tile < (g.two ? 2 : 1); ++tile) {
+            const int rows = min(tokens - tile * TQ, TQ) * G;
+            for (int r = 0; r < rows;) {
+                if (rows - r <= 32) {
+                    work(std::integral_constant<int, 2>{}, tile * kTile + r);
+                    r += 32;
+                } else {
+                    work(std::integral_constant<int, 4>{}, tile * kTile + r);
+                    r += 64;
+                }
+            }
         }
     }
 }
