@@ -6,7 +6,7 @@
 // for two of them; keys and values of the next 64 keys arrive (cp.async) while these are worked on.  Warps whose rows are all
 // padding, as most are for a drafted chunk's few rows, skip the arithmetic.
 // What bounds it: the FMA pipes for chunks of prompts; for few rows the latency of a run's steps (16 chunks of 9 rows over up
-// to 700 tokens, 12 / 4 heads x 64: 28 us for 14 MB; a block per row and head took 109).
+// to 700 tokens, 12 / 4 heads x 64: 29 us for 14 MB; a block per row and head took 109).
 #include <atomic>
 #include <cstddef>
 #include <type_traits>
