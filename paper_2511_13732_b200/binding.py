@@ -168,6 +168,38 @@ def _stream_ptr(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+# A call on a stream other than the caller's current one: PyTorch's allocator orders the reuse of memory by the stream
+# that was current when it was allocated, so the call's own buffers are made on the call's stream, and the caller's
+# tensors are marked as used there.  (What the call reads has to be complete on that stream: its order is the caller's.)
+def _beside(stream, dev: int):
+    """The call's stream, where it is not device `dev`'s current one; else None."""
+    import torch
+
+    if stream is None or stream.cuda_stream == torch._C._cuda_getCurrentRawStream(dev):
+        return None
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=dev)
+
+
+def _empty(like, shape, dtype, beside):
+    """A new tensor on the device of `like`, for a call on the current stream or on the one `beside` it."""
+    import torch
+
+    if beside is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(beside):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream(like.device))  # a caller who waits for the call may read it there
+    return t
+
+
+def _lend(beside, *tensors):
+    """Memory of the caller's tensors is not given out again before the call on `beside` is done with it."""
+    if beside is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(beside)
+
+
 def dtype_code(t) -> int:
     import torch
 
@@ -227,11 +259,12 @@ def pcg_group_probs(logits, groups: Groups, temperature: float = 1.0, out=None, 
 
     if logits.dim() != 2 or logits.shape[1] != groups.V or not logits.is_contiguous() or not logits.is_cuda:
         raise ValueError("logits must be a contiguous CUDA tensor [rows, V]")
-    rows = logits.shape[0]
+    rows, beside = logits.shape[0], _beside(stream, logits.get_device())
     if out is None:
-        out = torch.empty((rows, groups.M), dtype=torch.float32, device=logits.device)
+        out = _empty(logits, (rows, groups.M), torch.float32, beside)
     elif tuple(out.shape) != (rows, groups.M) or out.dtype != torch.float32 or not out.is_contiguous() or out.device != logits.device:
         raise ValueError("out must be a contiguous float32 tensor [rows, M] on the logits' device")
+    _lend(beside, logits, out, workspace)
     if workspace is None:
         _check(load().pcg_group_probs(_dev_ptr(logits), dtype_code(logits), rows, float(temperature), groups.handle,
                                       _dev_ptr(out), _stream_ptr(stream)))
@@ -287,18 +320,19 @@ def pcg_verify(target_logits, draft_logits, draft_tokens, groups: Groups, unifor
     import torch
 
     B, K, V = _check_verify_tensors(target_logits, draft_logits, draft_tokens, groups, uniforms, out)
-    dev = target_logits.device
     dt = dtype_code(target_logits)
     need = pcg_verify_workspace_bytes(B, K, V, groups.M, dt, mode)
+    beside = _beside(stream, target_logits.get_device())
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        workspace = _empty(target_logits, need, torch.uint8, beside)
     if out is None:
-        accept_len = torch.empty(B, dtype=torch.int32, device=dev)
-        tokens = torch.empty((B, K + 1), dtype=torch.int32, device=dev)
-        grp = torch.empty((B, K + 1), dtype=torch.int32, device=dev) if want_groups else None
-        flags = torch.empty(B, dtype=torch.int32, device=dev) if want_flags else None
+        accept_len = _empty(target_logits, B, torch.int32, beside)
+        tokens = _empty(target_logits, (B, K + 1), torch.int32, beside)
+        grp = _empty(target_logits, (B, K + 1), torch.int32, beside) if want_groups else None
+        flags = _empty(target_logits, B, torch.int32, beside) if want_flags else None
     else:
         accept_len, tokens, grp, flags = out
+    _lend(beside, target_logits, draft_logits, draft_tokens, uniforms, workspace, accept_len, tokens, grp, flags)
     ev = None
     if stage_events is not None:
         ev = (ctypes.c_void_p * 3)(*[ctypes.c_void_p(e.cuda_event) for e in stage_events])
@@ -334,6 +368,7 @@ def pcg_verify_static(target_logits, draft_logits, draft_tokens, groups: Groups,
     in ``out`` included (groups and flags may be None), is supplied by the caller; nothing is allocated here."""
     B, K, V = _check_verify_tensors(target_logits, draft_logits, draft_tokens, groups, uniforms, out)
     accept_len, tokens, grp, flags = out
+    _lend(_beside(stream, target_logits.get_device()), target_logits, draft_logits, draft_tokens, uniforms, *out)
     _check(load().pcg_verify_static(_dev_ptr(target_logits), _dev_ptr(draft_logits), dtype_code(target_logits), B,
                                     K, _dev_ptr(draft_tokens), groups.handle, _dev_ptr(uniforms),
                                     float(temperature), _dev_ptr(accept_len), _dev_ptr(tokens), _dev_ptr(grp),
@@ -359,15 +394,14 @@ def pcg_verify_thinning(target_logits, draft_logits, draft_tokens, groups: Group
     n_trials = int(thin_uniforms.shape[1])
     B, K, V = _check_verify_tensors(target_logits, draft_logits, draft_tokens, groups, uniforms, out,
                                     extra=[(thin_uniforms, (target_logits.shape[0], n_trials, 3), torch.float32)])
-    dev = target_logits.device
     dt = dtype_code(target_logits)
+    beside = _beside(stream, target_logits.get_device())
     if workspace is None:
-        workspace = torch.empty(pcg_verify_thinning_workspace_bytes(B, K, V, groups.M, dt), dtype=torch.uint8, device=dev)
+        workspace = _empty(target_logits, pcg_verify_thinning_workspace_bytes(B, K, V, groups.M, dt), torch.uint8, beside)
     if out is None:
-        out = (torch.empty(B, dtype=torch.int32, device=dev), torch.empty((B, K + 1), dtype=torch.int32, device=dev),
-               torch.empty((B, K + 1), dtype=torch.int32, device=dev), torch.empty(B, dtype=torch.int32, device=dev),
-               torch.empty(B, dtype=torch.int32, device=dev))
+        out = tuple(_empty(target_logits, shape, torch.int32, beside) for shape in (B, (B, K + 1), (B, K + 1), B, B))
     accept_len, tokens, grp, flags, trials = out
+    _lend(beside, target_logits, draft_logits, draft_tokens, uniforms, thin_uniforms, workspace, *out)
     ev = None
     if stage_events is not None:
         ev = (ctypes.c_void_p * 3)(*[ctypes.c_void_p(e.cuda_event) for e in stage_events])
@@ -502,8 +536,9 @@ def pcg_cache_plan(cached_len, new_len, held, block_table, free_ring, ring_state
             _int_ptr(block_table, (B, max_blocks), dev), _int_ptr(free_ring, (ring_size,), dev), ring_size,
             _int_ptr(ring_state, (2,), dev), rows)
     sizes = (B, B, B, B + 1, rows, rows, 2, B)
+    beside = _beside(stream, dev)
     if out is None:
-        buf = cached_len.new_empty(5 * B + 2 * rows + 3)
+        buf = _empty(cached_len, 5 * B + 2 * rows + 3, torch.int32, beside)
         p = buf.data_ptr()
         ptrs = []
         for n in sizes:
@@ -512,6 +547,7 @@ def pcg_cache_plan(cached_len, new_len, held, block_table, free_ring, ring_state
         out = CachePlan(*torch.split_with_sizes(buf, sizes))
     else:
         ptrs = [None if t is None else _int_ptr(t, (n,), dev) for t, n in zip(out, sizes)]
+    _lend(beside, cached_len, new_len, held, block_table, free_ring, ring_state, accept_len, *out)
     _check((_lib or load()).pcg_cache_plan(*args, *ptrs, _stream_of(stream, dev)))
     return out
 
@@ -524,6 +560,7 @@ def pcg_cache_append(k, v, slots, k_cache, v_cache, stream=None):
     vshape, vs = _packed(v, "v", k_cache.dtype, dev)
     _need(shape == vshape and shape[1] == cache.kv_heads and shape[2] == cache.head_dim,
           "k and v must be [rows, kv_heads, head_dim] of the cache")
+    _lend(_beside(stream, dev), k, v, slots, k_cache, v_cache)
     _check((_lib or load()).pcg_cache_append(k.data_ptr(), ks, v.data_ptr(), vs, shape[0], _int_ptr(slots, shape[:1], dev),
                                              ctypes.byref(cache), _stream_of(stream, dev)))
     return k_cache, v_cache
@@ -534,15 +571,15 @@ def pcg_attention_workspace_bytes(B: int, q_heads: int, kv_heads: int, head_dim:
     return int(load().pcg_attention_workspace_bytes(B, q_heads, kv_heads, head_dim, dtype))
 
 
-def _attention_buffers(q, shape, out, workspace, B, kv_heads, dtype, dev):
+def _attention_buffers(q, shape, out, workspace, B, kv_heads, dtype, dev, beside):
     if out is None:
-        out = q.new_empty(shape)
+        out = _empty(q, shape, q.dtype, beside)
     else:
         _need(out.shape == shape and out.dtype is q.dtype and out.is_contiguous() and out.get_device() == dev,
               "out must be contiguous, of q's shape, type and device")
     if workspace is None:
         need = pcg_attention_workspace_bytes(B, shape[1], kv_heads, shape[2], dtype)
-        workspace = q.new_empty(need, dtype=torch.uint8)
+        workspace = _empty(q, need, torch.uint8, beside)
     else:
         _need(workspace.get_device() == dev and workspace.is_contiguous(), "workspace must be contiguous, on the current device")
     return out, workspace
@@ -561,7 +598,9 @@ def pcg_cache_attention(q, row_start, kv_len, block_table, k_cache, v_cache, sca
     _need(shape[2] == cache.head_dim and block_table.dim() == 2 and row_start.dim() == 1,
           "q must have the cache's head_dim, block_table be [B, max_blocks], row_start [B + 1]")
     B, max_blocks = block_table.shape
-    out, workspace = _attention_buffers(q, shape, out, workspace, B, cache.kv_heads, cache.dtype, dev)
+    beside = _beside(stream, dev)
+    out, workspace = _attention_buffers(q, shape, out, workspace, B, cache.kv_heads, cache.dtype, dev, beside)
+    _lend(beside, q, row_start, kv_len, block_table, k_cache, v_cache, out, workspace)
     _check((_lib or load()).pcg_cache_attention(
         q.data_ptr(), stride, shape[0], shape[1], _int_ptr(row_start, (B + 1,), dev), _int_ptr(kv_len, (B,), dev),
         _int_ptr(block_table, (B, max_blocks), dev), B, max_blocks, ctypes.byref(cache),
@@ -580,7 +619,9 @@ def pcg_prompt_attention(q, k, v, row_start, scale: Optional[float] = None, out=
     _need(kshape == vshape and kshape[0] == shape[0] and kshape[2] == shape[2] and row_start.dim() == 1 and row_start.shape[0] > 0,
           "k and v must be [rows, kv_heads, head_dim] with q's rows and head_dim, row_start [B + 1]")
     B, dtype = row_start.shape[0] - 1, _DTYPES.get(q.dtype) or dtype_code(q)
-    out, workspace = _attention_buffers(q, shape, out, workspace, B, kshape[1], dtype, dev)
+    beside = _beside(stream, dev)
+    out, workspace = _attention_buffers(q, shape, out, workspace, B, kshape[1], dtype, dev, beside)
+    _lend(beside, q, k, v, row_start, out, workspace)
     _check((_lib or load()).pcg_prompt_attention(
         q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dtype, shape[0], shape[1], kshape[1], shape[2],
         _int_ptr(row_start, (B + 1,), dev), B, shape[2] ** -0.5 if scale is None else scale, out.data_ptr(),
