@@ -14,8 +14,10 @@ over what is cached, and ends with the verification of the drafts, whose accept 
             o = state.attend(layer, q, k, v)
         accept_len, tokens, groups, flags = state.verify(target_logits, draft_logits, draft_tokens, handle, uniforms)
 
-Nothing here waits for the GPU: lengths stay there from round to round.  The arithmetic is the library's
-(``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cache_attention``, ``pcg_prompt_attention``, ``pcg_verify``).
+Nothing here waits for the GPU: lengths stay there from round to round.  A call runs on its ``stream``, or on the current
+one; where that is another one than the last call's, it is put behind it, so that a round may use several.  The
+arithmetic is the library's (``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cache_attention``, ``pcg_prompt_attention``,
+``pcg_verify``).
 """
 from __future__ import annotations
 
@@ -52,6 +54,22 @@ class DecodeRounds:
         self.new_len = None
         self.plan: Optional[binding.CachePlan] = None
         self._workspace = None
+        # of the last call; there is none for a state in host memory, of which the lengths can be followed without a GPU
+        self._stream = torch.cuda.current_stream(self.cached_len.device) if self.cached_len.is_cuda else None
+
+    def _behind(self, stream):
+        """The stream of a call: the given one, or the current one.  One that the last call was not on waits for it, and
+        the state's memory is not given out again before that stream, too, is done with it."""
+        if self._stream is None:
+            return None
+        dev = self.cached_len.get_device()
+        if binding._stream_of(stream, dev) != self._stream.cuda_stream:
+            last, self._stream = self._stream, binding._beside(stream, dev) or torch.cuda.current_stream(dev)
+            if not torch.cuda.is_current_stream_capturing():  # a captured call cannot wait for what is not in the graph
+                self._stream.wait_stream(last)
+            binding._lend(self._stream, self.cached_len, self.held, self.ring_state, self.accept_len, self.block_table, self.free_ring,
+                          self.k_cache, self.v_cache, self.new_len, self._workspace)
+        return self._stream
 
     def begin(self, new_len, rows: int, stream=None) -> binding.CachePlan:
         """Plans a round of ``new_len`` [B] new tokens a sequence (int32, on the device; negative: the sequence has
@@ -59,6 +77,7 @@ class DecodeRounds:
         ``plan.positions`` say which row is which token; a sequence with ``plan.flags`` set has no part in the round."""
         if self.plan is not None:
             raise RuntimeError("the last round has not ended: verify() or keep_all()")
+        stream = self._behind(stream)
         plan = binding.pcg_cache_plan(self.cached_len, new_len, self.held, self.block_table, self.free_ring, self.ring_state,
                                       self.block_size, rows, accept_len=self.accept_len, stream=stream)
         self.plan, self.new_len = plan, new_len
@@ -73,28 +92,32 @@ class DecodeRounds:
         if self.plan is None:
             raise RuntimeError("no round has begun")
         plan, kc, vc = self.plan, self.k_cache[layer], self.v_cache[layer]
+        stream = self._behind(stream)
         if self._workspace is None:
             need = binding.pcg_attention_workspace_bytes(self.B, q.shape[1], k.shape[1], q.shape[2], binding.dtype_code(q))
-            self._workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            self._workspace = binding._empty(self.cached_len, need, torch.uint8, binding._beside(stream, self.cached_len.get_device()))
         binding.pcg_cache_append(k, v, plan.slots, kc, vc, stream=stream)
         if fresh:
             return binding.pcg_prompt_attention(q, k, v, plan.row_start, scale=scale, out=out, workspace=self._workspace, stream=stream)
         return binding.pcg_cache_attention(q, plan.row_start, plan.kv_len, self.block_table, kc, vc, scale=scale, out=out,
                                            workspace=self._workspace, stream=stream)
 
-    def verify(self, target_logits, draft_logits, draft_tokens, groups, uniforms, temperature: float = 1.0, **kw):
+    def verify(self, target_logits, draft_logits, draft_tokens, groups, uniforms, temperature: float = 1.0, stream=None, **kw):
         """``pcg_verify`` of the round's drafts; of the chunk, its first token and the accepted drafts stay cached."""
         if self.plan is None:
             raise RuntimeError("no round has begun")
-        result = binding.pcg_verify(target_logits, draft_logits, draft_tokens, groups, uniforms, temperature, **kw)
-        self._end(result[0])
+        stream = self._behind(stream)
+        result = binding.pcg_verify(target_logits, draft_logits, draft_tokens, groups, uniforms, temperature, stream=stream, **kw)
+        with torch.cuda.stream(stream):
+            self._end(result[0])
         return result
 
-    def keep_all(self):
+    def keep_all(self, stream=None):
         """Ends a round without drafts (a prompt, or a chunk of one): all of its tokens stay cached."""
         if self.plan is None:
             raise RuntimeError("no round has begun")
-        self._end(self.new_len - 1)
+        with torch.cuda.stream(self._behind(stream)):
+            self._end(self.new_len - 1)
 
     def _end(self, accept_len):
         # a flagged sequence had no slots, a finished one has no tokens: nothing of the round stays

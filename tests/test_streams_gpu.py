@@ -140,3 +140,77 @@ def test_calls_on_two_given_streams_do_not_disturb_each_other(name):
         for o in outs:
             for a, b in zip(want if isinstance(want, tuple) else [want], o if isinstance(o, tuple) else [o]):
                 assert torch.equal(a, b)
+
+
+# ---- decoding rounds ---------------------------------------------------------------------------------------------------
+def test_a_round_ends_behind_the_stream_that_it_ran_on(recorder):
+    """Nothing is launched but a delay on the round's stream, which the end of the round has to wait for."""
+    from paper_2511_13732_b200.rounds import DecodeRounds
+
+    state = DecodeRounds(2, 1, 8, 16, 1, 64, 4)
+    side = torch.cuda.Stream()
+    state.begin(_ints([3, 4]), 7)
+    state.keep_all()  # loads the kernels of torch that it uses
+    new = _ints([3, 4])
+    torch.cuda.synchronize()
+    state.begin(new, 7, stream=side)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1_000_000_000)  # half a second
+    state.keep_all()
+    end = torch.cuda.Event()
+    end.record()
+    while not end.query() and not side.query():
+        pass
+    assert side.query()
+    side.synchronize()
+
+
+@pytest.mark.parametrize("plan", ["one stream", "streams in turn"])
+def test_rounds_on_given_streams_follow_rounds_on_the_current_one(plan):
+    from gpu_util import logits_to_device, make_handle
+    from paper_2511_13732_b200.rounds import DecodeRounds
+
+    B, K, V = 4, 4, 2000
+    cfg = W.scaled(W.CONFIGS["C1"], V=V, M=100, B=B, K=K)
+    bt, handle = W.make_batch(cfg), make_handle(W.make_groups(cfg))
+    target, draft = logits_to_device(bt.target_logits), logits_to_device(bt.draft_logits)
+    tokens = torch.from_numpy(bt.draft_tokens).cuda()
+    g = torch.Generator(device="cuda").manual_seed(5)
+    sides = [torch.cuda.Stream() for _ in range(2)]
+    pick = iter(range(10 ** 6))
+
+    def stream(on):
+        """A stream for the next call, which starts late."""
+        if not on:
+            return None
+        s = sides[0] if plan == "one stream" else [sides[0], None, sides[1]][next(pick) % 3]
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(4_000_000)
+        return s
+
+    states = [DecodeRounds(B, 2, 60, 16, 2, 64, 12) for _ in range(2)]
+    lens = _ints([40, 7, 1, 90])
+    rows = [torch.randn((n, 8, 64), generator=g, device="cuda").bfloat16() for n in (138, 138, 20, 20, 20, 20, 20, 20)]
+    us = [torch.rand((B, K + 1, 2), generator=g, device="cuda") for _ in range(3)]
+    drafts = _ints([K + 1] * B)
+    torch.cuda.synchronize()
+    got = []
+    for on, state in enumerate(states):
+        outs = []
+
+        def round_(new_len, n, qs):
+            p = state.begin(new_len, n, stream=stream(on))
+            return [*p] + [state.attend(i, q, q[:, :2], q[:, 2:4], stream=stream(on)) for i, q in enumerate(qs)]
+
+        outs += round_(lens, 138, rows[:2])
+        state.keep_all(stream=stream(on))
+        for r in range(3):
+            outs += round_(drafts, 20, rows[2 + 2 * r: 4 + 2 * r])
+            outs += state.verify(target, draft, tokens, handle, us[r], stream=stream(on))
+        outs += round_(drafts, 20, rows[2:4])
+        got.append(outs)
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(*got)):
+        assert torch.equal(a, b), i
+    assert got[0][-10].tolist() != [40, 7, 1, 90]  # (the cached lengths of the last round)
