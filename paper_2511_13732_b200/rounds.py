@@ -1,7 +1,8 @@
 """Decoding rounds: the paged cache of a batch of sequences, from one verification to the next.
 
 A round feeds every sequence a chunk of new tokens (its last token and K drafted ones, or a prompt), attends from them
-over what is cached, and ends with the verification of the drafts, whose accept lengths decide what stays cached::
+over what is cached, and ends with the verification of the drafts, whose accept lengths decide what stays cached (prompts
+and chunks with fewer drafts may be among them)::
 
     state = DecodeRounds(B, layers, n_blocks, block_size, kv_heads, head_dim, max_blocks)
     plan = state.begin(prompt_lens, rows)            # rows: the host's bound for the sum of the lengths
@@ -102,14 +103,27 @@ class DecodeRounds:
         return binding.pcg_cache_attention(q, plan.row_start, plan.kv_len, self.block_table, kc, vc, scale=scale, out=out,
                                            workspace=self._workspace, stream=stream)
 
-    def verify(self, target_logits, draft_logits, draft_tokens, groups, uniforms, temperature: float = 1.0, stream=None, **kw):
-        """``pcg_verify`` of the round's drafts; of the chunk, its first token and the accepted drafts stay cached."""
+    def verify(self, target_logits, draft_logits, draft_tokens, groups, uniforms, temperature: float = 1.0, whole=None, stream=None, **kw):
+        """``pcg_verify`` of the round's drafts: all ``B`` sequences, K drafted tokens each.
+
+        Of a chunk its first token and the accepted drafts stay cached; of one with fewer than K drafts, those that it
+        has.  A chunk of more than K + 1 tokens is a prompt and stays whole, and so do the chunks of the sequences that
+        ``whole`` [B] (bool, on the device) names: short prompts.  What is returned is ``pcg_verify``'s, of K drafts for
+        every sequence: a prompt's part of it means nothing, nor do accepted drafts beyond those that a chunk has."""
         if self.plan is None:
             raise RuntimeError("no round has begun")
+        if draft_tokens.dim() != 2 or draft_tokens.shape[0] != self.B:
+            raise ValueError(f"the round is verified as a batch of all {self.B} sequences: draft_tokens must be [B, K]")
+        if whole is not None and (whole.shape != (self.B,) or whole.dtype is not torch.bool or whole.device != self.cached_len.device):
+            raise ValueError("whole must be a bool tensor [B] on the state's device")
         stream = self._behind(stream)
         result = binding.pcg_verify(target_logits, draft_logits, draft_tokens, groups, uniforms, temperature, stream=stream, **kw)
+        if whole is not None and stream is not None:
+            whole.record_stream(stream)
         with torch.cuda.stream(stream):
-            self._end(result[0])
+            prompt = self.new_len > draft_tokens.shape[1] + 1
+            last = self.new_len - 1
+            self._end(torch.where(prompt if whole is None else prompt | whole, last, torch.minimum(result[0], last)))
         return result
 
     def keep_all(self, stream=None):

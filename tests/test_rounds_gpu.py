@@ -170,3 +170,52 @@ def test_a_captured_round_replays():
             assert torch.equal(keys[-4:], k[at]) and torch.equal(values[-4:], v[at])
             lim = [kv[b] - 3 + i for i in range(4)]
             cache_ref.check(out[at], cache_ref.attention(q[at], keys, values, lim, 0.125), torch.bfloat16, 64, kv[b])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_prompt_joins_a_round_of_drafts(dtype):
+    """A prompt, a short prompt, a single token and full drafts in one round, whose cache the next rounds attend over.
+    Slots that hold nothing that stays are NaN."""
+    from gpu_util import make_handle
+    from paper_2511_13732_b200.rounds import DecodeRounds
+    import cache_ref
+
+    V, B, K, qh, kvh, d = 512, 5, 4, 4, 2, 64
+    handle = make_handle(W.make_groups(W.scaled(W.CONFIGS["C1"], V=V, M=64, B=B, K=K)))
+    g = torch.Generator(device="cuda").manual_seed(9)
+    rnd = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    state = DecodeRounds(B, 1, 80, 16, kvh, d, 24, dtype=dtype)
+    state.k_cache.fill_(float("nan")), state.v_cache.fill_(float("nan"))
+    kept = [[torch.empty((0, kvh, d), dtype=dtype, device="cuda")] * 2 for _ in range(B)]
+
+    def run(lens):
+        """Checks the round against what was kept of the rounds before; its keys and values."""
+        n = sum(lens)
+        q, k, v = (rnd(n, h, d).to(dtype) for h in (qh, kvh, kvh))
+        plan = state.begin(_ints(lens), n)
+        assert plan.flags.tolist() == [0] * B and plan.cached_len.tolist() == [x[0].shape[0] for x in kept]
+        out = state.attend(0, q, k, v)
+        parts = []
+        for b, (lo, hi) in enumerate(zip(plan.row_start.tolist(), plan.row_start.tolist()[1:])):
+            kv = [torch.cat([old, new[lo:hi]]) for old, new in zip(kept[b], (k, v))]
+            parts.append(kv)
+            lim = [kept[b][0].shape[0] + i + 1 for i in range(hi - lo)]
+            if lim:
+                cache_ref.check(out[lo:hi], cache_ref.attention(q[lo:hi], *kv, lim, d ** -0.5), dtype, d, lim[-1], b)
+        return parts
+
+    def verify(lens, parts, whole, all_accepted):
+        target = rnd(B, K + 1, V)
+        draft = target[:, :K].clone() if all_accepted else rnd(B, K, V)
+        mask = torch.tensor(whole, device="cuda") if any(whole) else None
+        accept = state.verify(target, draft, torch.randint(0, V, (B, K), generator=g, device="cuda").to(torch.int32), handle,
+                              torch.rand((B, K + 1, 2), generator=g, device="cuda"), whole=mask)[0].tolist()
+        assert not all_accepted or accept == [K] * B
+        for b, n in enumerate(lens):
+            m = n if whole[b] or n > K + 1 else min(accept[b] + 1, n)
+            kept[b] = [x[: kept[b][0].shape[0] + m] for x in parts[b]]
+
+    for lens, whole, all_accepted in (([40, 3, 5, 5, 70], [True, True, False, False, False], True), ([5, 1, 130, 2, 5], [False] * 5, True),
+                                      ([5, 5, 5, 3, 0], [False, False, False, True, False], False), ([5, 5, 1, 5, 9], [False] * 5, False),
+                                      ([5] * 5, [False] * 5, True)):
+        verify(lens, run(lens), whole, all_accepted)
