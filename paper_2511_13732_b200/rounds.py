@@ -52,7 +52,6 @@ class DecodeRounds:
         self.ring_state = torch.tensor([0, n_blocks], dtype=torch.int32, device=device)
         self.cached_len, self.held = ints(B), ints(B)
         self.accept_len = ints(B, fill=-1)  # of the last round; -1: none of its tokens stays
-        self.new_len = None
         self.plan: Optional[binding.CachePlan] = None
         self._workspace = None
         # of the last call; there is none for a state in host memory, of which the lengths can be followed without a GPU
@@ -69,7 +68,7 @@ class DecodeRounds:
             if not torch.cuda.is_current_stream_capturing():  # a captured call cannot wait for what is not in the graph
                 self._stream.wait_stream(last)
             binding._lend(self._stream, self.cached_len, self.held, self.ring_state, self.accept_len, self.block_table, self.free_ring,
-                          self.k_cache, self.v_cache, self.new_len, self._workspace)
+                          self.k_cache, self.v_cache, self._workspace)
         return self._stream
 
     def begin(self, new_len, rows: int, stream=None) -> binding.CachePlan:
@@ -81,7 +80,7 @@ class DecodeRounds:
         stream = self._behind(stream)
         plan = binding.pcg_cache_plan(self.cached_len, new_len, self.held, self.block_table, self.free_ring, self.ring_state,
                                       self.block_size, rows, accept_len=self.accept_len, stream=stream)
-        self.plan, self.new_len = plan, new_len
+        self.plan = plan
         self.cached_len, self.held, self.ring_state = plan.cached_len, plan.held, plan.ring_state
         return plan
 
@@ -121,9 +120,9 @@ class DecodeRounds:
         if whole is not None and stream is not None:
             whole.record_stream(stream)
         with torch.cuda.stream(stream):
-            prompt = self.new_len > draft_tokens.shape[1] + 1
-            last = self.new_len - 1
-            self._end(torch.where(prompt if whole is None else prompt | whole, last, torch.minimum(result[0], last)))
+            n = self._fed()
+            prompt = n > draft_tokens.shape[1] + 1
+            self._end(torch.where(prompt if whole is None else prompt | whole, n - 1, result[0]))
         return result
 
     def keep_all(self, stream=None):
@@ -131,10 +130,15 @@ class DecodeRounds:
         if self.plan is None:
             raise RuntimeError("no round has begun")
         with torch.cuda.stream(self._behind(stream)):
-            self._end(self.new_len - 1)
+            self._end(self._fed() - 1)
+
+    def _fed(self):
+        """Tokens of the round [B], by the plan (the caller's lengths may be the next round's by now); of a flagged sequence,
+        which had no slots, and of a finished one 0 or less."""
+        return self.plan.kv_len - self.plan.cached_len
 
     def _end(self, accept_len):
-        # a flagged sequence had no slots, a finished one has no tokens: nothing of the round stays
-        none = (self.plan.flags != 0) | (self.new_len < 1)
-        self.accept_len = torch.where(none, -1, accept_len).to(torch.int32)
+        # no more than was fed stays, and nothing of a sequence that fed nothing
+        n = self._fed()
+        self.accept_len = torch.where(n < 1, -1, torch.minimum(accept_len, n - 1)).to(torch.int32)
         self.plan = None

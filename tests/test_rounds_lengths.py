@@ -74,3 +74,18 @@ def test_a_flagged_sequence_keeps_nothing_of_its_chunk(rounds):
     accepts.append([1, 4, 4])
     _verify(s, 3, 4, whole=torch.tensor([False, True, True]))
     assert s.begin(_ints([0] * 3), 100).cached_len.tolist() == [40, 0, 0]
+
+
+@pytest.mark.parametrize("verified", [True, False])
+def test_a_buffer_of_chunk_lengths_may_be_refilled_at_once(rounds, verified):
+    make, accepts = rounds
+    s = make(3)
+    new = _ints([20, 5, 0])
+    s.begin(new, 30)
+    new.copy_(_ints([-1, 1, 5]))  # the next round's
+    if verified:
+        accepts.append([0, 3, 2])
+        _verify(s, 3, 4)
+    else:
+        s.keep_all()
+    assert s.begin(_ints([1] * 3), 30).cached_len.tolist() == [20, 4 if verified else 5, 0]
