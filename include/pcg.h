@@ -390,7 +390,8 @@ typedef struct {
  *   block_table  [B, max_blocks], in and out: only the entries named above are written
  *   free_ring    [ring_size], in and out: block ids; the free ones are the ring_state[1] entries from ring_state[0]
  *                on, cyclically.  Released blocks are written behind them (they are not handed out by the same call).
- *                ring_size >= n_blocks, so that the ring holds every block; entries beyond that are dropped.
+ *                ring_size >= n_blocks, so that the ring holds every block; what it has no room for (behind the entries that
+ *                are free when the call is made) is dropped and not counted.
  *   rows         capacity of the packed rows (the host's bound for the sum of the new lengths)
  *   out_cached_len = c, out_kv_len = c + n, out_held  [B];  out_row_start [B + 1], entries at most `rows`
  *   out_slots    [rows], out_positions [rows] or NULL; rows behind the last sequence are -1

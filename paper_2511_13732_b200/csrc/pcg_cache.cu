@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const __grid_c
     plan_scan(granted, scratch, &taken);  // its barriers also publish the shared arrays
     if (blockIdx.x == 0 && tid == 0) {
         a.out_ring_state[0] = (int32_t)((head + taken) % N);
-        a.out_ring_state[1] = (int32_t)min(count - taken + total_freed, (int64_t)N);
+        a.out_ring_state[1] = (int32_t)(count - taken + min(total_freed, (int64_t)(N - count)));  // what was dropped is not free
         a.out_row_start[B] = row_start[B];
     }
     const int gtid = blockIdx.x * kPlanThreads + tid, gthreads = gridDim.x * kPlanThreads;

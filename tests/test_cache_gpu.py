@@ -110,6 +110,37 @@ def test_released_blocks_never_overrun_the_ring():
     _compare(st, 4)
 
 
+@pytest.mark.parametrize("B,room,seed", [(2, 2, 0), (20, 0, 1), (20, 7, 2), (300, 40, 3)])
+def test_what_a_full_ring_drops_is_not_counted_as_free(B, room, seed):
+    """The call releases more than the ring has room for, and takes blocks as well: no block is then both held and free."""
+    from paper_2511_13732_b200 import binding
+
+    rng = random.Random(seed)
+    bs, max_blocks = 16, 8
+    held = [rng.randint(1, 5) for _ in range(B)]
+    new = [-1 if b % 2 == 0 else rng.randint(0, 16) for b in range(B)]
+    cached = [bs * h for h in held]  # full: a new token needs a block
+    ids = list(range(sum(held) + B + room))
+    rng.shuffle(ids)
+    table = [[ids.pop() for _ in range(h)] + [-1] * (max_blocks - h) for h in held]
+    free = [ids.pop() for _ in range(B)]  # enough for every sequence
+    N, head = len(free) + room, rng.randrange(len(free) + room)
+    ring = [-7] * N
+    for i, x in enumerate(free):
+        ring[(head + i) % N] = x
+    taken = sum(1 for n in new if n > 0)
+    released = [x for b in range(B) if new[b] < 0 for x in table[b][: held[b]]]
+    assert taken > 0 and len(released) > room
+    d_table, d_ring = _ints(table), _ints(ring)
+    p = binding.pcg_cache_plan(_ints(cached), _ints(new), _ints(held), d_table, d_ring, _ints([head, len(free)]), bs, 16 * B)
+    at, count = p.ring_state.tolist()
+    assert p.flags.tolist() == [0] * B and count == len(free) - taken + room
+    now = [d_ring.tolist()[(at + i) % N] for i in range(count)]
+    assert now == free[taken:] + released[:room]
+    owned = [x for row, h in zip(d_table.tolist(), p.held.tolist()) for x in row[:h]]
+    assert not set(owned) & set(now)
+
+
 def test_a_plan_feeds_the_next_one():
     """Forty rounds by swapping two sets of tensors: no block is ever in two hands, none is lost."""
     from paper_2511_13732_b200 import binding
