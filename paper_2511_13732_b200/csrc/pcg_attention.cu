@@ -128,9 +128,9 @@ __global__ void __launch_bounds__(kSimpleThreads) attention_simple_kernel(const 
     __syncthreads();
     float top = kNegInf, total = 0.f;
     for (int w = 0; w < NW; ++w) top = fmaxf(top, part[w][32 * DPL]);
-    // a warp that has met no score above -inf has m = -inf and counts for nothing
-    for (int w = 0; w < NW; ++w)
-        if (part[w][32 * DPL] != kNegInf) total += part[w][32 * DPL + 1] * exp2f(part[w][32 * DPL] - top);
+    // a warp that has met no score above -inf has m = -inf and counts for nothing, unless one of its scores is NaN: its sum
+    // of weights then is (0 otherwise), and so is the row
+    for (int w = 0; w < NW; ++w) total += part[w][32 * DPL + 1] * (part[w][32 * DPL] != kNegInf ? exp2f(part[w][32 * DPL] - top) : 0.f);
     T *out = (T *)a.out + ((int64_t)r * a.q_heads + h) * d;
     for (int i = tid; i < d; i += kSimpleThreads) {
         float o = 0.f;

@@ -175,6 +175,19 @@ def test_infinite_and_undefined_scores(d, dtype):
     cache_ref.check(got[:1, :1], (o, a, m), dtype, d, 201)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [80, 24, 256, 64, 128])
+@pytest.mark.parametrize("lo,hi", [(0, 32), (32, 64), (200, 201), (192, 201), (0, 201)])
+def test_undefined_scores_next_to_each_other(dtype, d, lo, hi):
+    """A row that sees a score that is NaN is NaN, however many of its neighbours are; the other head is untouched."""
+    s = Paged([(200, 1), (200, 1)], 2, 2, d, 64, dtype, seed=13)
+    want = s.run()
+    for p in range(lo, hi):
+        s.kc[s.table[0, p // 64], 0, p % 64, d - 1] = float("nan")
+    got = s.run()
+    assert bool(torch.isnan(got[0, 0]).all()) and torch.equal(got[0, 1], want[0, 1]) and torch.equal(got[1], want[1])
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("B,n", [(1, 1), (3, 5), (70, 17), (2, 200), (300, 1)])
 def test_results_do_not_depend_on_the_run(dtype, B, n):
