@@ -1,4 +1,6 @@
 """Helpers shared by the GPU parity tests: moving seeded inputs to the device and calling the C-ABI binding."""
+import ctypes
+
 import numpy as np
 import torch
 
@@ -39,3 +41,20 @@ def library_candidate_order(V: int, logits: np.ndarray) -> np.ndarray:
     W = 16 // logits.dtype.itemsize
     t = np.arange(V)
     return np.lexsort((t, (t // W) % 128)).astype(np.int32)
+
+
+class Recorder:
+    """Stands for the library: notes the arguments of the calls that launch kernels, and launches none."""
+
+    def __init__(self, lib):
+        self.lib, self.calls = lib, []
+
+    def __getattr__(self, name):
+        if name.endswith("_bytes") or not name.startswith(("pcg_verify", "pcg_group_probs", "pcg_cache", "pcg_prompt")):
+            return getattr(self.lib, name)
+
+        def call(*args):
+            self.calls.append([a.value if isinstance(a, ctypes.c_void_p) else a for a in args])
+            return 0
+
+        return call

@@ -1,6 +1,4 @@
 """Calls on a given stream that is not the current one: whose memory they use, and until when."""
-import ctypes
-
 import pytest
 
 from paper_2511_13732_b200 import workloads as W
@@ -13,25 +11,9 @@ def _ints(x):
     return torch.tensor(x, dtype=torch.int32, device="cuda")
 
 
-class Recorder:
-    """Stands for the library: notes the arguments of the calls that launch kernels, and launches none."""
-
-    def __init__(self, lib):
-        self.lib, self.calls = lib, []
-
-    def __getattr__(self, name):
-        if name.endswith("_bytes") or not name.startswith(("pcg_verify", "pcg_group_probs", "pcg_cache", "pcg_prompt")):
-            return getattr(self.lib, name)
-
-        def call(*args):
-            self.calls.append([a.value if isinstance(a, ctypes.c_void_p) else a for a in args])
-            return 0
-
-        return call
-
-
 @pytest.fixture
 def recorder(monkeypatch):
+    from gpu_util import Recorder
     from paper_2511_13732_b200 import binding
 
     r = Recorder(binding.load())
