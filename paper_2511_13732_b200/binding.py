@@ -15,11 +15,6 @@ from typing import NamedTuple, Optional
 
 import numpy as np
 
-try:
-    import torch
-except ImportError:  # the entry points that take numpy arrays do without it
-    torch = None
-
 from . import build as _build
 
 PCG_F32, PCG_BF16, PCG_F16 = 0, 1, 2
@@ -477,8 +472,21 @@ def _need(ok: bool, text: str):
         raise ValueError(text)
 
 
+torch = None  # imported by the first of these calls: the entry points that take numpy arrays do without it
+_DTYPES = {}
+
+
+def _import_torch():
+    global torch
+    import torch
+
+    _DTYPES.update({torch.bfloat16: PCG_BF16, torch.float16: PCG_F16})
+
+
 def _device(t) -> int:
     """The device of a call: its first tensor's, which has to be the current one (the library launches there)."""
+    if torch is None:
+        _import_torch()
     if not t.is_cuda or t.get_device() != torch.cuda.current_device():
         raise ValueError(f"expected CUDA tensors of the current device, got one on {t.device}")
     return t.get_device()
@@ -493,6 +501,8 @@ def _int_ptr(t, shape, dev: int) -> int:
 
 
 def _stream_of(stream, dev: int) -> int:
+    import torch
+
     return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
@@ -505,9 +515,6 @@ def _packed(t, name: str, dtype, dev: int):
     if (s[2] != 1 and d != 1) or (s[1] != d and h != 1):
         raise ValueError(f"{name}: a token's heads must be dense")
     return shape, s[0] if n > 1 else h * d
-
-
-_DTYPES = {} if torch is None else {torch.bfloat16: PCG_BF16, torch.float16: PCG_F16}
 
 
 def _cache_struct(k_cache, v_cache, dev: int) -> _Cache:
