@@ -92,6 +92,9 @@ class DecodeRounds:
         if self.plan is None:
             raise RuntimeError("no round has begun")
         plan, kc, vc = self.plan, self.k_cache[layer], self.v_cache[layer]
+        rows = plan.slots.shape[0]
+        if q.shape[0] != rows or k.shape[0] != rows:  # fewer would cut sequences short, whose rows then see fewer keys
+            raise ValueError(f"the round has {rows} rows; q has {q.shape[0]}, k {k.shape[0]}")
         stream = self._behind(stream)
         if self._workspace is None:
             need = binding.pcg_attention_workspace_bytes(self.B, q.shape[1], k.shape[1], q.shape[2], binding.dtype_code(q))

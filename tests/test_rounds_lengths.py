@@ -89,3 +89,13 @@ def test_a_buffer_of_chunk_lengths_may_be_refilled_at_once(rounds, verified):
     else:
         s.keep_all()
     assert s.begin(_ints([1] * 3), 30).cached_len.tolist() == [20, 4 if verified else 5, 0]
+
+
+def test_attention_of_other_rows_than_the_round_has_is_refused(rounds):
+    make, _ = rounds
+    s = make(2)
+    s.begin(_ints([3, 4]), 9)
+    rows = lambda n, heads: torch.zeros(n, heads, 8, dtype=torch.bfloat16)  # noqa: E731
+    for q, k in ((7, 9), (9, 7), (10, 9), (0, 0)):
+        with pytest.raises(ValueError, match="9 rows"):
+            s.attend(0, rows(q, 2), rows(k, 1), rows(k, 1))
