@@ -177,10 +177,10 @@ def _beside(stream, dev: int):
 
 def _empty(like, shape, dtype, beside):
     """A new tensor on the device of `like`, for a call on the current stream or on the one `beside` it."""
-    import torch
-
     if beside is None:
         return like.new_empty(shape, dtype=dtype)
+    import torch
+
     with torch.cuda.stream(beside):
         t = like.new_empty(shape, dtype=dtype)
     t.record_stream(torch.cuda.current_stream(like.device))  # a caller who waits for the call may read it there
@@ -500,10 +500,11 @@ def _int_ptr(t, shape, dev: int) -> int:
     return t.data_ptr()
 
 
-def _stream_of(stream, dev: int) -> int:
-    import torch
-
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+def _place(stream, dev: int):
+    """The address of a call's stream, and the stream itself where it is not the current one."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev), None
+    return stream.cuda_stream, _beside(stream, dev)
 
 
 def _packed(t, name: str, dtype, dev: int):
@@ -543,7 +544,7 @@ def pcg_cache_plan(cached_len, new_len, held, block_table, free_ring, ring_state
             _int_ptr(block_table, (B, max_blocks), dev), _int_ptr(free_ring, (ring_size,), dev), ring_size,
             _int_ptr(ring_state, (2,), dev), rows)
     sizes = (B, B, B, B + 1, rows, rows, 2, B)
-    beside = _beside(stream, dev)
+    at, beside = _place(stream, dev)
     if out is None:
         buf = _empty(cached_len, 5 * B + 2 * rows + 3, torch.int32, beside)
         p = buf.data_ptr()
@@ -554,8 +555,9 @@ def pcg_cache_plan(cached_len, new_len, held, block_table, free_ring, ring_state
         out = CachePlan(*torch.split_with_sizes(buf, sizes))
     else:
         ptrs = [None if t is None else _int_ptr(t, (n,), dev) for t, n in zip(out, sizes)]
-    _lend(beside, cached_len, new_len, held, block_table, free_ring, ring_state, accept_len, *out)
-    _check((_lib or load()).pcg_cache_plan(*args, *ptrs, _stream_of(stream, dev)))
+    if beside is not None:
+        _lend(beside, cached_len, new_len, held, block_table, free_ring, ring_state, accept_len, *out)
+    _check((_lib or load()).pcg_cache_plan(*args, *ptrs, at))
     return out
 
 
@@ -567,9 +569,11 @@ def pcg_cache_append(k, v, slots, k_cache, v_cache, stream=None):
     vshape, vs = _packed(v, "v", k_cache.dtype, dev)
     _need(shape == vshape and shape[1] == cache.kv_heads and shape[2] == cache.head_dim,
           "k and v must be [rows, kv_heads, head_dim] of the cache")
-    _lend(_beside(stream, dev), k, v, slots, k_cache, v_cache)
+    at, beside = _place(stream, dev)
+    if beside is not None:
+        _lend(beside, k, v, slots, k_cache, v_cache)
     _check((_lib or load()).pcg_cache_append(k.data_ptr(), ks, v.data_ptr(), vs, shape[0], _int_ptr(slots, shape[:1], dev),
-                                             ctypes.byref(cache), _stream_of(stream, dev)))
+                                             ctypes.byref(cache), at))
     return k_cache, v_cache
 
 
@@ -605,14 +609,15 @@ def pcg_cache_attention(q, row_start, kv_len, block_table, k_cache, v_cache, sca
     _need(shape[2] == cache.head_dim and block_table.dim() == 2 and row_start.dim() == 1,
           "q must have the cache's head_dim, block_table be [B, max_blocks], row_start [B + 1]")
     B, max_blocks = block_table.shape
-    beside = _beside(stream, dev)
+    at, beside = _place(stream, dev)
     out, workspace = _attention_buffers(q, shape, out, workspace, B, cache.kv_heads, cache.dtype, dev, beside)
-    _lend(beside, q, row_start, kv_len, block_table, k_cache, v_cache, out, workspace)
+    if beside is not None:
+        _lend(beside, q, row_start, kv_len, block_table, k_cache, v_cache, out, workspace)
     _check((_lib or load()).pcg_cache_attention(
         q.data_ptr(), stride, shape[0], shape[1], _int_ptr(row_start, (B + 1,), dev), _int_ptr(kv_len, (B,), dev),
         _int_ptr(block_table, (B, max_blocks), dev), B, max_blocks, ctypes.byref(cache),
         shape[2] ** -0.5 if scale is None else scale, out.data_ptr(), workspace.data_ptr(),
-        workspace.numel() * workspace.element_size(), _stream_of(stream, dev)))
+        workspace.numel() * workspace.element_size(), at))
     return out
 
 
@@ -626,11 +631,12 @@ def pcg_prompt_attention(q, k, v, row_start, scale: Optional[float] = None, out=
     _need(kshape == vshape and kshape[0] == shape[0] and kshape[2] == shape[2] and row_start.dim() == 1 and row_start.shape[0] > 0,
           "k and v must be [rows, kv_heads, head_dim] with q's rows and head_dim, row_start [B + 1]")
     B, dtype = row_start.shape[0] - 1, _DTYPES.get(q.dtype) or dtype_code(q)
-    beside = _beside(stream, dev)
+    at, beside = _place(stream, dev)
     out, workspace = _attention_buffers(q, shape, out, workspace, B, kshape[1], dtype, dev, beside)
-    _lend(beside, q, k, v, row_start, out, workspace)
+    if beside is not None:
+        _lend(beside, q, k, v, row_start, out, workspace)
     _check((_lib or load()).pcg_prompt_attention(
         q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dtype, shape[0], shape[1], kshape[1], shape[2],
         _int_ptr(row_start, (B + 1,), dev), B, shape[2] ** -0.5 if scale is None else scale, out.data_ptr(),
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_of(stream, dev)))
+        workspace.data_ptr(), workspace.numel() * workspace.element_size(), at))
     return out

@@ -22,6 +22,7 @@ arithmetic is the library's (``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cac
 """
 from __future__ import annotations
 
+from contextlib import nullcontext
 from typing import Optional
 
 import torch
@@ -55,21 +56,28 @@ class DecodeRounds:
         self.plan: Optional[binding.CachePlan] = None
         self._workspace = None
         # of the last call; there is none for a state in host memory, of which the lengths can be followed without a GPU
-        self._stream = torch.cuda.current_stream(self.cached_len.device) if self.cached_len.is_cuda else None
+        self._device = self.cached_len.get_device()
+        self._stream = torch.cuda.current_stream(self._device) if self.cached_len.is_cuda else None
+        self._at = None if self._stream is None else self._stream.cuda_stream
 
     def _behind(self, stream):
-        """The stream of a call: the given one, or the current one.  One that the last call was not on waits for it, and
-        the state's memory is not given out again before that stream, too, is done with it."""
+        """The given stream of a call, or None where that is the current one.  A stream that the last call was not on waits
+        for it, and the state's memory is not given out again before that stream, too, is done with it."""
         if self._stream is None:
             return None
-        dev = self.cached_len.get_device()
-        if binding._stream_of(stream, dev) != self._stream.cuda_stream:
-            last, self._stream = self._stream, binding._beside(stream, dev) or torch.cuda.current_stream(dev)
+        dev = self._device
+        at = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+        stream = None if stream is None else binding._beside(stream, dev)
+        if at != self._at:
+            last, self._stream, self._at = self._stream, stream or torch.cuda.current_stream(dev), at
             if not torch.cuda.is_current_stream_capturing():  # a captured call cannot wait for what is not in the graph
                 self._stream.wait_stream(last)
             binding._lend(self._stream, self.cached_len, self.held, self.ring_state, self.accept_len, self.block_table, self.free_ring,
                           self.k_cache, self.v_cache, self._workspace)
-        return self._stream
+        return stream
+
+    def _on(self, stream):
+        return nullcontext() if stream is None else torch.cuda.stream(stream)
 
     def begin(self, new_len, rows: int, stream=None) -> binding.CachePlan:
         """Plans a round of ``new_len`` [B] new tokens a sequence (int32, on the device; negative: the sequence has
@@ -98,7 +106,7 @@ class DecodeRounds:
         stream = self._behind(stream)
         if self._workspace is None:
             need = binding.pcg_attention_workspace_bytes(self.B, q.shape[1], k.shape[1], q.shape[2], binding.dtype_code(q))
-            self._workspace = binding._empty(self.cached_len, need, torch.uint8, binding._beside(stream, self.cached_len.get_device()))
+            self._workspace = binding._empty(self.cached_len, need, torch.uint8, stream)
         binding.pcg_cache_append(k, v, plan.slots, kc, vc, stream=stream)
         if fresh:
             return binding.pcg_prompt_attention(q, k, v, plan.row_start, scale=scale, out=out, workspace=self._workspace, stream=stream)
@@ -122,26 +130,26 @@ class DecodeRounds:
         result = binding.pcg_verify(target_logits, draft_logits, draft_tokens, groups, uniforms, temperature, stream=stream, **kw)
         if whole is not None and stream is not None:
             whole.record_stream(stream)
-        with torch.cuda.stream(stream):
-            n = self._fed()
-            prompt = n > draft_tokens.shape[1] + 1
-            self._end(torch.where(prompt if whole is None else prompt | whole, n - 1, result[0]))
+        with self._on(stream):
+            last = self._last()
+            prompt = last > draft_tokens.shape[1]
+            self._end(torch.where(prompt if whole is None else prompt | whole, last, result[0]), last)
         return result
 
     def keep_all(self, stream=None):
         """Ends a round without drafts (a prompt, or a chunk of one): all of its tokens stay cached."""
         if self.plan is None:
             raise RuntimeError("no round has begun")
-        with torch.cuda.stream(self._behind(stream)):
-            self._end(self._fed() - 1)
+        with self._on(self._behind(stream)):
+            last = self._last()
+            self._end(last, last)
 
-    def _fed(self):
-        """Tokens of the round [B], by the plan (the caller's lengths may be the next round's by now); of a flagged sequence,
-        which had no slots, and of a finished one 0 or less."""
-        return self.plan.kv_len - self.plan.cached_len
+    def _last(self):
+        """Number of the last token that each sequence fed, by the plan (the caller's lengths may be the next round's by
+        now); below 0 where it fed none, as a flagged or finished one."""
+        return self.plan.kv_len - self.plan.cached_len - 1
 
-    def _end(self, accept_len):
-        # no more than was fed stays, and nothing of a sequence that fed nothing
-        n = self._fed()
-        self.accept_len = torch.where(n < 1, -1, torch.minimum(accept_len, n - 1)).to(torch.int32)
+    def _end(self, accept_len, last=None):
+        # no more than was fed stays
+        self.accept_len = torch.minimum(accept_len, self._last() if last is None else last).clamp(min=-1)
         self.plan = None
