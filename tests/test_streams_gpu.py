@@ -196,3 +196,43 @@ def test_rounds_on_given_streams_follow_rounds_on_the_current_one(plan):
     for i, (a, b) in enumerate(zip(*got)):
         assert torch.equal(a, b), i
     assert got[0][-10].tolist() != [40, 7, 1, 90]  # (the cached lengths of the last round)
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_the_attention_of_a_round_is_captured_and_replayed(given):
+    """The layers of a round in a graph (on the capturing stream, or on one forked from it), between eager begins and ends."""
+    from paper_2511_13732_b200.rounds import DecodeRounds
+
+    g = torch.Generator(device="cuda").manual_seed(8)
+    lens = [_ints([40, 7, 30]), _ints([5, 5, 5])]
+    q = [torch.randn((n, 8, 64), generator=g, device="cuda").bfloat16() for n in (77, 15)]
+    side = torch.cuda.Stream()
+    got = []
+    for captured in (False, True):
+        state, outs = DecodeRounds(3, 2, 30, 16, 2, 64, 8), []
+        for i in range(2):
+            state.begin(lens[i], q[i].shape[0])
+            out = [torch.empty_like(q[i]) for _ in range(2)]
+
+            def layers(stream=None):
+                for layer in range(2):
+                    state.attend(layer, q[i], q[i][:, :2], q[i][:, 2:4], out=out[layer], stream=stream)
+
+            if captured:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    if given:
+                        side.wait_stream(torch.cuda.current_stream())
+                    layers(side if given else None)
+                    if given:
+                        torch.cuda.current_stream().wait_stream(side)
+                graph.replay()
+            else:
+                layers()
+            outs += [o.clone() for o in out]
+            state.keep_all()
+        outs += [*state.begin(lens[1], 15)]
+        got.append(outs)
+    torch.cuda.synchronize()
+    for i, (a, b) in enumerate(zip(*got)):
+        assert torch.equal(a, b), i
