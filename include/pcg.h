@@ -441,7 +441,8 @@ size_t pcg_attention_workspace_bytes(int32_t B, int32_t q_heads, int32_t kv_head
  * A used entry outside 0 .. n_blocks - 1 stands for a block of zeros.  Scores, the softmax and the sums are kept in 32
  * bits; of the 16-bit types, head dimensions 64 and 128 run on the tensor cores, where the weights are rounded to the
  * type before they meet the values.  Values of tokens that a sequence does attend to have to be finite there: a row
- * also comes out NaN where a value of a LATER token of its own chunk is infinite or NaN.
+ * also comes out NaN where a value of a LATER token of its own chunk is infinite or NaN.  A row that sees a score of +inf or
+ * NaN, or scores of -inf alone, is NaN, as its softmax is.
  * Results are bit-identical from run to run.
  * Errors: INVALID_ARG, UNSUPPORTED (q_heads / kv_heads > 128, B > 16384), WORKSPACE, CUDA.
  */

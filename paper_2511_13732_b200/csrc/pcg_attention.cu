@@ -29,7 +29,11 @@ struct Narrow<f16_t> {
 // ---------------------------------------------------------------------------------------------- any type and head size
 // One block per (row, query head): its eight warps take keys 32 at a time in turn, a lane scores one key (16-byte loads,
 // the query in shared memory), and the warp sums the 32 weighted values with lane = head dimension.  The warps'
-// running sums meet in shared memory at the end.  Serves the head dimensions that the other kernels are not built for.  Blocks of one sequence and head group re-read its keys out of L2.
+// running sums meet in shared memory at the end.  Serves the head dimensions that the other kernels are not built for.
+// What bounds it: every key is read again, out of L2, for each row and each query head of its group, and products run on the
+// FMA pipes: 2.3 to 4.9 TFLOP/s.  64 tokens over 2000 cached, 32 / 8 heads, bf16: 560 us at 80 dimensions, 1072 at 256 (118 at
+// 128, on the tensor cores); a prompt of 2048: 6.4 ms, 15.0 ms (0.083 ms).  float16 above 64 dimensions spills 12 to 24 bytes
+// a thread.
 constexpr int kSimpleThreads = 256;
 
 template <typename T, int DPL>  // DPL: values per lane, 32 * DPL >= d

@@ -44,8 +44,9 @@ __device__ __forceinline__ int tiles_of(int n, int len, int TQ, int p) {
 }
 
 // Sum over 0 <= i < n of floor((a i + b) / 128), a, b >= 0.  a a power of two, as it is where the query heads a key head
-// are: floor((i + floor(b / a)) / (128 / a)), in closed form.  Else Euclid's steps on a and the divisor, the first of
-// them by shifts; what is left fits 32 bits.
+// are: floor((i + floor(b / a)) / (128 / a)), in closed form.  Else the sum of floors of a line by the Euclidean algorithm
+// (points below the line are points beside it with the axes exchanged, and a and the divisor shrink as in a greatest common
+// divisor), its first step by shifts; what is left fits 32 bits.
 __device__ __forceinline__ int64_t floor_sum_128(uint32_t n, uint32_t a, int64_t b) {
     const int64_t nn = n;
     if ((a & (a - 1)) == 0) {

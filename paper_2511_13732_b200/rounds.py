@@ -16,9 +16,9 @@ and chunks with fewer drafts may be among them)::
         accept_len, tokens, groups, flags = state.verify(target_logits, draft_logits, draft_tokens, handle, uniforms)
 
 Nothing here waits for the GPU: lengths stay there from round to round.  A call runs on its ``stream``, or on the current
-one; where that is another one than the last call's, it is put behind it, so that a round may use several.  The
-arithmetic is the library's (``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cache_attention``, ``pcg_prompt_attention``,
-``pcg_verify``).
+one; where that is another one than the last call's, it is put behind it, so that a round may use several (what a graph
+replays is the caller's to order).  What a call reads has to be complete on its stream.  The arithmetic is the library's
+(``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cache_attention``, ``pcg_prompt_attention``, ``pcg_verify``).
 """
 from __future__ import annotations
 
