@@ -461,6 +461,92 @@ pcg_status pcg_prompt_attention(const void *q, int64_t q_stride, const void *k, 
                                 int32_t head_dim, const int32_t *row_start, int32_t B, float scale, void *out,
                                 void *workspace, size_t workspace_bytes, pcg_stream stream);
 
+/*
+ * Positions.  A model with rotary positions turns queries and keys by the angles of their tokens' positions before the
+ * products.  Of the first `dim` dimensions x of a head, in pairs (x1, x2), with cos and sin of the pair's angle:
+ *     y1 = x1 cos - x2 sin,   y2 = x2 cos + x1 sin
+ * each product and each sum rounded to float32, the result once to the type.  Pair i < dim / 2 is (i, i + dim / 2), or
+ * (2 i, 2 i + 1) where interleaved.  The other dimensions stay as they are.
+ */
+typedef struct {
+    int32_t dim;         /* dimensions that are turned: a multiple of 16, 16 .. head_dim */
+    int32_t interleaved; /* 0 or 1 */
+    int32_t positions;   /* rows of the table, at least 1 */
+    const float *table;  /* [positions, dim], 16-byte aligned: the cosines of the dim / 2 pairs, then their sines */
+} pcg_rotary;
+
+/*
+ * pcg_cache_append of keys that are turned on the way, with the queries of the same rows.
+ *   q         [rows, q_heads, head_dim] of the cache's type, token r at q + r * q_stride elements (alignment and strides as
+ *             for k); NULL with q_heads = 0: keys and values alone
+ *   positions [rows], what pcg_cache_plan writes.  A row with a negative position has no part in the call.  One with a
+ *             position that the table does not have comes out NaN where it is turned.
+ *   q_out     [rows, q_heads, head_dim], token r at q_out + r * q_out_stride elements (alignment and stride as q's): the
+ *             turned queries; may be q itself, with q's stride
+ *   k_out     the same of the keys, for an attention that reads the rows' own (pcg_prompt_attention); may be k itself, with
+ *             k's stride; NULL: not wanted
+ * Rows whose slot is outside the cache get their q_out and k_out all the same.  One launch; no workspace.
+ * Errors: INVALID_ARG, CUDA.
+ */
+pcg_status pcg_cache_append_rotary(const void *q, int64_t q_stride, int32_t q_heads, const void *k, int64_t k_stride,
+                                   const void *v, int64_t v_stride, int32_t rows, const int32_t *slots,
+                                   const int32_t *positions, const pcg_rotary *rotary, const pcg_cache *cache, void *q_out,
+                                   int64_t q_out_stride, void *k_out, int64_t k_out_stride, pcg_stream stream);
+
+/*
+ * A cache that holds 4.5 bits a value, for contexts whose reading bounds a round: 3.6 times less than 16-bit types.
+ *
+ * Of each 16 dimensions x of a token's key (or value), with g = k_scale (or v_scale) of the whole cache:
+ *     s = e4m3(max |x| / (6 g)),   c = e2m1(x / (s g)),   and c s g is what is held
+ * in float32, both roundings to nearest, ties to even, ending at the largest value (448 and 6).  e2m1 has the magnitudes 0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6.  Where s is 0 all 16 are held as 0; an infinite value is held as 2688 g with its sign; a group
+ * that has a NaN is NaN.  c s has six significant bits: with a scale of 1 what is held is exact in every type.
+ *
+ * Blocks and slots are those of pcg_cache.  A block is block_size / 16 pages of 16 tokens; a page of one head is 18 head_dim
+ * bytes, keys and values together, laid out for the tensor cores' operands (a key a lane, a value dimension a lane):
+ *     key codes    [head_dim / 32][16 tokens][16 bytes]   byte j: dimension 2 j, in the upper half 2 j + 1, of the 32
+ *     key scales   [16 tokens][head_dim / 16]
+ *     value codes  [head_dim][8 bytes]                    byte j: token 2 j, in the upper half 2 j + 1
+ *     value scales [head_dim / 16][16 tokens]
+ * A code's bit 3 is its sign, bits 0 to 2 number the magnitude.
+ */
+typedef struct {
+    int32_t n_blocks;   /* n_blocks * block_size < 2^31 */
+    int32_t block_size; /* 16, 32, 64, 128 or 256 */
+    int32_t kv_heads;   /* 1 .. 1024 */
+    int32_t head_dim;   /* a multiple of 32, 32 .. 256 */
+    float k_scale, v_scale; /* 2^-60 .. 2^60 */
+    void *data;         /* 16-byte aligned, [n_blocks, kv_heads, block_size / 16, 18 * head_dim] bytes */
+} pcg_fourbit_cache;
+
+/*
+ * pcg_cache_append_rotary into such a cache; what is quantised is the turned key in float32.
+ *   dtype     of q, k, v and the outputs
+ *   rotary    NULL: nothing is turned and positions is not read (q and q_out are then NULL, q_heads 0).  Its dim is a
+ *             multiple of 32 here.
+ *   k_out, v_out  [rows, kv_heads, head_dim], dense, 16-byte aligned: what the cache holds of the rows, rounded to the type
+ *             (for an attention over the rows' own keys and values that sees what later rounds will); NULL: not wanted.
+ *             May not overlap the inputs.
+ * Tokens of one page that are written by rows that do not follow one another are right too; two rows with one slot leave
+ * that slot with a mixture of both.  One launch; no workspace.
+ * Errors: INVALID_ARG, UNSUPPORTED (rows / 16 * kv_heads + rows over 2^31), CUDA.
+ */
+pcg_status pcg_cache_append_fourbit(const void *q, int64_t q_stride, int32_t q_heads, const void *k, int64_t k_stride,
+                                    const void *v, int64_t v_stride, pcg_dtype dtype, int32_t rows, const int32_t *slots,
+                                    const int32_t *positions, const pcg_rotary *rotary, const pcg_fourbit_cache *cache,
+                                    void *q_out, int64_t q_out_stride, void *k_out, void *v_out, pcg_stream stream);
+
+/*
+ * pcg_cache_attention over such a cache: the same arguments and rules, with q and out of `dtype`, over the values that the
+ * cache holds.  Scores, the softmax and the sums are kept in 32 bits; of the 16-bit types, head dimensions 64 and 128 with at
+ * most 48 query heads a key head run on the tensor cores, where keys and values are held exactly, queries with 11 significant
+ * bits at least, and the weights are rounded to 11 before they meet the values.
+ */
+pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_stride, pcg_dtype dtype, int32_t rows, int32_t q_heads,
+                                       const int32_t *row_start, const int32_t *kv_len, const int32_t *block_table, int32_t B,
+                                       int32_t max_blocks, const pcg_fourbit_cache *cache, float scale, void *out,
+                                       void *workspace, size_t workspace_bytes, pcg_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,6 +30,7 @@ EXPORTS = [
     "pcg_group_probs", "pcg_group_probs_workspace_bytes", "pcg_group_probs_ws", "pcg_verify_workspace_bytes", "pcg_verify", "pcg_verify_host_arena_bytes", "pcg_verify_host",
     "pcg_verify_static", "pcg_verify_thinning_workspace_bytes", "pcg_verify_thinning", "pcg_asg_create", "pcg_asg_info", "pcg_asg_csr", "pcg_asg_destroy",
     "pcg_cache_plan", "pcg_cache_append", "pcg_attention_workspace_bytes", "pcg_cache_attention", "pcg_prompt_attention",
+    "pcg_cache_append_rotary", "pcg_cache_append_fourbit", "pcg_cache_attention_fourbit",
 ]
 
 
@@ -60,6 +61,15 @@ class AsgInfo(ctypes.Structure):
 class _Cache(ctypes.Structure):
     _fields_ = [("n_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("positions", ctypes.c_int32), ("table", ctypes.c_void_p)]
+
+
+class _FourbitCache(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("k_scale", ctypes.c_float), ("v_scale", ctypes.c_float), ("data", ctypes.c_void_p)]
 
 
 class CachePlan(NamedTuple):
@@ -138,6 +148,13 @@ def load(build_if_missing: bool = True):
     lib.pcg_cache_attention.restype = ctypes.c_int
     lib.pcg_prompt_attention.argtypes = [vp, i64, vp, i64, vp, i64, ctypes.c_int, i32, i32, i32, i32, vp, i32, f32, vp, vp, sz, vp]
     lib.pcg_prompt_attention.restype = ctypes.c_int
+    rotary, fourbit = ctypes.POINTER(_Rotary), ctypes.POINTER(_FourbitCache)
+    lib.pcg_cache_append_rotary.argtypes = [vp, i64, i32, vp, i64, vp, i64, i32, vp, vp, rotary, cache, vp, i64, vp, i64, vp]
+    lib.pcg_cache_append_rotary.restype = ctypes.c_int
+    lib.pcg_cache_append_fourbit.argtypes = [vp, i64, i32, vp, i64, vp, i64, ctypes.c_int, i32, vp, vp, rotary, fourbit, vp, i64, vp, vp, vp]
+    lib.pcg_cache_append_fourbit.restype = ctypes.c_int
+    lib.pcg_cache_attention_fourbit.argtypes = [vp, i64, ctypes.c_int, i32, i32, vp, vp, vp, i32, i32, fourbit, f32, vp, vp, sz, vp]
+    lib.pcg_cache_attention_fourbit.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -639,4 +656,128 @@ def pcg_prompt_attention(q, k, v, row_start, scale: Optional[float] = None, out=
         q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, dtype, shape[0], shape[1], kshape[1], shape[2],
         _int_ptr(row_start, (B + 1,), dev), B, shape[2] ** -0.5 if scale is None else scale, out.data_ptr(),
         workspace.data_ptr(), workspace.numel() * workspace.element_size(), at))
+    return out
+
+
+# ---- positions, and the cache that holds 4.5 bits a value --------------------------------------------------
+def _rotary_struct(table, interleaved: bool, dev: int) -> _Rotary:
+    _need(table.dim() == 2 and table.dtype is torch.float32 and table.is_contiguous() and table.get_device() == dev,
+          "table must be a contiguous float32 tensor [positions, dim] on the current device")
+    return _Rotary(table.shape[1], bool(interleaved), table.shape[0], table.data_ptr())
+
+
+def _rows_out(t, name: str, shape, dtype, dev: int):
+    """Stride of a given output [rows, heads, head_dim] whose heads are dense."""
+    got, stride = _packed(t, name, dtype, dev)
+    _need(got == shape, f"{name} must be {tuple(shape)}")
+    return stride
+
+
+def _queries(q, q_out, kshape, dtype, dev: int, beside):
+    """(address, stride, heads, q_out, its address, its stride) of the queries that a call turns."""
+    if q is None:
+        _need(q_out is None, "q_out without q")
+        return None, 0, 0, None, None, 0
+    shape, stride = _packed(q, "q", dtype, dev)
+    _need(shape[0] == kshape[0] and shape[2] == kshape[2], "q must have k's rows and head_dim")
+    if q_out is None:
+        q_out = _empty(q, shape, dtype, beside)
+        return q.data_ptr(), stride, shape[1], q_out, q_out.data_ptr(), shape[1] * shape[2]
+    return q.data_ptr(), stride, shape[1], q_out, q_out.data_ptr(), _rows_out(q_out, "q_out", shape, dtype, dev)
+
+
+def pcg_cache_append_rotary(q, k, v, slots, positions, table, k_cache, v_cache, interleaved: bool = False, q_out=None, k_out=None,
+                            stream=None):
+    """``pcg_cache_append_rotary``: the append of keys that are turned by the angles of their ``positions`` on the way, and
+    the queries of the same rows, turned; returns those.
+
+    ``table`` [positions, dim] float32 holds the cosines, then the sines, of dim / 2 pairs; dimensions behind ``dim`` stay as
+    they are.  ``q`` may be None.  ``q_out`` (allocated here if omitted) may be ``q``; ``k_out``, if given, receives the
+    turned keys and may be ``k``.  Rows with a negative position are left alone, in every output."""
+    dev = _device(k)
+    cache = _cache_struct(k_cache, v_cache, dev)
+    shape, ks = _packed(k, "k", k_cache.dtype, dev)
+    vshape, vs = _packed(v, "v", k_cache.dtype, dev)
+    _need(shape == vshape and shape[1] == cache.kv_heads and shape[2] == cache.head_dim,
+          "k and v must be [rows, kv_heads, head_dim] of the cache")
+    rotary = _rotary_struct(table, interleaved, dev)
+    rows = shape[:1]
+    slot_ptr, pos_ptr = _int_ptr(slots, rows, dev), _int_ptr(positions, rows, dev)
+    at, beside = _place(stream, dev)
+    q_ptr, qs, heads, q_out, out_ptr, os = _queries(q, q_out, shape, k.dtype, dev, beside)
+    ko_ptr, kos = (None, 0) if k_out is None else (k_out.data_ptr(), _rows_out(k_out, "k_out", shape, k.dtype, dev))
+    if beside is not None:
+        _lend(beside, q, k, v, slots, positions, table, k_cache, v_cache, q_out, k_out)
+    _check((_lib or load()).pcg_cache_append_rotary(q_ptr, qs, heads, k.data_ptr(), ks, v.data_ptr(), vs, shape[0], slot_ptr, pos_ptr,
+                                                    ctypes.byref(rotary), ctypes.byref(cache), out_ptr, os, ko_ptr, kos, at))
+    return q_out
+
+
+def pcg_fourbit_cache_shape(n_blocks: int, kv_heads: int, block_size: int, head_dim: int):
+    """Shape of a cache that holds 4.5 bits a value (uint8): pages of 16 tokens, keys and values together."""
+    return n_blocks, kv_heads, block_size // 16, 18 * head_dim
+
+
+def _fourbit_struct(cache, k_scale: float, v_scale: float, dev: int) -> _FourbitCache:
+    shape = cache.shape
+    _need(len(shape) == 4 and cache.dtype is torch.uint8 and cache.is_contiguous() and cache.get_device() == dev and shape[3] % 18 == 0,
+          "cache must be a contiguous uint8 tensor [n_blocks, kv_heads, block_size / 16, 18 * head_dim] on the current device")
+    return _FourbitCache(shape[0], shape[2] * 16, shape[1], shape[3] // 18, k_scale, v_scale, cache.data_ptr())
+
+
+def _held_out(t, name: str, shape, dtype, dev: int):
+    if t is None:
+        return None
+    _need(t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev, f"{name} must be contiguous, of k's shape, type and device")
+    return t.data_ptr()
+
+
+def pcg_cache_append_fourbit(q, k, v, slots, cache, positions=None, table=None, interleaved: bool = False, k_scale: float = 1.0,
+                             v_scale: float = 1.0, q_out=None, k_out=None, v_out=None, stream=None):
+    """``pcg_cache_append_fourbit``: keys and values [rows, kv_heads, head_dim] into a cache of ``pcg_fourbit_cache_shape``.
+
+    With ``table`` the keys are turned by the angles of their ``positions`` first, and so are the queries ``q``, which are
+    returned (see ``pcg_cache_append_rotary``); without, ``q`` is None.  ``k_out`` and ``v_out``, if given, receive what the
+    cache now holds of the rows."""
+    dev = _device(k)
+    four = _fourbit_struct(cache, k_scale, v_scale, dev)
+    shape, ks = _packed(k, "k", k.dtype, dev)
+    vshape, vs = _packed(v, "v", k.dtype, dev)
+    _need(shape == vshape and shape[1] == four.kv_heads and shape[2] == four.head_dim,
+          "k and v must be [rows, kv_heads, head_dim] of the cache")
+    _need((table is None) == (positions is None) and (q is None or table is not None), "positions and table go together, and q with them")
+    rows = shape[:1]
+    slot_ptr, pos_ptr, rotary = _int_ptr(slots, rows, dev), None, None
+    if table is not None:
+        pos_ptr, rotary = _int_ptr(positions, rows, dev), ctypes.byref(_rotary_struct(table, interleaved, dev))
+    at, beside = _place(stream, dev)
+    ko_ptr, vo_ptr = _held_out(k_out, "k_out", shape, k.dtype, dev), _held_out(v_out, "v_out", shape, k.dtype, dev)
+    q_ptr, qs, heads, q_out, out_ptr, os = _queries(q, q_out, shape, k.dtype, dev, beside)
+    if beside is not None:
+        _lend(beside, q, k, v, slots, positions, table, cache, q_out, k_out, v_out)
+    _check((_lib or load()).pcg_cache_append_fourbit(q_ptr, qs, heads, k.data_ptr(), ks, v.data_ptr(), vs,
+                                                     _DTYPES.get(k.dtype) or dtype_code(k), shape[0], slot_ptr, pos_ptr, rotary,
+                                                     ctypes.byref(four), out_ptr, os, ko_ptr, vo_ptr, at))
+    return q_out
+
+
+def pcg_cache_attention_fourbit(q, row_start, kv_len, block_table, cache, scale: Optional[float] = None, k_scale: float = 1.0,
+                                v_scale: float = 1.0, out=None, workspace=None, stream=None):
+    """``pcg_cache_attention_fourbit``: ``pcg_cache_attention`` over what a cache of ``pcg_fourbit_cache_shape`` holds;
+    ``k_scale`` and ``v_scale`` are those that it was written with."""
+    dev = _device(q)
+    four = _fourbit_struct(cache, k_scale, v_scale, dev)
+    shape, stride = _packed(q, "q", q.dtype, dev)
+    _need(shape[2] == four.head_dim and block_table.dim() == 2 and row_start.dim() == 1,
+          "q must have the cache's head_dim, block_table be [B, max_blocks], row_start [B + 1]")
+    B, max_blocks = block_table.shape
+    dtype = _DTYPES.get(q.dtype) or dtype_code(q)
+    at, beside = _place(stream, dev)
+    out, workspace = _attention_buffers(q, shape, out, workspace, B, four.kv_heads, dtype, dev, beside)
+    if beside is not None:
+        _lend(beside, q, row_start, kv_len, block_table, cache, out, workspace)
+    _check((_lib or load()).pcg_cache_attention_fourbit(
+        q.data_ptr(), stride, dtype, shape[0], shape[1], _int_ptr(row_start, (B + 1,), dev), _int_ptr(kv_len, (B,), dev),
+        _int_ptr(block_table, (B, max_blocks), dev), B, max_blocks, ctypes.byref(four), shape[2] ** -0.5 if scale is None else scale,
+        out.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), at))
     return out

@@ -171,7 +171,6 @@ pcg_status run_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, vo
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
 }
 
-// What both calls refuse alike.
 pcg_status check_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, float scale) {
     if (a.rows < 0 || a.B < 0 || a.q_heads < 1 || a.kv_heads < 1 || a.q_heads % a.kv_heads || a.q_heads > 65535 ||
         !(scale > 0.f) || !std::isfinite(scale)) {

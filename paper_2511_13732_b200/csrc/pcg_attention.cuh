@@ -22,6 +22,8 @@ constexpr int kAttnMaxB = 16384, kAttnMaxGroup = 128;
 // cores, float32 on the FMA pipes.  Both need attention_work_bytes(d) of workspace.
 inline bool attention_shares(int d) { return d == 64 || d == 128; }
 size_t attention_work_bytes(int32_t d);
+// What all attention calls refuse alike.
+pcg_status check_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, float scale);
 pcg_status attention_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream);
 pcg_status attention_f32(const char *who, const AttnArgs &a, void *workspace, cudaStream_t stream);
 

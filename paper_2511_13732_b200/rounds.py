@@ -18,7 +18,8 @@ and chunks with fewer drafts may be among them)::
 Nothing here waits for the GPU: lengths stay there from round to round.  A call runs on its ``stream``, or on the current
 one; where that is another one than the last call's, it is put behind it, so that a round may use several (what a graph
 replays is the caller's to order).  What a call reads has to be complete on its stream.  The arithmetic is the library's
-(``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cache_attention``, ``pcg_prompt_attention``, ``pcg_verify``).
+(``pcg_cache_plan``, ``pcg_cache_append``, ``pcg_cache_attention``, ``pcg_prompt_attention``, ``pcg_verify``; with positions
+``pcg_cache_append_rotary``; with 4 bits ``pcg_cache_append_fourbit`` and ``pcg_cache_attention_fourbit``).
 """
 from __future__ import annotations
 
@@ -34,19 +35,31 @@ class DecodeRounds:
     """Cache, block tables and lengths of ``B`` sequences (rows of a batch; a finished one's row is free for another).
 
     ``n_blocks`` blocks of ``block_size`` tokens are shared by all sequences and all layers' caches alike; a sequence
-    holds ``max_blocks`` at most."""
+    holds ``max_blocks`` at most.
+
+    ``rotary``: a table [positions, dim] float32 of the cosines, then the sines, of each position's angles; queries and keys
+    are then turned by the angles of their tokens' positions (pairs of adjacent dimensions where ``interleaved``).
+    ``fourbit``: the cache holds 4.5 bits a value, with ``k_scale`` and ``v_scale`` as ``pcg_cache_append_fourbit`` says;
+    ``dtype`` is then not used, q, k and v may be of any type."""
 
     def __init__(self, B: int, layers: int, n_blocks: int, block_size: int, kv_heads: int, head_dim: int, max_blocks: int,
-                 dtype=torch.bfloat16, device="cuda"):
+                 dtype=torch.bfloat16, device="cuda", rotary=None, interleaved: bool = False, fourbit: bool = False, k_scale: float = 1.0,
+                 v_scale: float = 1.0):
         if min(B, layers, n_blocks, max_blocks) < 1:
             raise ValueError("B, layers, n_blocks and max_blocks must be at least 1")
 
         def ints(*shape, fill=0):
             return torch.full(shape, fill, dtype=torch.int32, device=device)
 
-        shape = (layers, n_blocks, kv_heads, block_size, head_dim)
-        self.k_cache = torch.empty(shape, dtype=dtype, device=device)
-        self.v_cache = torch.empty(shape, dtype=dtype, device=device)
+        self.k_cache = self.v_cache = self.cache = None
+        if fourbit:
+            shape = (layers, *binding.pcg_fourbit_cache_shape(n_blocks, kv_heads, block_size, head_dim))
+            self.cache = torch.empty(shape, dtype=torch.uint8, device=device)
+        else:
+            shape = (layers, n_blocks, kv_heads, block_size, head_dim)
+            self.k_cache = torch.empty(shape, dtype=dtype, device=device)
+            self.v_cache = torch.empty(shape, dtype=dtype, device=device)
+        self.rotary, self.interleaved, self._scales = rotary, interleaved, dict(k_scale=k_scale, v_scale=v_scale)
         self.block_size, self.B = block_size, B
         self.block_table = ints(B, max_blocks, fill=-1)
         self.free_ring = torch.arange(n_blocks, dtype=torch.int32, device=device)
@@ -73,7 +86,7 @@ class DecodeRounds:
             if not torch.cuda.is_current_stream_capturing():  # a captured call cannot wait for what is not in the graph
                 self._stream.wait_stream(last)
             binding._lend(self._stream, self.cached_len, self.held, self.ring_state, self.accept_len, self.block_table, self.free_ring,
-                          self.k_cache, self.v_cache, self._workspace)
+                          self.k_cache, self.v_cache, self.cache, self.rotary, self._workspace)
         return stream
 
     def _on(self, stream):
@@ -95,11 +108,12 @@ class DecodeRounds:
     def attend(self, layer: int, q, k, v, scale: Optional[float] = None, fresh: bool = False, out=None, stream=None):
         """One layer's attention of the round's rows: q [rows, q_heads, head_dim], k and v [rows, kv_heads, head_dim].
 
-        Writes k and v to the cache first.  ``fresh`` says that no sequence has anything cached, and every one of the
-        round's was given its blocks: the rows' own keys and values are then read instead of the cache."""
+        Writes k and v to the cache first, where the state has a rotation turned with q.  ``fresh`` says that no sequence has
+        anything cached, and every one of the round's was given its blocks: the rows' own keys and values are then read instead
+        of the cache (as it holds them, where that is in 4 bits)."""
         if self.plan is None:
             raise RuntimeError("no round has begun")
-        plan, kc, vc = self.plan, self.k_cache[layer], self.v_cache[layer]
+        plan = self.plan
         rows = plan.slots.shape[0]
         if q.shape[0] != rows or k.shape[0] != rows:  # fewer would cut sequences short, whose rows then see fewer keys
             raise ValueError(f"the round has {rows} rows; q has {q.shape[0]}, k {k.shape[0]}")
@@ -107,9 +121,29 @@ class DecodeRounds:
         if self._workspace is None:
             need = binding.pcg_attention_workspace_bytes(self.B, q.shape[1], k.shape[1], q.shape[2], binding.dtype_code(q))
             self._workspace = binding._empty(self.cached_len, need, torch.uint8, stream)
-        binding.pcg_cache_append(k, v, plan.slots, kc, vc, stream=stream)
+        turned = self.rotary is not None
+        if self.cache is not None:
+            cache, k_out, v_out = self.cache[layer], None, None
+            if fresh:
+                k_out, v_out = (binding._empty(t, t.shape, t.dtype, stream) for t in (k, v))
+            q_turned = binding.pcg_cache_append_fourbit(q if turned else None, k, v, plan.slots, cache, k_out=k_out, v_out=v_out, stream=stream,
+                                                        positions=plan.positions if turned else None, table=self.rotary,
+                                                        interleaved=self.interleaved, **self._scales)
+            q, k, v = q_turned if turned else q, k_out, v_out
+        elif turned:
+            kc, vc = self.k_cache[layer], self.v_cache[layer]
+            k_out = binding._empty(k, k.shape, k.dtype, stream) if fresh else None
+            q = binding.pcg_cache_append_rotary(q, k, v, plan.slots, plan.positions, self.rotary, kc, vc, interleaved=self.interleaved,
+                                                k_out=k_out, stream=stream)
+            k = k_out
+        else:
+            kc, vc = self.k_cache[layer], self.v_cache[layer]
+            binding.pcg_cache_append(k, v, plan.slots, kc, vc, stream=stream)
         if fresh:
             return binding.pcg_prompt_attention(q, k, v, plan.row_start, scale=scale, out=out, workspace=self._workspace, stream=stream)
+        if self.cache is not None:
+            return binding.pcg_cache_attention_fourbit(q, plan.row_start, plan.kv_len, self.block_table, cache, scale=scale, out=out,
+                                                       workspace=self._workspace, stream=stream, **self._scales)
         return binding.pcg_cache_attention(q, plan.row_start, plan.kv_len, self.block_table, kc, vc, scale=scale, out=out,
                                            workspace=self._workspace, stream=stream)
 
