@@ -27,6 +27,11 @@ pcg_status check_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, 
 pcg_status attention_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream);
 pcg_status attention_f32(const char *who, const AttnArgs &a, void *workspace, cudaStream_t stream);
 
+// Over the cache that holds 4.5 bits a value (k: its pages): 16-bit types, head dimensions 64 and 128, up to kFourbitCols query
+// heads a key head.  Needs attention_work_bytes(d) of workspace.
+constexpr int kFourbitCols = 48;
+pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, float v_scale, void *workspace, cudaStream_t stream);
+
 #ifdef __CUDACC__
 
 // Rows of sequence b, cut to the packed rows whatever row_start holds, and the keys that its last row may see.

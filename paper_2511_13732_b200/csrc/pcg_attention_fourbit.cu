@@ -197,6 +197,8 @@ extern "C" pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_strid
     }
     st = check_here(who, out);
     if (st != PCG_OK) return st;
+    if (dtype != PCG_F32 && (a.d == 64 || a.d == 128) && q_heads / a.kv_heads <= kFourbitCols)
+        return attention_fourbit_tc(who, a, dtype, cache->v_scale, workspace, (cudaStream_t)stream);
     PCG_DISPATCH_DTYPE(dtype, launch_fourbit_simple<LogitT>(a, cache->v_scale, (cudaStream_t)stream));
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);

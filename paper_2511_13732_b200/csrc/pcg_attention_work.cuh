@@ -100,7 +100,8 @@ inline __device__ int64_t tiles_before(int n, int len, int TQ, int p) {
 constexpr int kItemUnits = 4, kLeast = 4;
 
 // By all threads of the block: where runs `block` and `block + 1` begin, to out[0] and out[1].  `scratch` holds B
-// int64_t and B int32_t (192 KB of shared memory at the most).
+// int64_t and B int32_t (192 KB of shared memory at the most).  The two costs are the calling kernel's.
+template <int kItemUnits = pcg::kItemUnits, int kLeast = pcg::kLeast>
 inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int64_t *warp_units, int64_t *warp_items, Run *out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, B = a.B;
     int64_t *units = scratch;                                 // [B] of the sequences before b
