@@ -30,6 +30,9 @@ pcg_status attention_f32(const char *who, const AttnArgs &a, void *workspace, cu
 // Over the cache that holds 4.5 bits a value (k: its pages): 16-bit types, head dimensions 64 and 128, up to kFourbitCols query
 // heads a key head.  Needs attention_work_bytes(d) of workspace.
 constexpr int kFourbitCols = 48;
+// The other one takes calls of few rows: `rows` of a sequence and key head, on average, up to few_rows(d).
+inline int few_rows(int d) { return d == 64 ? 32 : 24; }
+pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int rows, float v_scale, void *workspace, cudaStream_t stream);
 pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, float v_scale, void *workspace, cudaStream_t stream);
 
 #ifdef __CUDACC__

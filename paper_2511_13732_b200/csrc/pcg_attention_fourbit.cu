@@ -197,8 +197,12 @@ extern "C" pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_strid
     }
     st = check_here(who, out);
     if (st != PCG_OK) return st;
-    if (dtype != PCG_F32 && (a.d == 64 || a.d == 128) && q_heads / a.kv_heads <= kFourbitCols)
+    if (dtype != PCG_F32 && (a.d == 64 || a.d == 128) && q_heads / a.kv_heads <= kFourbitCols) {
+        // how many rows a sequence has is on the GPU: their average is known here
+        const int64_t few = ((int64_t)rows + B - 1) / B * (q_heads / a.kv_heads);
+        if (few <= few_rows(a.d)) return attention_fourbit_few(who, a, dtype, (int)few, cache->v_scale, workspace, (cudaStream_t)stream);
         return attention_fourbit_tc(who, a, dtype, cache->v_scale, workspace, (cudaStream_t)stream);
+    }
     PCG_DISPATCH_DTYPE(dtype, launch_fourbit_simple<LogitT>(a, cache->v_scale, (cudaStream_t)stream));
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);

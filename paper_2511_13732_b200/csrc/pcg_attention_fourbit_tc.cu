@@ -19,7 +19,8 @@
 //              first tile and where that bit is set.
 // Warps 8-11   keys, 12-15 values: codes to operands.
 // Warp 16      copies: pages of 16 tokens are contiguous, whatever the block size; a tile is 8 of them.
-// Warp 17      products.      Warp 18  queries: rounded to float16 with a power of two for each row.
+// Warp 17      products for the scores, 19 for the outputs.  (By one warp, each product also waited for the other kind's turn.)
+// Warp 18      queries: rounded to float16 with a power of two for each row.
 #include <cuda_bf16.h>
 
 #include <atomic>
@@ -34,7 +35,12 @@ namespace pcg {
 namespace {
 
 constexpr int kCols = kFourbitCols, kKeys = 128;  // rows of a slot; keys of a tile
-constexpr int kFourbitThreads = 32 * 19;
+constexpr int kFourbitThreads = 32 * 20;
+// Registers: 640 threads are launched with 96; the softmax's 8 warps take 144, which the other 12 leave by keeping 64
+// (8 * 32 * 144 + 12 * 32 * 64 = 640 * 96).
+#define PCG_SOFTMAX_REGISTERS "144"
+#define PCG_OTHER_REGISTERS "64"
+constexpr int kScoreBufs = 3;  // scores in tensor memory: those of the tiles and slots in turn
 constexpr int kPBytes = kKeys * 128;  // weights of a tile: 64 columns of 16 bits a key, 128-byte swizzled
 constexpr float kSlack = 8.f;         // the reference may lag the maximum by a factor 2^8 before sums are scaled
 // Weights are kept 2^7 higher than the reference says, out of the range where float16 loses bits: 2^8 above the reference is
@@ -48,8 +54,9 @@ struct Sizes4 {
     static constexpr int kQBytes = 4 * kQSlot;           // two slots, of this item and the next
     static constexpr int kWeights = 4 * kPBytes;         // two slots, two tiles each
     static constexpr int kStage = 8 * page_bytes(D);
-    static constexpr int kStages = D == 128 ? 6 : 12;
-    static constexpr int kSmem = kQBytes + kWeights + kStages * kStage;
+    static constexpr int kScales = D / 16 * kKeys * 2;   // of a tile's values, as float16
+    static constexpr int kStages = D == 128 ? 5 : 12;
+    static constexpr int kSmem = kQBytes + kWeights + 2 * kScales + kStages * kStage;
     static_assert(kSmem >= kAttnMaxB * 12, "the cut's scratch");
 };
 
@@ -74,6 +81,24 @@ __device__ __forceinline__ float *four_part(void *ws, int block, int which) {
     return reinterpret_cast<float *>((char *)ws + kHeadBytes) + ((size_t)block * 2 + which) * kFourPartRows * (D + 2);
 }
 
+// bar_wait_hot with a poll that may sleep for 10 us: of 20 warps most wait, and their polls would take the issue slots (and
+// instruction cache) of those that work.
+constexpr uint32_t kPollTime = 10000;
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile int *failed) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < (1u << 17); ++i) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(bar), "r"(parity), "r"(kPollTime)
+            : "memory");
+        if (done) return true;
+        if (*failed) return false;
+    }
+    *failed = 1;
+    return false;
+}
 __device__ __forceinline__ void warps_meet(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 // Whether any of a slot's 128 threads says so.
 __device__ __forceinline__ bool slot_any(int id, bool mine) {
@@ -94,13 +119,14 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     const __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
     return *reinterpret_cast<const uint32_t *>(&r);
 }
-// Sums of 16 columns over a warp's lanes: lane i and lane i + 16 end with column i's.
-__device__ __forceinline__ float column_sums(const float *x, int lane) {
-    float v[16];
+// Sums of N (8 or 16) columns, held in pairs, over a warp's lanes: lane i < N ends with column i's.
+template <int N>
+__device__ __forceinline__ float column_sums(const uint64_t *x, int lane) {
+    float v[N];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = x[i];
+    for (int i = 0; i < N; i += 2) unpair(x[i / 2], v[i], v[i + 1]);
 #pragma unroll
-    for (int w = 8; w >= 1; w >>= 1) {
+    for (int w = N / 2; w >= 1; w >>= 1) {
         const bool up = lane & w;
 #pragma unroll
         for (int i = 0; i < w; ++i) {
@@ -108,7 +134,24 @@ __device__ __forceinline__ float column_sums(const float *x, int lane) {
             v[i] = keep + __shfl_xor_sync(0xffffffffu, give, w);
         }
     }
-    return v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
+#pragma unroll
+    for (int w = N; w < 32; w <<= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], w);
+    return v[0];
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t *v) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : PCG_R8(v, 0) : "r"(addr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t *v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr), PCG_W8(v, 0) : "memory");
+}
+// N (8, 16, 32 or 48) columns of the warp's lanes, waited for.
+template <int N>
+__device__ __forceinline__ void load_columns(uint32_t addr, uint32_t (&v)[N]) {
+    if (N == 8) tmem_ld8(addr, v);
+    if (N >= 32) tmem_ld32(addr, v);
+    if (N == 16 || N == 48) tmem_ld16(addr + (N & 32), v + (N & 32));
+    tmem_wait_ld();
+    tmem_loaded<N>(v);
 }
 
 template <typename T>
@@ -129,7 +172,7 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     __shared__ int64_t warp_units[kFourbitThreads / 32], warp_items[kFourbitThreads / 32];
     __shared__ Run run[2];
-    __shared__ __align__(8) uint64_t bars[2 * S + 29];
+    __shared__ __align__(8) uint64_t bars[2 * S + 32];
     __shared__ float q_by[2][2][kCols];      // of an item's rows (buffer, slot): what a product is multiplied by, 0 for padding
     __shared__ int q_lim[2][2][kCols];       // ... how many keys it sees
     __shared__ float4 col[2][kCols / 2];     // of a slot's column pairs: factors, then -reference + lift; later the joined factors
@@ -138,8 +181,8 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
     __shared__ uint32_t tmem_slot;
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t qbuf = smem_u32(smem_raw), pbuf = qbuf + Z::kQBytes, ring = pbuf + Z::kWeights, bar0 = smem_u32(bars);
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const uint32_t qbuf = smem_u32(smem_raw), pbuf = qbuf + Z::kQBytes, scale_buf = pbuf + Z::kWeights, ring = scale_buf + 2 * Z::kScales, bar0 = smem_u32(bars);
     auto full_bar = [&](int s) { return bar0 + 8u * s; };         // a stage has landed
     auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };  // ... been read
     const uint32_t more = bar0 + 16u * S;
@@ -147,24 +190,24 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
     auto k_empty = [&](int i) { return more + 16u + 8u * i; };
     auto v_full = [&](int i) { return more + 32u + 8u * i; };
     auto v_empty = [&](int i) { return more + 48u + 8u * i; };
-    auto s_full = [&](int s) { return more + 64u + 8u * s; };     // a slot's scores are complete
-    auto s_empty = [&](int s) { return more + 80u + 8u * s; };    // ... read
-    auto p_full = [&](int s, int i) { return more + 96u + 16u * s + 8u * i; };  // a slot's weights are in place (two buffers)
-    auto p_empty = [&](int s, int i) { return more + 128u + 16u * s + 8u * i; };
-    auto o_full = [&](int s) { return more + 160u + 8u * s; };    // a slot's last product of a part is complete
-    auto o_empty = [&](int s) { return more + 176u + 8u * s; };   // its outputs have been read
-    auto q_full = [&](int i) { return more + 192u + 8u * i; };    // an item's queries are in place (two buffers)
-    auto q_empty = [&](int i) { return more + 208u + 8u * i; };
-    const uint32_t drain = more + 224u;
+    auto s_full = [&](int i) { return more + 64u + 8u * i; };     // scores are complete (a ring of three)
+    auto s_empty = [&](int i) { return more + 88u + 8u * i; };    // ... read
+    auto p_full = [&](int s, int i) { return more + 112u + 16u * s + 8u * i; };  // a slot's weights are in place (two buffers)
+    auto p_empty = [&](int s, int i) { return more + 144u + 16u * s + 8u * i; };
+    auto o_full = [&](int s) { return more + 176u + 8u * s; };    // a slot's last product of a part is complete
+    auto o_empty = [&](int s) { return more + 192u + 8u * s; };   // its outputs have been read
+    auto q_full = [&](int i) { return more + 208u + 8u * i; };    // an item's queries are in place (two buffers)
+    auto q_empty = [&](int i) { return more + 224u + 8u * i; };
+    const uint32_t drain = more + 240u;  // of the two warps that issue products
 
     if (tid == 0) {
-        for (int i = 0; i < 2 * S + 29; ++i) {
+        for (int i = 0; i < 2 * S + 32; ++i) {
             const uint32_t bar = bar0 + 8u * i;
             uint32_t count = 1;  // by the hardware, or one thread
             if (bar >= empty_bar(0) && bar < more) count = 4 + kValueWarps;
             if (bar == k_full(0) || bar == k_full(1)) count = 4;
             if (bar == v_full(0) || bar == v_full(1)) count = kValueWarps;
-            if ((bar >= s_empty(0) && bar <= p_full(1, 1))) count = 4;
+            if (bar >= s_empty(0) && bar <= p_full(1, 1)) count = 4;
             if (bar == o_empty(0) || bar == o_empty(1)) count = 4;
             if (bar == q_empty(0) || bar == q_empty(1)) count = 9;
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
@@ -182,8 +225,9 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
     const uint32_t tmem = tmem_slot;
     auto k_col = [&](int i) { return tmem + (uint32_t)(i * 64); };
     auto v_col = [&](int i) { return tmem + (uint32_t)(128 + i * 64); };
-    auto s_col = [&](int s) { return tmem + (uint32_t)(256 + s * 64); };
-    auto o_col = [&](int s) { return tmem + (uint32_t)(384 + s * 64); };
+    auto s_col = [&](int i) { return tmem + (uint32_t)(256 + i * kCols); };
+    auto o_col = [&](int s) { return tmem + (uint32_t)(256 + (kScoreBufs + s) * kCols); };
+    static_assert(256 + (kScoreBufs + 2) * kCols <= 512, "tensor memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int G = a.q_heads / a.kv_heads, TQ = kCols / G;
@@ -200,21 +244,23 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
 
     if (warp < 8) {
         // ------------------------------------------------------------------ softmax: thread = key of a tile
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 " PCG_SOFTMAX_REGISTERS ";");
         const int slot = warp >> 2, row = (warp & 3) * 32 + lane, wg_id = 1 + slot, wt = tid & 127;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t sc = s_col(slot) + lanes, oc = o_col(slot) + lanes;
+        const uint32_t oc = o_col(slot) + lanes;
         uint32_t count = 0, outs = 0, outs_other = 0, part = 0;  // tiles of this slot, its outputs, the other's, parts so far
+        uint32_t sb = 0, s_phase = 0;                             // buffer of the next scores (of either slot), its phase
         // After a wait that ran out the waits return at once; the role goes on to its end, since its warps meet at barriers.
         for (; walk.next(a, TQ, g); ++part) {
             const int qb = part & 1;
             const Split sp = split_of(g.n, g.pair, TQ);
             const int tokens = !g.two ? sp.tokens : slot ? sp.tokens - sp.tq : sp.tq, t_first = g.pair * 2 * TQ + (g.two && slot ? sp.tq : 0);
-            const int rows = tokens * G, chunks = (rows + 15) >> 4;
+            const int rows = tokens * G;
             const int nt = tiles(g), first = g.two ? 0 : slot, step = g.two ? 1 : 2, k_first = first_key(g), k_end = last_key(g);
             const int qs = g.two ? slot : 0;  // whose queries
             const int least = min(g.len - g.n + t_first + 1, k_end);  // keys that every row sees
             const bool mine = first < nt, shared = !g.two && nt > 1;
-            bar_wait_hot(q_full(qb), (part >> 1) & 1, failed);
+            wait_for(q_full(qb), (part >> 1) & 1, failed);
             if (wt < kCols) {
                 float *c = reinterpret_cast<float *>(&col[slot][wt >> 1]) + (wt & 1);
                 c[0] = q_by[qb][qs][wt];
@@ -222,143 +268,150 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
                 col_m[qb][slot][wt] = kNegInf;
             }
             warps_meet(wg_id, 128);
-            float l[kCols];
-#pragma unroll
-            for (int i = 0; i < kCols; ++i) l[i] = 0.f;
-#pragma unroll 1
-            for (int t = first; t < nt; t += step, ++count) {
-                bar_wait_hot(s_full(slot), count & 1, failed);
-                fence_after();
-                const int key = k_first + t * kKeys + row;
-                uint32_t x[16];
-                if (key - row + kKeys > least) {  // scores of keys that a row does not see become -inf where they lie
-#pragma unroll 1
-                    for (int c = 0; c < chunks; ++c) {
-                        tmem_ld16(sc + c * 16, x);
-                        tmem_wait_ld();
-                        tmem_loaded<16>(x);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (key >= min(q_lim[qb][qs][c * 16 + i], k_end)) x[i] = __float_as_uint(kNegInf);
-                        tmem_st16(sc + c * 16, x);
-                    }
-                    tmem_wait_st();
+            auto next_scores = [&]() {
+                if (++sb == kScoreBufs) {
+                    sb = 0;
+                    s_phase ^= 1;
                 }
-                bool move = t == first;
-                if (!move) {
-                    float top = kNegInf;
-#pragma unroll 1
-                    for (int c = 0; c < chunks; ++c) {
-                        tmem_ld16(sc + c * 16, x);
-                        tmem_wait_ld();
-                        tmem_loaded<16>(x);
+            };
+            if (slot) next_scores();  // slot 0's first tile's come before this one's
+            // The part's tiles with N columns: as many as the slot has rows, or the next of 8, 16, 32, 48.  Their sums stay in
+            // registers, and the scores of a tile.
+            auto part_of = [&](auto columns) {
+                constexpr int N = decltype(columns)::value;
+                uint64_t l[N / 2];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 f = col[slot][c * 8 + i];
+                for (int i = 0; i < N / 2; ++i) l[i] = 0;
+#pragma unroll 1
+                for (int t = first; t < nt; t += step, ++count) {
+                    wait_for(s_full(sb), s_phase, failed);
+                    fence_after();
+                    const int k0 = k_first + t * kKeys, key = k0 + row;
+                    const uint32_t sc = s_col(sb) + lanes;
+                    uint32_t x[N];
+                    auto load = [&]() {
+                        load_columns<N>(sc, x);
+                        if (__builtin_expect(k0 + kKeys > least, 0)) {  // keys that a row does not see
+#pragma unroll
+                            for (int i = 0; i < N; ++i)
+                                if (key >= min(q_lim[qb][qs][i], k_end)) x[i] = __float_as_uint(kNegInf);
+                        }
+                    };
+                    auto relate = [&]() {  // scores to the references
+#pragma unroll
+                        for (int i = 0; i < N / 2; ++i) {
+                            const float4 f = col[slot][i];
                             float t0, t1;
                             unpair(fma2(pair(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), pair(f.x, f.y), pair(f.z, f.w)), t0, t1);
-                            top = fmaxf(top, fmaxf(t0, t1));
+                            x[2 * i] = __float_as_uint(t0);
+                            x[2 * i + 1] = __float_as_uint(t1);
                         }
-                    }
-                    move = slot_any(wg_id, top > kSlack + kLift);
-                }
-                if (move) {
-#pragma unroll 1
-                    for (int c = 0; c < chunks; ++c) {
-                        tmem_ld16(sc + c * 16, x);
-                        tmem_wait_ld();
-                        tmem_loaded<16>(x);
-                        float most = 0.f;
+                    };
+                    bool place = t == first;  // whether references are moved
+                    load();
+                    if (!place) {
+                        relate();
+                        float top = kNegInf;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
+                        for (int i = 0; i < N; i += 2)  // (NaN counts for nothing)
+                            asm("max.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(__uint_as_float(x[i])), "f"(__uint_as_float(x[i + 1])));
+                        place = slot_any(wg_id, top > kSlack + kLift);
+                        if (__builtin_expect(place, 0)) load();
+                    }
+                    if (__builtin_expect(place, 0)) {
+                        float most[(N + 15) / 16];
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
                             const float m = warp_max(__uint_as_float(x[i]));
-                            if (lane == i) most = m;
+                            if ((i & 15) == 0 || lane == (i & 15)) most[i / 16] = m;
                         }
-                        if (lane < 16) warp_col[slot][warp & 3][c * 16 + lane] = most;
-                    }
-                    warps_meet(wg_id, 128);
-                    if (wt < rows) {
-                        float *c = reinterpret_cast<float *>(&col[slot][wt >> 1]) + (wt & 1);
-                        float top = warp_col[slot][0][wt];
 #pragma unroll
-                        for (int w = 1; w < 4; ++w) top = fmaxf(top, warp_col[slot][w][wt]);
-                        top *= c[0];
-                        const float m = col_m[qb][slot][wt];
-                        // also when the first score above -inf is met
-                        const bool up = top > m + kSlack;
-                        col_f[slot][wt] = up ? ex2(m - top) : 1.f;
-                        if (up) {
-                            col_m[qb][slot][wt] = top;
-                            c[2] = kLift - top;
+                        for (int j = 0; j < (N + 15) / 16; ++j)
+                            if (lane < 16 && j * 16 + lane < N) warp_col[slot][warp & 3][j * 16 + lane] = most[j];
+                        warps_meet(wg_id, 128);
+                        if (wt < rows) {
+                            float *c = reinterpret_cast<float *>(&col[slot][wt >> 1]) + (wt & 1);
+                            float top = warp_col[slot][0][wt];
+#pragma unroll
+                            for (int w = 1; w < 4; ++w) top = fmaxf(top, warp_col[slot][w][wt]);
+                            top *= c[0];
+                            const float m = col_m[qb][slot][wt];
+                            // also when the first score above -inf is met
+                            const bool up = top > m + kSlack;
+                            col_f[slot][wt] = up ? ex2(m - top) : 1.f;
+                            if (up) {
+                                col_m[qb][slot][wt] = top;
+                                c[2] = kLift - top;
+                            }
+                        } else if (wt < kCols) {
+                            col_f[slot][wt] = 1.f;
                         }
-                    } else if (wt < kCols) {
-                        col_f[slot][wt] = 1.f;
-                    }
-                    warps_meet(wg_id, 128);
-                    if (t > first) {
-                        // the product before this one is complete: then the outputs so far are scaled
-                        bar_wait_hot(p_empty(slot, (count - 1) & 1), ((count - 1) >> 1) & 1, failed);
-                        fence_after();
+                        warps_meet(wg_id, 128);
+                        if (t > first) {
+                            // the product before this one is complete: then the outputs so far are scaled
+                            wait_for(p_empty(slot, (count - 1) & 1), ((count - 1) >> 1) & 1, failed);
+                            fence_after();
 #pragma unroll 1
-                        for (int c = 0; c < chunks; ++c) {
-                            tmem_ld16(oc + c * 16, x);
-                            tmem_wait_ld();
-                            tmem_loaded<16>(x);
+                            for (int c = 0; c < N; c += 8) {
+                                uint32_t o[8];
+                                load_columns<8>(oc + c, o);
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * col_f[slot][c * 16 + i]);
-                            tmem_st16(oc + c * 16, x);
+                                for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * col_f[slot][c + i]);
+                                tmem_st8(oc + c, o);
+                            }
+                            tmem_wait_st();
                         }
-                        tmem_wait_st();
+#pragma unroll
+                        for (int i = 0; i < N / 2; ++i) {
+                            const float2 f = reinterpret_cast<const float2 *>(col_f[slot])[i];
+                            l[i] = fma2(l[i], pair(f.x, f.y), 0);
+                        }
+                        relate();
                     }
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(s_empty(sb));
+                    next_scores();
+                    if ((g.two && !slot) || t + 1 < nt) next_scores();  // the other slot's, of this tile or the next
+                    const int pb = count & 1;
+                    wait_for(p_empty(slot, pb), ((count >> 1) & 1) ^ 1, failed);
+                    const uint32_t to = pbuf + (slot * 2 + pb) * kPBytes + row * 128;
 #pragma unroll
-                    for (int i = 0; i < kCols; ++i) l[i] *= col_f[slot][i];
-                }
-                // weights, 16 columns at a time: 32 bytes of the key's row
-                const int pb = count & 1;
-                bar_wait_hot(p_empty(slot, pb), ((count >> 1) & 1) ^ 1, failed);
-                const uint32_t to = pbuf + (slot * 2 + pb) * kPBytes + row * 128;
+                    for (int c = 0; c < N; c += 8) {  // 16 bytes of the key's row
+                        uint32_t p[4];
 #pragma unroll
-                for (int c = 0; c < kCols / 16; ++c) {
-                    if (c >= chunks) break;
-                    tmem_ld16(sc + c * 16, x);
-                    tmem_wait_ld();
-                    tmem_loaded<16>(x);
-                    uint32_t p[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 f = col[slot][c * 8 + i];
-                        float t0, t1;
-                        unpair(fma2(pair(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), pair(f.x, f.y), pair(f.z, f.w)), t0, t1);
-                        t0 = ex2(t0);
-                        t1 = ex2(t1);
-                        l[c * 16 + 2 * i] += t0;
-                        l[c * 16 + 2 * i + 1] += t1;
-                        p[i] = pack2<false>(t0, t1);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((2 * c + i) ^ (row & 7)) * 16)), "r"(p[4 * i]),
-                                     "r"(p[4 * i + 1]), "r"(p[4 * i + 2]), "r"(p[4 * i + 3])
+                        for (int i = 0; i < 4; ++i) {
+                            const float t0 = ex2(__uint_as_float(x[c + 2 * i])), t1 = ex2(__uint_as_float(x[c + 2 * i + 1]));
+                            l[c / 2 + i] = add2(l[c / 2 + i], pair(t0, t1));
+                            p[i] = pack2<false>(t0, t1);
+                        }
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + (((c >> 3) ^ (row & 7)) * 16)), "r"(p[0]), "r"(p[1]),
+                                     "r"(p[2]), "r"(p[3])
                                      : "memory");
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(p_full(slot, pb));
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    bar_arrive(s_empty(slot));
-                    bar_arrive(p_full(slot, pb));
+                if (mine) {
+#pragma unroll
+                    for (int c = 0; c < N; c += 16) {
+                        const float s = column_sums<(N < 16 ? N : 16)>(l + c / 2, lane);
+                        if (lane < 16 && c + lane < N) warp_col[slot][warp & 3][c + lane] = s;
+                    }
                 }
-            }
+            };
+            if (rows <= 8)
+                part_of(std::integral_constant<int, 8>());
+            else if (rows <= 16)
+                part_of(std::integral_constant<int, 16>());
+            else if (rows <= 32)
+                part_of(std::integral_constant<int, 32>());
+            else
+                part_of(std::integral_constant<int, 48>());
             // ---- end of the part: the columns' sums, then the outputs, thread = dimension
             if (mine) {
-                for (int c = 0; c < kCols / 16; ++c) {
-                    if (c >= chunks) break;
-                    float s = 0.f;
-#pragma unroll
-                    for (int j = 0; j < kCols / 16; ++j)
-                        if (j == c) s = column_sums(l + j * 16, lane);
-                    if (lane < 16) warp_col[slot][warp & 3][c * 16 + lane] = s;
-                }
                 warps_meet(wg_id, 128);
                 if (wt < rows) {
                     const float s = (warp_col[slot][0][wt] + warp_col[slot][1][wt]) + (warp_col[slot][2][wt] + warp_col[slot][3][wt]);
@@ -367,11 +420,11 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
                     // within 2^8 of the reference that stands in until then, which is 0
                     if (col_m[qb][slot][wt] == kNegInf && s != 0.f) col_m[qb][slot][wt] = 0.f;
                 }
-                bar_wait_hot(o_full(slot), outs++ & 1, failed);
+                wait_for(o_full(slot), outs++ & 1, failed);
             }
             if (shared) {  // the slots join their sums, each for half of the rows
                 warps_meet(3, 256);
-                bar_wait_hot(o_full(slot ^ 1), outs_other++ & 1, failed);
+                wait_for(o_full(slot ^ 1), outs_other++ & 1, failed);
             } else if (g.two || !mine) {
                 ++outs_other;
             }
@@ -445,6 +498,7 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
         }
     } else if (warp < 16) {
         // ------------------------------------------------------------------ codes to operands: thread = key, or value dimension
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
         const bool keys = warp < 12;
         const int row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -454,78 +508,97 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
             const int nt = tiles(g), k_first = first_key(g), k_end = last_key(g);
 #pragma unroll 1
             for (int t = 0; t < nt; ++t, ++T0) {
-                ok = __all_sync(0xffffffffu, bar_wait_hot(full_bar(stage), stage_phase, failed));
+                ok = __all_sync(0xffffffffu, wait_for(full_bar(stage), stage_phase, failed));
                 const uint32_t buf = T0 & 1, parity = ((T0 >> 1) & 1) ^ 1;
-                ok = ok && __all_sync(0xffffffffu, bar_wait_hot(keys ? k_empty(buf) : v_empty(buf), parity, failed));
+                ok = ok && __all_sync(0xffffffffu, wait_for(keys ? k_empty(buf) : v_empty(buf), parity, failed));
                 if (!ok) break;
                 fence_after();
+                // (small loops: in line, the two took 1,300 and 2,000 cycles a tile, out of the instruction cache)
                 const uint32_t at = ring + stage * Z::kStage;
                 if (keys) {
                     const uint32_t page = at + (row >> 4) * kPage;
-                    uint32_t scale[D / 32];  // two a register
+                    uint32_t codes = page + (row & 15) * 16, to = k_col(buf) + lanes;
+                    uint64_t scales;
                     if (D == 128) {
-                        uint32_t w[2];
-                        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(page + key_scales_at(D) + (row & 15) * 8) : "memory");
-                        widen_scales(w[0], reinterpret_cast<uint32_t(&)[2]>(scale[0]));
-                        widen_scales(w[1], reinterpret_cast<uint32_t(&)[2]>(scale[D / 32 - 2]));
+                        asm volatile("ld.shared.b64 %0, [%1];" : "=l"(scales) : "r"(page + key_scales_at(D) + (row & 15) * 8) : "memory");
                     } else {
-                        uint32_t w;
-                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(page + key_scales_at(D) + (row & 15) * 4) : "memory");
-                        widen_scales(w, reinterpret_cast<uint32_t(&)[2]>(scale[0]));
+                        uint32_t four;
+                        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(four) : "r"(page + key_scales_at(D) + (row & 15) * 4) : "memory");
+                        scales = four;
                     }
+#pragma unroll 1
+                    for (int c = 0; c < D / 64; ++c) {  // 64 dimensions, four scales
+                        uint32_t w[8], s[2];
 #pragma unroll
-                    for (int h = 0; h < D / 64; ++h) {
-                        uint32_t r[32];
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            uint32_t w[4];
+                        for (int h = 0; h < 2; ++h)
                             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                         : "r"(page + (2 * h + c) * 256 + (row & 15) * 16)
+                                         : "=r"(w[4 * h]), "=r"(w[4 * h + 1]), "=r"(w[4 * h + 2]), "=r"(w[4 * h + 3])
+                                         : "r"(codes + h * 256)
                                          : "memory");
-                            const uint32_t s = scale[2 * h + c], s0 = __byte_perm(s, s, 0x1010), s1 = __byte_perm(s, s, 0x3232);
+                        widen_scales((uint32_t)scales, s);
+                        scales >>= 32;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t s0 = __byte_perm(s[h], s[h], 0x1010), s1 = __byte_perm(s[h], s[h], 0x3232);
+                            uint32_t r[16];
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 uint32_t v[4];
-                                widen_codes(w[i], v);
+                                widen_codes(w[4 * h + i], v);
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) r[c * 16 + i * 4 + j] = mul2(v[j], i < 2 ? s0 : s1);
+                                for (int j = 0; j < 4; ++j) r[i * 4 + j] = mul2(v[j], i < 2 ? s0 : s1);
                             }
+                            tmem_st16(to + h * 16, r);
                         }
-                        tmem_st32(k_col(buf) + lanes + h * 32, r);
+                        codes += 512;
+                        to += 32;
                     }
                 } else {
-                    const int left = k_end - (k_first + t * kKeys);  // tokens of this tile; what lies behind them may be anything
+                    // The scales first, 8 a thread, as float16 to where all 16 dimensions of a group find them; those of tokens
+                    // behind the part's last key, which may be anything, as 0.
+                    const int left = k_end - (k_first + t * kKeys), groups = D / 16;
+                    const int page_of = row / (2 * groups), in = row % (2 * groups), token = page_of * 16 + (in & 1) * 8;
+                    uint32_t two[2], f[4];
+                    asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(two[0]), "=r"(two[1]) : "r"(at + page_of * kPage + value_scales_at(D) + in * 8) : "memory");
+                    widen_scales(two[0], reinterpret_cast<uint32_t(&)[2]>(f[0]));
+                    widen_scales(two[1], reinterpret_cast<uint32_t(&)[2]>(f[2]));
+                    if (__builtin_expect(left < kKeys, 0)) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t r[32];
+                        for (int i = 0; i < 4; ++i)
+                            f[i] = token + 2 * i >= left ? 0u : token + 2 * i + 1 >= left ? f[i] & 0xffffu : f[i];
+                    }
+                    const uint32_t table = scale_buf + buf * Z::kScales;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(table + (in >> 1) * (kKeys * 2) + token * 2), "r"(f[0]), "r"(f[1]),
+                                 "r"(f[2]), "r"(f[3])
+                                 : "memory");
+                    warps_meet(4, kValueWarps * 32);
+                    uint32_t codes = at + value_codes_at(D) + row * 8, scales = table + (row >> 4) * (kKeys * 2), to = v_col(buf) + lanes;
+#pragma unroll 1
+                    for (int h = 0; h < 4; ++h) {  // two pages
+                        uint32_t r[16];
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            const uint32_t page = at + (h * 4 + q) * kPage;
-                            uint32_t c[2], w[4];
-                            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(page + value_codes_at(D) + row * 8) : "memory");
-                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                                         : "r"(page + value_scales_at(D) + (row & ~15))
-                                         : "memory");
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t c[2], s[8];
+                            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(codes + q * kPage) : "memory");
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                uint32_t v[4], s[4];
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                                             : "=r"(s[4 * i]), "=r"(s[4 * i + 1]), "=r"(s[4 * i + 2]), "=r"(s[4 * i + 3])
+                                             : "r"(scales + q * 32 + i * 16)
+                                             : "memory");
+                            }
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                uint32_t v[4];
                                 widen_codes(c[i], v);
-                                widen_scales(w[2 * i], reinterpret_cast<uint32_t(&)[2]>(s[0]));
-                                widen_scales(w[2 * i + 1], reinterpret_cast<uint32_t(&)[2]>(s[2]));
 #pragma unroll
-                                for (int j = 0; j < 4; ++j) r[q * 8 + i * 4 + j] = mul2(v[j], s[j]);
+                                for (int j = 0; j < 4; ++j) r[q * 8 + i * 4 + j] = mul2(v[j], s[i * 4 + j]);
                             }
                         }
-                        if (left < kKeys) {
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                const int token = h * 64 + 2 * i;
-                                r[i] = token >= left ? 0u : token + 1 >= left ? r[i] & 0xffffu : r[i];
-                            }
-                        }
-                        tmem_st32(v_col(buf) + lanes + h * 32, r);
+                        tmem_st16(to, r);
+                        codes += 2 * kPage;
+                        scales += 64;
+                        to += 16;
                     }
                 }
                 __syncwarp();
@@ -540,7 +613,9 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
                 }
             }
         }
-    } else if (warp == 16) {
+    } else {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+      if (warp == 16) {
         // ------------------------------------------------------------------ copies: a lane per copy looks its block up
         const int unit = min(1 << a.bs_shift, 64);  // tokens of one copy
         uint32_t it = 0, stage = 0, stage_phase = 1;
@@ -565,7 +640,7 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
 #pragma unroll 1
             for (int t = 0; t < nt; ++t) {
                 const int32_t later = block_of(g, t + 2);  // its latency passes under the wait
-                ok = __all_sync(0xffffffffu, bar_wait_hot(empty_bar(stage), stage_phase, failed));
+                ok = __all_sync(0xffffffffu, wait_for(empty_bar(stage), stage_phase, failed));
                 if (!ok) break;
                 const int k0 = k_first + t * kKeys, p = k0 + lane * unit;
                 const int pages = now == -1 ? 0 : min(unit, k_end - p + 15) >> 4;
@@ -616,74 +691,96 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
         if (*failed)  // giving up: copies already asked for may still be landing
             for (uint32_t back = 1; back <= S && back <= it; ++back) bar_drain(full_bar((it - back) % S), ((it - back) / S) & 1);
     } else if (warp == 17) {
-        // ------------------------------------------------------------------ products, all by one lane
-        if (elect_one()) {
-            uint32_t T0 = 0, part = 0, issued[2] = {0, 0}, used[2] = {0, 0};  // tiles; of each slot: scores and weights taken
-            bool ok = true;
-            auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && bar_wait_hot(bar, parity, failed); };
-            auto scores = [&](int s, int kb, uint64_t q, uint32_t idesc) {
-                constexpr int kPart = (kCols * 128) >> 4;
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) mma_ts(s_col(s), k_col(kb) + kk * 8, q + (kk >> 2) * kPart + (kk & 3) * 2, idesc, kk > 0);
-                mma_commit(s_full(s));
-            };
-            auto outputs = [&](int s, int vb, uint64_t p, uint32_t idesc, bool begun) {
-#pragma unroll
-                for (int kk = 0; kk < kKeys / 16; ++kk) mma_ts(o_col(s), v_col(vb) + kk * 8, p + kk * (2048 >> 4), idesc, begun || kk > 0);
-            };
-            while (ok && walk.next(a, TQ, g)) {
-                const int qb = part & 1, nt = tiles(g);
-                const Split sp = split_of(g.n, g.pair, TQ);
-                uint32_t n_of[2];  // N / 8 of the slots' products, in its place in the instruction descriptor
-                n_of[0] = (uint32_t)((sp.tq * G + 15) >> 4) << 18;
-                n_of[1] = g.two ? (uint32_t)(((sp.tokens - sp.tq) * G + 15) >> 4) << 18 : n_of[0];
-                wait(q_full(qb), (part >> 1) & 1);
+        // ------------------------------------------------------------------ scores, issued by an elected lane
+        uint32_t T0 = 0, part = 0, sb = 0, s_phase = 1;  // tiles, parts; buffer and phase of the next scores
+        bool ok = true;
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, wait_for(bar, parity, failed)); };
+        while (ok && walk.next(a, TQ, g)) {
+            const Split sp = split_of(g.n, g.pair, TQ);
+            const int qb = part & 1;
+            // (the same in all lanes, and known to be: operands of products then stay in uniform registers)
+            const int nt = __shfl_sync(0xffffffffu, tiles(g), 0), two = __shfl_sync(0xffffffffu, (int)g.two, 0);
+            // N / 8 of the slots' products, in its place in the instruction descriptor
+            const uint32_t n0 = __shfl_sync(0xffffffffu, (uint32_t)((sp.tq * G + 15) >> 4) << 18, 0);
+            const uint32_t n1 = two ? __shfl_sync(0xffffffffu, (uint32_t)(((sp.tokens - sp.tq) * G + 15) >> 4) << 18, 0) : n0;
+            wait(q_full(qb), (part >> 1) & 1);
 #pragma unroll 1
-                for (int t = 0; ok && t <= nt; ++t) {
-                    if (t < nt) {
-                        const int kb = (T0 + t) & 1;
-                        wait(k_full(kb), ((T0 + t) >> 1) & 1);
+            for (int t = 0; ok && t < nt; ++t) {
+                const int kb = (T0 + t) & 1;
+                wait(k_full(kb), ((T0 + t) >> 1) & 1);
 #pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            if (!g.two && s != (t & 1)) continue;
-                            wait(s_empty(s), (issued[s] & 1) ^ 1);
-                            if (!ok) break;
-                            fence_after();
-                            scores(s, kb, desc_k(qbuf + qb * (2 * Z::kQSlot) + (g.two ? s : 0) * Z::kQSlot), kIdescQK | n_of[s]);
-                            ++issued[s];
-                        }
-                        if (!ok) break;
-                        mma_commit(k_empty(kb));
-                        if (t == nt - 1) mma_commit(q_empty(qb));
+                for (int s = 0; s < 2; ++s) {
+                    if (!two && s != (t & 1)) continue;
+                    wait(s_empty(sb), s_phase);
+                    if (!ok) break;
+                    fence_after();
+                    constexpr int kPart = (kCols * 128) >> 4;
+                    const uint64_t q = desc_k(qbuf + qb * (2 * Z::kQSlot) + (two ? s : 0) * Z::kQSlot);
+                    const uint32_t idesc = kIdescQK | (s ? n1 : n0);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk)
+                            mma_ts(s_col(sb), k_col(kb) + kk * 8, q + (kk >> 2) * kPart + (kk & 3) * 2, idesc, kk > 0);
+                        mma_commit(s_full(sb));
+                        if (s || !two) mma_commit(k_empty(kb));
+                        if ((s || !two) && t == nt - 1) mma_commit(q_empty(qb));
                     }
-                    if (t > 0) {
-                        const int u = t - 1, vb = (T0 + u) & 1;
-                        wait(v_full(vb), ((T0 + u) >> 1) & 1);
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            if (!g.two && s != (u & 1)) continue;
-                            const bool begun = u >= (g.two ? 1 : 2), last = u + (g.two ? 1 : 2) >= nt;
-                            const uint32_t pb = used[s] & 1;
-                            wait(p_full(s, pb), (used[s] >> 1) & 1);
-                            if (!begun) wait(o_empty(s), (part & 1) ^ 1);
-                            if (!ok) break;
-                            fence_after();
-                            outputs(s, vb, desc_mn(pbuf + (s * 2 + pb) * kPBytes, kKeys), kIdescPV | n_of[s], begun);
-                            mma_commit(p_empty(s, pb));
-                            if (last) mma_commit(o_full(s));
-                            ++used[s];
-                        }
-                        if (!ok) break;
-                        mma_commit(v_empty(vb));
+                    __syncwarp();
+                    if (++sb == kScoreBufs) {
+                        sb = 0;
+                        s_phase ^= 1;
                     }
                 }
-                T0 += nt;
-                ++part;
             }
-            if (*failed) {  // products already issued may still be writing tensor memory: it is freed when they have retired
-                mma_commit(drain);
-                bar_drain(drain, 0);
+            T0 += nt;
+            ++part;
+        }
+        if (*failed) {  // products already issued may still be writing tensor memory: it is freed when they have retired
+            if (elect_one()) mma_commit(drain);
+            bar_drain(drain, 0);
+        }
+    } else if (warp == 19) {
+        // ------------------------------------------------------------------ outputs, likewise
+        uint32_t T0 = 0, part = 0, used[2] = {0, 0};  // tiles; of the slots: weights taken
+        bool ok = true;
+        auto wait = [&](uint32_t bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, wait_for(bar, parity, failed)); };
+        while (ok && walk.next(a, TQ, g)) {
+            const Split sp = split_of(g.n, g.pair, TQ);
+            const int nt = __shfl_sync(0xffffffffu, tiles(g), 0), two = __shfl_sync(0xffffffffu, (int)g.two, 0), each = two ? 1 : 2;
+            const uint32_t n0 = __shfl_sync(0xffffffffu, (uint32_t)((sp.tq * G + 15) >> 4) << 18, 0);
+            const uint32_t n1 = two ? __shfl_sync(0xffffffffu, (uint32_t)(((sp.tokens - sp.tq) * G + 15) >> 4) << 18, 0) : n0;
+#pragma unroll 1
+            for (int t = 0; ok && t < nt; ++t) {
+                const int vb = (T0 + t) & 1;
+                wait(v_full(vb), ((T0 + t) >> 1) & 1);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (!two && s != (t & 1)) continue;
+                    const int pb = used[s] & 1, begun = t >= each;
+                    wait(p_full(s, pb), (used[s] >> 1) & 1);
+                    if (!begun) wait(o_empty(s), (part & 1) ^ 1);
+                    if (!ok) break;
+                    fence_after();
+                    ++used[s];
+                    const uint64_t p = desc_mn(pbuf + (s * 2 + pb) * kPBytes, kKeys);
+                    const uint32_t idesc = kIdescPV | (s ? n1 : n0);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int kk = 0; kk < kKeys / 16; ++kk)
+                            mma_ts(o_col(s), v_col(vb) + kk * 8, p + kk * (2048 >> 4), idesc, begun || kk > 0);
+                        mma_commit(p_empty(s, pb));
+                        if (t + each >= nt) mma_commit(o_full(s));
+                        if (s || !two) mma_commit(v_empty(vb));
+                    }
+                    __syncwarp();
+                }
             }
+            T0 += nt;
+            ++part;
+        }
+        if (*failed) {
+            if (elect_one()) mma_commit(drain + 8);
+            bar_drain(drain + 8, 0);
         }
     } else {
         // ------------------------------------------------------------------ queries of the next item
@@ -693,7 +790,7 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
         for (uint32_t part = 0; ok && walk.next(a, TQ, g); ++part) {
             const int qb = part & 1;
             const Split sp = split_of(g.n, g.pair, TQ);
-            ok = __all_sync(0xffffffffu, bar_wait_hot(q_empty(qb), ((part >> 1) & 1) ^ 1, failed));
+            ok = __all_sync(0xffffffffu, wait_for(q_empty(qb), ((part >> 1) & 1) ^ 1, failed));
             if (!ok) break;
 #pragma unroll 1
             for (int s = 0; s < (g.two ? 2 : 1); ++s) {
@@ -747,6 +844,7 @@ __global__ void __launch_bounds__(kFourbitThreads, 1)
             __syncwarp();
             if (lane == 0) bar_arrive(q_full(qb));
         }
+      }
     }
     fence_before();
     __syncthreads();

@@ -35,11 +35,14 @@ __device__ __forceinline__ float *part_base(void *ws, int block, int which, int 
 }
 
 // ---------------------------------------------------------------------------------------------- items
-__host__ __device__ __forceinline__ int pairs_of(int n, int TQ) { return (n + 2 * TQ - 1) / (2 * TQ); }
+// P row tiles an item, two or one; "pair" is the item's number among those of its sequence and key head.
+template <int P = 2>
+__host__ __device__ __forceinline__ int pairs_of(int n, int TQ) { return (n + P * TQ - 1) / (P * TQ); }
 // Keys of pair p in units of 64: up to what its last row sees, in whole key tiles, and one of them where it sees nothing.
+template <int P = 2>
 __device__ __forceinline__ int tiles_of(int n, int len, int TQ, int p) {
-    const int tokens = min(n - p * 2 * TQ, 2 * TQ), lim = len - n + p * 2 * TQ + tokens;
-    if (tokens > TQ) return lim <= kTile ? 2 : (lim + kTile - 1) / kTile * 2;
+    const int tokens = min(n - p * P * TQ, P * TQ), lim = len - n + p * P * TQ + tokens;
+    if (P == 2 && tokens > TQ) return lim <= kTile ? 2 : (lim + kTile - 1) / kTile * 2;
     return lim <= kHalf ? 1 : (lim + kHalf - 1) / kHalf;
 }
 
@@ -81,15 +84,18 @@ __device__ __forceinline__ int64_t floor_sum_128(uint32_t n, uint32_t a, int64_t
     return s;
 }
 // The same of a sequence's first p pairs together.
+template <int P = 2>
 inline __device__ int64_t tiles_before(int n, int len, int TQ, int p) {
-    const int step = 2 * TQ, whole = n / step, q = min(p, whole);  // `whole` pairs of 2 * TQ tokens, then one of fewer
-    // pairs whose last row sees at most one tile of keys count 1 each: (i + 1) * step <= 128 - (len - n)
+    constexpr int kKeys = P == 2 ? kTile : kHalf;  // of a key tile
+    const int step = P * TQ, whole = n / step, q = min(p, whole);  // `whole` pairs of P * TQ tokens, then one of fewer
+    // pairs whose last row sees at most one tile of keys count 1 each: (i + 1) * step <= kKeys - (len - n)
     const int base = len - n;
-    const int head = base >= kTile ? 0 : (int)min((int64_t)q, (kTile - (int64_t)base) / step);
+    const int head = base >= kKeys ? 0 : (int)min((int64_t)q, (kKeys - (int64_t)base) / step);
     int64_t s = head;
-    if (q > head) s += floor_sum_128(q - head, step, base + (int64_t)(head + 1) * step + kTile - 1);
-    s *= 2;
-    if (p > whole) s += tiles_of(n, len, TQ, whole);
+    if (q > head)  // (floors of 64ths as floors of 128ths of twice as much)
+        s += floor_sum_128(q - head, kTile / kKeys * step, kTile / kKeys * (base + (int64_t)(head + 1) * step + kKeys - 1));
+    s *= P;
+    if (p > whole) s += tiles_of<P>(n, len, TQ, whole);
     return s;
 }
 
@@ -99,9 +105,10 @@ inline __device__ int64_t tiles_before(int n, int len, int TQ, int p) {
 // short call's parts cost more to join than they save.
 constexpr int kItemUnits = 4, kLeast = 4;
 
-// By all threads of the block: where runs `block` and `block + 1` begin, to out[0] and out[1].  `scratch` holds B
+// By all threads of the block: where its W runs (numbers j * kMaxBlocks + block) and those behind them begin, to out[2 j] and
+// out[2 j + 1].  `scratch` holds B
 // int64_t and B int32_t (192 KB of shared memory at the most).  The two costs are the calling kernel's.
-template <int kItemUnits = pcg::kItemUnits, int kLeast = pcg::kLeast>
+template <int kItemUnits = pcg::kItemUnits, int kLeast = pcg::kLeast, int P = 2, int W = 1>
 inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int64_t *warp_units, int64_t *warp_items, Run *out) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, B = a.B;
     int64_t *units = scratch;                                 // [B] of the sequences before b
@@ -113,9 +120,9 @@ inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int
         items[b] = (int32_t)isum;
         int begin, n, len;
         attn_sequence(a, b, begin, n, len);
-        const int pairs = pairs_of(n, TQ);
+        const int pairs = pairs_of<P>(n, TQ);
         if (n > 0) {
-            const int64_t tiles = pairs == 1 ? tiles_of(n, len, TQ, 0) : tiles_before(n, len, TQ, pairs);
+            const int64_t tiles = pairs == 1 ? tiles_of<P>(n, len, TQ, 0) : tiles_before<P>(n, len, TQ, pairs);
             usum += (tiles + (int64_t)kItemUnits * pairs) * a.kv_heads;
             isum += pairs;
         }
@@ -148,8 +155,8 @@ inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int
         items[b] += (int32_t)ibase;
     }
     __syncthreads();
-    if (warp < 2) {  // a warp for each of the two
-        const int blocks = (int)max((int64_t)1, min((int64_t)kMaxBlocks, total / kLeast)), c = blockIdx.x + warp;
+    for (int j = warp; j < 2 * W; j += threads / 32) {  // a warp for each
+        const int blocks = (int)max((int64_t)1, min((int64_t)kMaxBlocks * W, total / kLeast)), c = (j >> 1) * kMaxBlocks + blockIdx.x + (j & 1);
         Run r{total - (int64_t)kItemUnits * a.kv_heads * all_items, 0, 0, 0, 0};  // behind the last keys
         // (64-bit divisions are calls; below 2^31 units, 32 bits do)
         const bool small = total <= 0x7fffffff;
@@ -167,8 +174,8 @@ inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int
             }
             int begin, n, len;
             attn_sequence(a, x, begin, n, len);
-            const int pairs = pairs_of(n, TQ);
-            const int64_t tiles = pairs == 1 ? tiles_of(n, len, TQ, 0) : tiles_before(n, len, TQ, pairs);
+            const int pairs = pairs_of<P>(n, TQ);
+            const int64_t tiles = pairs == 1 ? tiles_of<P>(n, len, TQ, 0) : tiles_before<P>(n, len, TQ, pairs);
             const int64_t per_head = tiles + (int64_t)kItemUnits * pairs, in = u - units[x];
             const int h = small ? (int)((uint32_t)in / (uint32_t)per_head) : (int)(in / per_head);
             const int64_t rest = in - h * per_head;
@@ -177,7 +184,7 @@ inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int
             int64_t head_tiles = 0;
             while (count > 1) {
                 const int step = (count + 31) / 32, mine = p + lane * step;
-                const int64_t before = lane * step < count && mine > 0 ? tiles_before(n, len, TQ, mine) : 0;
+                const int64_t before = lane * step < count && mine > 0 ? tiles_before<P>(n, len, TQ, mine) : 0;
                 const bool below = lane * step < count && before + (int64_t)kItemUnits * mine <= rest;
                 const int top = 31 - __clz(__ballot_sync(0xffffffffu, below));  // lane 0's always is
                 head_tiles = __shfl_sync(0xffffffffu, before, top);
@@ -186,14 +193,14 @@ inline __device__ void cut_work(const AttnArgs &a, int TQ, int64_t *scratch, int
             }
             // an item's own units come first: a cut within them leaves the whole item to the run behind it
             int64_t tile = max((int64_t)0, rest - head_tiles - (int64_t)kItemUnits * p - kItemUnits);
-            if (n - p * 2 * TQ > TQ) tile &= ~(int64_t)1;  // a whole key tile
+            if (P == 2 && n - p * 2 * TQ > TQ) tile &= ~(int64_t)1;  // a whole key tile
             r.first = units[x] - (int64_t)kItemUnits * a.kv_heads * items[x] + h * tiles + head_tiles + tile;
             r.b = x;
             r.h = h;
             r.pair = p;
             r.tile = (int)tile;
         }
-        if (lane == 0) out[warp] = r;
+        if (lane == 0) out[j] = r;
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // copies land in the scratch's place
     __syncthreads();
@@ -217,6 +224,7 @@ struct Walk {
         left = (int)min(next.first - r.first, (int64_t)0x7fffffff);
         if (left > 0) attn_sequence(a, b, begin, n, len);
     }
+    template <int P = 2>
     __device__ __forceinline__ bool next(const AttnArgs &a, int TQ, Segment &s) {
         if (left <= 0) return false;
         s.b = b;
@@ -225,14 +233,14 @@ struct Walk {
         s.begin = begin;
         s.n = n;
         s.len = len;
-        s.two = n - pair * 2 * TQ > TQ;
-        const int all = tiles_of(n, len, TQ, pair), nt = min(left, all - tile);
+        s.two = P == 2 && n - pair * 2 * TQ > TQ;
+        const int all = tiles_of<P>(n, len, TQ, pair), nt = min(left, all - tile);
         s.whole = nt == all;
         s.t0 = s.two ? tile >> 1 : tile;
         s.nt = s.two ? max(nt >> 1, 1) : nt;
         left -= nt;
         tile = 0;
-        if (left > 0 && ++pair == pairs_of(n, TQ)) {
+        if (left > 0 && ++pair == pairs_of<P>(n, TQ)) {
             pair = 0;
             if (++h == a.kv_heads) {
                 h = 0;
