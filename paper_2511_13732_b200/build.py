@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpcg.so")
 SOURCES = ["pcg_groups.cu", "pcg_kernels.cu", "pcg_host.cu", "pcg_asg.cu", "pcg_cache.cu", "pcg_attention.cu", "pcg_attention_tc.cu",
            "pcg_attention_f32.cu", "pcg_cache_rotary.cu", "pcg_attention_fourbit.cu",
-           "pcg_attention_fourbit_tc.cu", "pcg_attention_fourbit_few.cu"]
+           "pcg_attention_fourbit_few.cu"]
 HEADERS = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))) + [
     os.path.join(ROOT, "include", "pcg.h")]
 

@@ -14,6 +14,7 @@ struct AttnArgs {
     int32_t max_blocks, n_blocks, bs_shift;
     float scale_log2;
     int32_t few_tokens;  // (tensor cores) tokens of one copy of an item with one row tile
+    float v_scale;       // (4 bits) what outputs are multiplied by
 };
 
 constexpr int kAttnMaxB = 16384, kAttnMaxGroup = 128;
@@ -27,13 +28,11 @@ pcg_status check_attention(const char *who, const AttnArgs &a, pcg_dtype dtype, 
 pcg_status attention_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream);
 pcg_status attention_f32(const char *who, const AttnArgs &a, void *workspace, cudaStream_t stream);
 
-// Over the cache that holds 4.5 bits a value (k: its pages): 16-bit types, head dimensions 64 and 128, up to kFourbitCols query
-// heads a key head.  Needs attention_work_bytes(d) of workspace.
-constexpr int kFourbitCols = 48;
-// The other one takes calls of few rows: `rows` of a sequence and key head, on average, up to few_rows(d).
+// Over the cache that holds 4.5 bits a value (k: its pages): 16-bit types, head dimensions 64 and 128, attention_work_bytes(d) of
+// workspace.  Calls of few rows, `rows` of a sequence and key head on average, up to few_rows(d), have a kernel of their own.
 inline int few_rows(int d) { return d == 64 ? 32 : 24; }
-pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int rows, float v_scale, void *workspace, cudaStream_t stream);
-pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, float v_scale, void *workspace, cudaStream_t stream);
+pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int rows, void *workspace, cudaStream_t stream);
+pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream);
 
 #ifdef __CUDACC__
 

@@ -26,7 +26,7 @@ template <>
 __device__ __forceinline__ f16_t narrow<f16_t>(float x) { return f16_t{__half_as_ushort(__float2half_rn(x))}; }
 
 template <typename T, int DPL>  // DPL: values per lane, 32 * DPL = d
-__global__ void __launch_bounds__(kSimpleThreads) attention_fourbit_simple_kernel(const __grid_constant__ AttnArgs a, float v_scale) {
+__global__ void __launch_bounds__(kSimpleThreads) attention_fourbit_simple_kernel(const __grid_constant__ AttnArgs a) {
     constexpr int NW = kSimpleThreads / 32, d = 32 * DPL;
     __shared__ float qs[d];
     __shared__ float part[NW][d + 2];
@@ -143,22 +143,22 @@ __global__ void __launch_bounds__(kSimpleThreads) attention_fourbit_simple_kerne
         float o = 0.f;
         for (int w = 0; w < NW; ++w)
             if (part[w][d] != kNegInf) o += part[w][i] * exp2f(part[w][d] - top);
-        out[i] = narrow<T>(lim > 0 ? o / total * v_scale : 0.f);
+        out[i] = narrow<T>(lim > 0 ? o / total * a.v_scale : 0.f);
     }
 }
 
 template <typename T>
-void launch_fourbit_simple(const AttnArgs &a, float v_scale, cudaStream_t s) {
+void launch_fourbit_simple(const AttnArgs &a, cudaStream_t s) {
     const dim3 grid(a.rows, a.q_heads);
     switch (a.d / 32) {
-        case 1: attention_fourbit_simple_kernel<T, 1><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
-        case 2: attention_fourbit_simple_kernel<T, 2><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
-        case 3: attention_fourbit_simple_kernel<T, 3><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
-        case 4: attention_fourbit_simple_kernel<T, 4><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
-        case 5: attention_fourbit_simple_kernel<T, 5><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
-        case 6: attention_fourbit_simple_kernel<T, 6><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
-        case 7: attention_fourbit_simple_kernel<T, 7><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
-        default: attention_fourbit_simple_kernel<T, 8><<<grid, kSimpleThreads, 0, s>>>(a, v_scale); break;
+        case 1: attention_fourbit_simple_kernel<T, 1><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 2: attention_fourbit_simple_kernel<T, 2><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 3: attention_fourbit_simple_kernel<T, 3><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 4: attention_fourbit_simple_kernel<T, 4><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 5: attention_fourbit_simple_kernel<T, 5><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 6: attention_fourbit_simple_kernel<T, 6><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 7: attention_fourbit_simple_kernel<T, 7><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        default: attention_fourbit_simple_kernel<T, 8><<<grid, kSimpleThreads, 0, s>>>(a); break;
     }
 }
 
@@ -179,7 +179,7 @@ extern "C" pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_strid
     }
     const AttnArgs a{q, cache->data, nullptr, out, row_start, kv_len, block_table, q_stride, 0, 0, rows, B, q_heads,
                      cache->kv_heads, cache->head_dim, max_blocks, cache->n_blocks, __builtin_ctz(cache->block_size),
-                     scale * 1.4426950408889634f * cache->k_scale, 0};
+                     scale * 1.4426950408889634f * cache->k_scale, 0, cache->v_scale};
     st = check_attention(who, a, dtype, scale);
     if (st == PCG_OK && !(a.scale_log2 > 0.f && std::isfinite(a.scale_log2))) {
         set_error("%s: the scale %g and the keys' %g have no product in float32", who, (double)scale, (double)cache->k_scale);
@@ -197,13 +197,13 @@ extern "C" pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_strid
     }
     st = check_here(who, out);
     if (st != PCG_OK) return st;
-    if (dtype != PCG_F32 && (a.d == 64 || a.d == 128) && q_heads / a.kv_heads <= kFourbitCols) {
+    if (dtype != PCG_F32 && (a.d == 64 || a.d == 128)) {
         // how many rows a sequence has is on the GPU: their average is known here
         const int64_t few = ((int64_t)rows + B - 1) / B * (q_heads / a.kv_heads);
-        if (few <= few_rows(a.d)) return attention_fourbit_few(who, a, dtype, (int)few, cache->v_scale, workspace, (cudaStream_t)stream);
-        return attention_fourbit_tc(who, a, dtype, cache->v_scale, workspace, (cudaStream_t)stream);
+        if (few <= few_rows(a.d)) return attention_fourbit_few(who, a, dtype, (int)few, workspace, (cudaStream_t)stream);
+        return attention_fourbit_tc(who, a, dtype, workspace, (cudaStream_t)stream);
     }
-    PCG_DISPATCH_DTYPE(dtype, launch_fourbit_simple<LogitT>(a, cache->v_scale, (cudaStream_t)stream));
+    PCG_DISPATCH_DTYPE(dtype, launch_fourbit_simple<LogitT>(a, (cudaStream_t)stream));
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
 }

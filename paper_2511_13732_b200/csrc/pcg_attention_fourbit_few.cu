@@ -103,7 +103,7 @@ __device__ __forceinline__ uint32_t round_pair(float lo, float hi) {
 
 template <int D, int NT, typename T>
 __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
-    attention_fourbit_few_kernel(const __grid_constant__ AttnArgs a, float v_scale, void *ws) {
+    attention_fourbit_few_kernel(const __grid_constant__ AttnArgs a, void *ws) {
     using Z = Few<D, NT>;
     constexpr int W = Z::kWarps, S = Z::kStages, kPage = page_bytes(D), QR = D / 8;  // QR: a lane's registers of 8 queries
     extern __shared__ __align__(1024) unsigned char smem_raw[];
@@ -415,7 +415,7 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
             for (int e = 0; e < 2; ++e) {
 #pragma unroll
                 for (int w = 4; w < 32; w <<= 1) l[j][e] += __shfl_xor_sync(0xffffffffu, l[j][e], w);
-                inv[e] = v_scale / l[j][e];  // a row that sees scores of -inf alone is 0 / 0 = NaN
+                inv[e] = a.v_scale / l[j][e];  // a row that sees scores of -inf alone is 0 / 0 = NaN
                 const int row = 8 * j + 2 * li + e;
                 if (!g.whole && lg == 0 && row < rows) {
                     part[Z::kRows * D + row] = l[j][e] == 0.f ? kNegInf : ref[j][e];  // (nothing seen: no reference)
@@ -457,7 +457,7 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
 constexpr int kJoinThreads = 1024;
 
 template <int D, int NT, typename T>
-__global__ void __launch_bounds__(kJoinThreads) attention_fourbit_few_join_kernel(const __grid_constant__ AttnArgs a, float v_scale, void *ws) {
+__global__ void __launch_bounds__(kJoinThreads) attention_fourbit_few_join_kernel(const __grid_constant__ AttnArgs a, void *ws) {
     using Z = Few<D, NT>;
     constexpr int kPer = (Z::kRuns + kJoinThreads - 1) / kJoinThreads, N = D / 32;
     __shared__ int64_t first_of[Z::kRuns + 1];
@@ -559,14 +559,14 @@ __global__ void __launch_bounds__(kJoinThreads) attention_fourbit_few_join_kerne
         const int tok = r / G, t_row = next.pair * TQ + tok;
         const bool empty = len - n + t_row + 1 <= 0;
         uint32_t *to = reinterpret_cast<uint32_t *>((T *)a.out + (((int64_t)begin + t_row) * a.q_heads + (int64_t)next.h * G + (r - tok * G)) * D + dim);
-        const float inv = v_scale / l;
+        const float inv = a.v_scale / l;
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) to[i] = empty ? 0u : round_pair<T>(o[2 * i] * inv, o[2 * i + 1] * inv);
     }
 }
 
 template <int D, int NT, typename T>
-cudaError_t launch(const AttnArgs &a, float v_scale, void *ws, cudaStream_t stream) {
+cudaError_t launch(const AttnArgs &a, void *ws, cudaStream_t stream) {
     using Z = Few<D, NT>;
     static_assert(few_bytes<D, NT>() <= 148ull * 2 * 256 * (D + 2) * 4 + 4096, "the workspace");
     static std::atomic<uint64_t> prepared{0};  // devices whose kernel has been given its shared memory
@@ -577,29 +577,29 @@ cudaError_t launch(const AttnArgs &a, float v_scale, void *ws, cudaStream_t stre
         if (e == cudaSuccess && dev <= 63) prepared.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     if (e == cudaSuccess)
-        e = launch_behind(attention_fourbit_few_kernel<D, NT, T>, dim3(kMaxBlocks), 32 * Z::kWarps, (size_t)Z::kSmem, stream, a, v_scale, ws);
+        e = launch_behind(attention_fourbit_few_kernel<D, NT, T>, dim3(kMaxBlocks), 32 * Z::kWarps, (size_t)Z::kSmem, stream, a, ws);
     if (e == cudaSuccess)
-        e = launch_behind(attention_fourbit_few_join_kernel<D, NT, T>, dim3(kMaxBlocks), kJoinThreads, 0, stream, a, v_scale, ws);
+        e = launch_behind(attention_fourbit_few_join_kernel<D, NT, T>, dim3(kMaxBlocks), kJoinThreads, 0, stream, a, ws);
     return e;
 }
 
 template <int D, typename T>
-cudaError_t dispatch(const AttnArgs &a, int rows, float v_scale, void *ws, cudaStream_t stream) {
-    if (rows <= 8) return launch<D, 1, T>(a, v_scale, ws, stream);
-    if (rows <= 16) return launch<D, 2, T>(a, v_scale, ws, stream);
+cudaError_t dispatch(const AttnArgs &a, int rows, void *ws, cudaStream_t stream) {
+    if (rows <= 8) return launch<D, 1, T>(a, ws, stream);
+    if (rows <= 16) return launch<D, 2, T>(a, ws, stream);
     if constexpr (D == 64)
-        if (rows > 24) return launch<D, 4, T>(a, v_scale, ws, stream);
-    return launch<D, 3, T>(a, v_scale, ws, stream);
+        if (rows > 24) return launch<D, 4, T>(a, ws, stream);
+    return launch<D, 3, T>(a, ws, stream);
 }
 
 }  // namespace
 
-pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int rows, float v_scale, void *ws, cudaStream_t stream) {
+pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int rows, void *ws, cudaStream_t stream) {
     cudaError_t e;
     if (a.d == 128)
-        e = dtype == PCG_BF16 ? dispatch<128, uint16_t>(a, rows, v_scale, ws, stream) : dispatch<128, f16_t>(a, rows, v_scale, ws, stream);
+        e = dtype == PCG_BF16 ? dispatch<128, uint16_t>(a, rows, ws, stream) : dispatch<128, f16_t>(a, rows, ws, stream);
     else
-        e = dtype == PCG_BF16 ? dispatch<64, uint16_t>(a, rows, v_scale, ws, stream) : dispatch<64, f16_t>(a, rows, v_scale, ws, stream);
+        e = dtype == PCG_BF16 ? dispatch<64, uint16_t>(a, rows, ws, stream) : dispatch<64, f16_t>(a, rows, ws, stream);
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
 }
 

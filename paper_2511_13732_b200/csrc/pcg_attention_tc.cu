@@ -35,12 +35,19 @@
 #include <type_traits>
 
 #include "pcg_attention_work.cuh"
+#include "pcg_fourbit.cuh"
 #include "pcg_tcgen05.cuh"
 
 namespace pcg {
 
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
+// Over the cache that holds 4.5 bits a value: 8 warps between the fetch and the products widen codes to float16 tiles, and one
+// rounds queries to float16.  640 threads are launched with 96 registers each; the softmax's 8 warps take 152, which the other
+// 12 leave by keeping 56 (8 * 32 * 152 + 12 * 32 * 56 = 60,416 of 61,440).
+constexpr int kWidenWarps = 8, kFourbitThreads = 32 * (kSoftmaxWarps + kWidenWarps + 4);
+#define PCG_SOFTMAX_REGISTERS "152"
+#define PCG_OTHER_REGISTERS "56"
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
 
 // 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs.  All by the special-function unit: with
@@ -69,39 +76,64 @@ __device__ __forceinline__ void store_row(void *p, const uint32_t (&w)[8], bool 
     }
 }
 
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+
 // ---------------------------------------------------------------------------------------------- main kernel
-template <int D>
+template <int D, bool FOUR>
 struct Sizes {
     static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
     // Ring, 160 KB: a stage holds 128 keys or their values, or 64 keys and then their values, each as D / 64 parts.
-    static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr int kSmem = (2 + kStages) * kTileBytes;  // 224 KB; 3 KB are left for all else
-    static_assert((2 + kStages) * kTileBytes >= kAttnMaxB * 12, "the cut's scratch");
+    // (4 bits: 128 KB; the codes of 64 keys and their values lie in one of three stages before it)
+    static constexpr int kStages = FOUR ? (D == 128 ? 4 : 9) : D == 128 ? 5 : 10;
+    static constexpr int kCodeStages = FOUR ? (D == 128 ? 3 : 6) : 0, kCodeBytes = 4 * page_bytes(D);
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + kCodeStages * kCodeBytes;  // 219 or 224 KB; 3 KB are left for all else
+    static_assert(kSmem >= kAttnMaxB * 12, "the cut's scratch");
 };
 
-template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads, 1)
+// FOUR: over the cache that holds 4.5 bits a value.  Operands are float16 whatever the queries' type: codes times scales have six
+// significant bits, bfloat16 queries are multiplied by a power of two, a row's own, that brings them into range.  Values are
+// K-major there (a dimension's keys together, as the codes are): parts of D rows of 64 keys.
+template <int D, bool BF16, bool FOUR>
+__global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap qmap,
                         const __grid_constant__ CUtensorMap qmap_few, const __grid_constant__ CUtensorMap kmap,
                         const __grid_constant__ CUtensorMap vmap, void *ws) {
-    constexpr int S = Sizes<D>::kStages, kParts = D / 64, kTileBytes = Sizes<D>::kTileBytes;
+    using Z = Sizes<D, FOUR>;
+    constexpr int S = Z::kStages, kParts = D / 64, kTileBytes = Z::kTileBytes, U = Z::kCodeStages, kAll = FOUR ? kFourbitThreads : kThreads;
+    constexpr bool kWide = BF16 && !FOUR;  // bfloat16 operands
     // instruction descriptors: D = fp32, A and B of one 16-bit type, M = 128; N = 128 keys, B K-major; N = D, B MN-major
-    constexpr uint32_t kType = BF16 ? (1u << 7) | (1u << 10) : 0u;
+    constexpr uint32_t kType = kWide ? (1u << 7) | (1u << 10) : 0u;
     constexpr uint32_t kIdescQK = (1u << 4) | kType | ((kTile >> 3) << 17) | ((kTile >> 4) << 24);
     constexpr uint32_t kIdescQKHalf = (1u << 4) | kType | ((kHalf >> 3) << 17) | ((kTile >> 4) << 24);  // N = 64 keys
-    constexpr uint32_t kIdescPV = (1u << 4) | kType | (1u << 16) | ((D >> 3) << 17) | ((kTile >> 4) << 24);
+    constexpr uint32_t kIdescPV = (1u << 4) | kType | (FOUR ? 0u : 1u << 16) | ((D >> 3) << 17) | ((kTile >> 4) << 24);
     // float16's weights are kept 2^7 higher than the reference says, out of the range where they lose bits: 2^8 above the
     // reference is then 2^15 at most.  The sums carry the same factor, so it cancels.
-    constexpr float kLift = BF16 ? 0.f : 7.f;
+    constexpr float kLift = kWide ? 0.f : 7.f;
 
     extern __shared__ __align__(1024) unsigned char smem_raw[];  // swizzled tiles start on 1024-byte boundaries
-    __shared__ int64_t warp_units[kThreads / 32], warp_items[kThreads / 32];
+    __shared__ int64_t warp_units[kAll / 32], warp_items[kAll / 32];
     __shared__ Run run[2];
-    __shared__ __align__(8) uint64_t bars[2 * S + 15];
+    __shared__ __align__(8) uint64_t bars[2 * S + 15 + (FOUR ? 2 * U + 4 : 0)];
+    __shared__ float q_by[FOUR ? 2 : 1][FOUR ? kTile : 1];  // (4 bits) of the rows of the queries' two tiles: what scores are multiplied by
     __shared__ float slot_m[2][kTile], slot_l[2][kTile];  // for the end of an item with one row tile
     __shared__ uint32_t tmem_slot;
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
+    auto wait_on = [](uint32_t bar, uint32_t parity, volatile int *failed) {
+        if constexpr (FOUR)
+            return bar_wait_small(bar, parity, failed);
+        else
+            return bar_wait(bar, parity, failed);
+    };
+    auto wait_hot = [](uint32_t bar, uint32_t parity, volatile int *failed) {
+        if constexpr (FOUR)
+            return bar_wait_small(bar, parity, failed);
+        else
+            return bar_wait_hot(bar, parity, failed);
+    };
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t qbuf = smem_u32(smem_raw), ring = qbuf + 2 * kTileBytes, bar0 = smem_u32(bars);
     auto full_bar = [&](int s) { return bar0 + 8u * s; };         // a stage has landed
@@ -113,13 +145,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     auto written = [&](int s) { return q_full + 104u + 8u * s; };  // a slot's outputs of an item are out of its stage
     auto p_half = [&](int s) { return q_full + 88u + 8u * s; };   // ... those of the first 64 keys
     const uint32_t merge_full = q_full + 72, merge_done = q_full + 80;  // both slots' references and sums are there, read
+    // 4 bits: the queries' two tiles have their own barriers, for an item with one row tile takes one of them, in turn, and the next
+    // item's are rounded meanwhile; codes of 64 keys have landed, been read
+    auto tile_full = [&](int i) { return q_full + 120u + 8u * i; };
+    auto tile_empty = [&](int i) { return q_full + 136u + 8u * i; };
+    auto code_full = [&](int i) { return q_full + 152u + 8u * i; };
+    auto code_empty = [&](int i) { return q_full + 152u + 8u * (U + i); };
+    const uint32_t codes = ring + S * kTileBytes;
 
     if (tid == 0) {
-        for (int i = 0; i < 2 * S + 15; ++i) {
+        for (int i = 0; i < 2 * S + 15 + (FOUR ? 2 * U + 4 : 0); ++i) {
             // by a slot's warps: its weights, its outputs (4); by both slots': the hand-over (8); by one thread or the
             // hardware: all others
             const uint32_t bar = bar0 + 8u * i;
-            const uint32_t count = bar == p_full(0) || bar == p_full(1) || bar >= p_half(0) ? 4 : bar >= merge_full ? 8 : 1;
+            uint32_t count = bar == p_full(0) || bar == p_full(1) || bar >= p_half(0) ? 4 : bar >= merge_full ? 8 : 1;
+            if constexpr (FOUR) {  // stages, and codes read: by the warps that widen; a tile of queries read: by the softmax and products
+                if (bar < empty_bar(0) || bar >= code_empty(0)) count = kWidenWarps;
+                if (bar >= tile_full(0) && bar < code_empty(0)) count = bar == tile_empty(0) || bar == tile_empty(1) ? kSoftmaxWarps + 1 : 1;
+            }
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -129,7 +172,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
     }
-    if (tid < 3 * 32 && lane == 0)
+    if (!FOUR && tid < 3 * 32 && lane == 0)
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(warp == 0 ? &qmap_few : warp == 1 ? &kmap : &vmap)) : "memory");
     fence_before();
     __syncthreads();
@@ -145,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // then cost little power, which the clock of a call bound by HBM depends on (64 tokens over 8000, call after call at
     // 1000 W: 247 -> 227 us).
     if (run[1].first - run[0].first >= 64) {
-        for (int i = tid; i < kTileBytes / 16; i += kThreads) reinterpret_cast<uint4 *>(smem_raw)[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = tid; i < kTileBytes / 16; i += kAll) reinterpret_cast<uint4 *>(smem_raw)[i] = make_uint4(0u, 0u, 0u, 0u);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncthreads();
     }
@@ -156,6 +199,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     Segment g;
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax: thread = row of the slot's row tile
+        if (FOUR) asm volatile("setmaxnreg.inc.sync.aligned.u32 " PCG_SOFTMAX_REGISTERS ";");
+        uint32_t q_used = 0, q_turn = 0;  // (4 bits) uses of the queries' tiles so far (16 bits each), the next to take
         const int slot = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t sc = s_col(slot) + lanes, oc = o_col(slot) + lanes;
@@ -169,19 +214,32 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int lim = valid ? g.len - g.n + t_row + 1 : 0x7fffffff;  // padding rows never ask for masking
             const bool warp_valid = __any_sync(0xffffffffu, valid);
             const int first = g.two ? 0 : slot, step = g.two ? 1 : 2;
+            float by_score = a.scale_log2;
+            if constexpr (FOUR) {
+                const uint32_t tile = g.two ? slot : q_turn, other = tile ^ 1;
+                ok = __all_sync(0xffffffffu, wait_on(tile_full(tile), q_used >> (16 * tile) & 1, failed));
+                if (!ok) break;
+                by_score = valid ? q_by[tile][row] : 0.f;
+                __syncwarp();
+                if (lane == 0) bar_arrive(tile_empty(tile));
+                if (g.two && lane == 0) bar_arrive(tile_empty(other));  // (the other slot's: read there)
+                q_used += g.two ? 0x10001u : 1u << (16 * tile);
+                q_used &= 0xff00ffu;
+                if (!g.two) q_turn ^= 1;
+            }
             float m = kNegInf, l = 0.f;
             bool bad = false;
             for (int t = first; t < g.nt; t += step, ++sn) {
-                ok = __all_sync(0xffffffffu, bar_wait(s_full(slot), sn & 1, failed));
+                ok = __all_sync(0xffffffffu, wait_on(s_full(slot), sn & 1, failed));
                 if (!ok) break;
                 fence_after();
                 const int keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
-                if (t == g.nt - 1 && k0 + keys > g.len && (!g.two || slot == 0)) {
+                if (!FOUR && t == g.nt - 1 && k0 + keys > g.len && (!g.two || slot == 0)) {
                     // Values behind the sequence's last token may hold anything, and 0 * NaN is NaN: they are zeroed
                     // where they lie.  This stage is the last of the part; the slot's weights are announced after it, and
                     // slot 1's product comes behind slot 0's.
                     const uint32_t i = loads + (g.two ? 2 * g.nt : g.nt) - 1;
-                    ok = __all_sync(0xffffffffu, bar_wait(full_bar(i % S), (i / S) & 1, failed));
+                    ok = __all_sync(0xffffffffu, wait_on(full_bar(i % S), (i / S) & 1, failed));
                     if (!ok) break;
                     if (row < keys && k0 + row >= g.len) {
                         const uint32_t at = ring + (i % S) * kTileBytes + (g.two ? 0 : kTileBytes / 2) + row * 128;
@@ -222,26 +280,38 @@ __global__ void __launch_bounds__(kThreads, 1)
                         for (; c < keys; c += 16) tmem_st16(sc + c, x);
                         tmem_wait_st();
                     }
-                    auto take_max = [&](const uint32_t (&x)[64]) {
+                    auto take_max = [&](const auto &x) {
+                        constexpr int kCount = (int)std::extent<typename std::remove_reference<decltype(x)>::type>::value;
 #pragma unroll
-                        for (int c = 0; c < 64; c += 2)
+                        for (int c = 0; c < kCount; c += 2)
                             top[(c >> 1) & 3] = max3_nan(top[(c >> 1) & 3], __uint_as_float(x[c]), __uint_as_float(x[c + 1]));
                     };
                     tmem_ld32(sc, v);
                     tmem_ld32(sc + 32, v + 32);
                     if (g.two) {
-                        uint32_t u[64];
-                        tmem_ld32(sc + 64, u);
-                        tmem_ld32(sc + 96, u + 32);
-                        tmem_wait_ld();
-                        tmem_loaded<64>(u);
-                        take_max(u);
+                        if constexpr (FOUR) {  // 32 at a time: there are fewer registers
+#pragma unroll 1
+                            for (int c = 64; c < 128; c += 32) {
+                                uint32_t u[32];
+                                tmem_ld32(sc + c, u);
+                                tmem_wait_ld();
+                                tmem_loaded<32>(u);
+                                take_max(u);
+                            }
+                        } else {
+                            uint32_t u[64];
+                            tmem_ld32(sc + 64, u);
+                            tmem_ld32(sc + 96, u + 32);
+                            tmem_wait_ld();
+                            tmem_loaded<64>(u);
+                            take_max(u);
+                        }
                     } else {
                         tmem_wait_ld();
                     }
                     tmem_loaded<64>(v);
                     take_max(v);
-                    const float mt = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * a.scale_log2;
+                    const float mt = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * by_score;
                     bad = bad || !(mt < -kNegInf);
                     // also when the first score above -inf is met; a row's reference depends on its own scores alone, and
                     // padding rows, whose scores are arbitrary, have none
@@ -265,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     // a row that has met no score above -inf yet weighs everything 0
                     const float by = !valid ? kNegInf : (m == kNegInf ? 0.f : -m) + kLift;  // (padding: 0 too)
-                    const uint64_t scale2 = pair(a.scale_log2, a.scale_log2), by2 = pair(by, by);
+                    const uint64_t scale2 = pair(by_score, by_score), by2 = pair(by, by);
                     uint64_t sum[4] = {0, 0, 0, 0};
                     // Half the keys at a time: the product with the first half's values starts while the other weights are
                     // computed.  The second half's scores are read again, into the registers that the first half leaves: a
@@ -278,9 +348,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                             tmem_wait_ld();
                             tmem_loaded<64>(v);
                         }
-                        weights<BF16>(v, scale2, by2, sum, p);
+                        weights<kWide>(v, scale2, by2, sum, p);
                         if (!h && g.two) tmem_ld32(sc + 64, v);
-                        weights<BF16>(v + 32, scale2, by2, sum, p + 16);
+                        weights<kWide>(v + 32, scale2, by2, sum, p + 16);
                         if (!h && g.two) tmem_ld32(sc + 96, v + 32);
                         tmem_st32(sc + h * 32, p);
                         tmem_wait_st();
@@ -307,15 +377,15 @@ __global__ void __launch_bounds__(kThreads, 1)
             // ---- end of the part
             const bool mine = first < g.nt;                    // this slot has had a key tile
             const bool shared = !g.two && g.nt > 1;            // both have, of one row tile
-            if (mine) ok = __all_sync(0xffffffffu, bar_wait(o_full(slot), on++ & 1, failed));
+            if (mine) ok = __all_sync(0xffffffffu, wait_on(o_full(slot), on++ & 1, failed));
             if (!ok) break;
             if (shared) {  // the slots join their sums, each for one half of the head dimensions
                 slot_m[slot][row] = m;
                 slot_l[slot][row] = l;
                 __syncwarp();
                 if (lane == 0) bar_arrive(merge_full);
-                ok = __all_sync(0xffffffffu, bar_wait(merge_full, mn & 1, failed)) &&
-                     __all_sync(0xffffffffu, bar_wait(o_full(slot ^ 1), on_other++ & 1, failed));
+                ok = __all_sync(0xffffffffu, wait_on(merge_full, mn & 1, failed)) &&
+                     __all_sync(0xffffffffu, wait_on(o_full(slot ^ 1), on_other++ & 1, failed));
                 if (!ok) break;
             } else if (g.two || !mine) {
                 ++on_other;
@@ -336,7 +406,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                     }
                     // a row that sees no key is 0 (below); one that sees scores of -inf alone is 0 / 0 = NaN
                     if (g.whole) {
-                        const float inv = 1.f / l;
+                        const float inv = (FOUR ? a.v_scale : 1.f) / l;
                         f0 *= inv;
                         f1 *= inv;
                     }
@@ -423,17 +493,257 @@ __global__ void __launch_bounds__(kThreads, 1)
                 if (g.two) {
                     if (lane == 0) bar_arrive(written(slot));
                     if ((warp & 3) == 0) {  // the stage is free when all four warps are through
-                        ok = __all_sync(0xffffffffu, bar_wait(written(slot), wn & 1, failed));
+                        ok = __all_sync(0xffffffffu, wait_on(written(slot), wn & 1, failed));
                         if (ok && lane == 0) bar_arrive(empty_bar(last));
                     }
                     ++wn;
                 } else if (shared) {  // the other slot has read this one's sums
                     if (lane == 0) bar_arrive(merge_done);
-                    ok = __all_sync(0xffffffffu, bar_wait(merge_done, mn++ & 1, failed));
+                    ok = __all_sync(0xffffffffu, wait_on(merge_done, mn++ & 1, failed));
                 }
             }
         }
-    } else if (warp == kSoftmaxWarps) {
+    } else if (FOUR && warp < kSoftmaxWarps + kWidenWarps) {
+        // ------------------------------------------------------------------ (4 bits) codes to tiles, by all eight warps each
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+        const int w = tid - 32 * kSoftmaxWarps;
+        uint32_t stage = 0, stage_phase = 1, unit = 0, unit_phase = 0;
+        bool ok = true;
+        auto next_unit = [&](uint32_t &u, uint32_t &phase) {
+            if (++u == U) {
+                u = 0;
+                phase ^= 1;
+            }
+        };
+        // `dims` dimensions from d0 on of key number `key` of the tile, whose page starts at `page`
+        auto widen_key = [&](uint32_t tile, int keys, uint32_t page, int key, int d0, int dims) {
+            const int tok = key & 15;
+#pragma unroll 1
+            for (int d = d0; d < d0 + dims; d += 16) {
+                uint32_t c[2], s[2], r[8];
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(page + (d >> 5) * 256 + tok * 16 + (d & 16) / 2) : "memory");
+                uint32_t one;
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(one) : "r"(page + key_scales_at(D) + tok * (D / 16) + d / 16) : "memory");
+                widen_scales(one, s);
+                const uint32_t by = __byte_perm(s[0], s[0], 0x1010);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t v[4];
+                    widen_codes(c[i], v);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) r[i * 4 + j] = mul_f16x2(v[j], by);
+                }
+                const uint32_t to = tile + (d >> 6) * (keys * 128) + key * 128;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((((d & 63) >> 3) + i) ^ (key & 7)) * 16), "r"(r[4 * i]),
+                                 "r"(r[4 * i + 1]), "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
+                                 : "memory");
+            }
+        };
+        // 16 values of dimension `dim`, of the page's tokens, `left` of which there are (scales behind them may be anything: 0)
+        auto widen_value = [&](uint32_t part, uint32_t page, int dim, int chunk, int left) {
+            uint32_t c[2], x[4], s[8], r[8];
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(page + value_codes_at(D) + dim * 8) : "memory");
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
+                         : "r"(page + value_scales_at(D) + (dim & ~15))
+                         : "memory");
+            if (left < 16) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = left - 4 * i;
+                    x[i] = n >= 4 ? x[i] : n <= 0 ? 0u : x[i] & ((1u << (8 * n)) - 1);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) widen_scales(x[i], reinterpret_cast<uint32_t(&)[2]>(s[2 * i]));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t v[4];
+                widen_codes(c[i], v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) r[i * 4 + j] = mul_f16x2(v[j], s[i * 4 + j]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part + dim * 128 + ((chunk + i) ^ (dim & 7)) * 16), "r"(r[4 * i]),
+                             "r"(r[4 * i + 1]), "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
+                             : "memory");
+        };
+        auto arrive = [&](uint32_t bar) {
+            __syncwarp();
+            if (lane == 0) bar_arrive(bar);
+        };
+        while (ok && walk.next(a, TQ, g)) {
+            const int loads = g.two ? 2 * g.nt : g.nt;
+#pragma unroll 1
+            for (int j = 0; j < loads; ++j) {
+                const int t = g.two ? j >> 1 : j, keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
+                const bool do_keys = !g.two || !(j & 1), do_values = !g.two || (j & 1);
+                ok = __all_sync(0xffffffffu, wait_on(empty_bar(stage), stage_phase, failed));
+                uint32_t u1 = unit, phase1 = unit_phase;  // the second 64 keys' codes
+                next_unit(u1, phase1);
+                ok = ok && __all_sync(0xffffffffu, wait_on(code_full(unit), unit_phase, failed));
+                if (g.two) ok = ok && __all_sync(0xffffffffu, wait_on(code_full(u1), phase1, failed));
+                if (!ok) break;
+                const uint32_t tile = ring + stage * kTileBytes, code0 = codes + unit * Z::kCodeBytes, code1 = codes + u1 * Z::kCodeBytes;
+                if (do_keys) {
+                    // two row tiles: 128 keys, half of the dimensions a thread; one: 64 keys, a quarter
+                    const int key = w & (keys - 1), dims = g.two ? D / 2 : D / 4, d0 = w / keys * dims;
+                    const uint32_t page = (key < 64 ? code0 : code1) + ((key & 63) >> 4) * page_bytes(D);
+                    if (dims >= 16) widen_key(tile, keys, page, key, d0, dims);
+                }
+                if (do_values) {
+                    // a dimension's keys, D / 256 of the tile's a thread
+                    const int dim = w & (D - 1), part_of = w / D, each = keys * D / 256;
+                    const uint32_t values = g.two ? tile : tile + kTileBytes / 2;
+#pragma unroll 1
+                    for (int k = part_of * each; k < (part_of + 1) * each; k += 16)
+                        widen_value(values + (k >> 6) * (D * 128), (k < 64 ? code0 : code1) + ((k & 63) >> 4) * page_bytes(D), dim, (k & 63) >> 3, g.len - k0 - k);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                arrive(full_bar(stage));
+                if (do_values) {  // the codes have been read
+                    if (lane == 0) bar_arrive(code_empty(unit));
+                    next_unit(unit, unit_phase);
+                    if (g.two) {
+                        if (lane == 0) bar_arrive(code_empty(unit));
+                        next_unit(unit, unit_phase);
+                    }
+                }
+                if (++stage == S) {
+                    stage = 0;
+                    stage_phase ^= 1;
+                }
+            }
+        }
+    } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps + 2) {
+        // ------------------------------------------------------------------ (4 bits) queries of the next item, rounded to float16
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+        constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 4;  // 16 bytes a lane, loads in flight
+        const int sub = lane / kLanes, chunk = lane % kLanes;
+        uint32_t used = 0, turn = 0;
+        bool ok = true;
+        while (ok && walk.next(a, TQ, g)) {
+            const int tokens = min(g.n - g.pair * 2 * TQ, 2 * TQ);
+#pragma unroll 1
+            for (int x = 0; ok && x < (g.two ? 2 : 1); ++x) {
+                const uint32_t tile = g.two ? x : turn;
+                ok = __all_sync(0xffffffffu, wait_on(tile_empty(tile), (used >> (16 * tile) & 1) ^ 1, failed));
+                if (!ok) break;
+                const int t0 = g.pair * 2 * TQ + x * TQ, rows = min(tokens - x * TQ, TQ) * G;
+                const uint32_t to = qbuf + tile * kTileBytes + (chunk >> 3) * (kTile * 128);
+#pragma unroll 1
+                for (int r0 = 0; r0 < rows; r0 += kAhead * kRowsAtOnce) {
+                    uint4 v[kAhead];
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        const int r = r0 + i * kRowsAtOnce + sub, tok = r / G;
+                        v[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (r < rows)
+                            v[i] = *reinterpret_cast<const uint4 *>((const uint16_t *)a.q + ((int64_t)g.begin + t0 + tok) * a.q_stride +
+                                                                    ((int64_t)g.h * G + (r - tok * G)) * D + chunk * 8);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        const int r = r0 + i * kRowsAtOnce + sub;
+                        const float by = BF16 ? narrow_row<kLanes>(v[i]) * a.scale_log2 : a.scale_log2;
+                        if (r < rows) {
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + r * 128 + ((chunk & 7) ^ (r & 7)) * 16), "r"(v[i].x),
+                                         "r"(v[i].y), "r"(v[i].z), "r"(v[i].w)
+                                         : "memory");
+                            // (never 0: 0 times a masked score would be NaN)
+                            if (chunk == 0) q_by[tile][r] = fminf(fmaxf(by, 1.17549435e-38f), 3.40282347e38f);
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(tile_full(tile));
+                used += 1u << (16 * tile);
+                used &= 0xff00ffu;
+            }
+            if (!g.two) turn ^= 1;
+        }
+    } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps + 3) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+    } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps) {
+        // ------------------------------------------------------------------ (4 bits) copies of 64 keys' pages: a lane per copy looks its block up
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+        const int size = min(1 << a.bs_shift, 64);  // tokens of one copy
+        constexpr int kPage = page_bytes(D);
+        uint32_t it = 0, unit = 0, phase = 1;
+        bool ok = true;
+        auto units = [](const Segment &g) { return g.two ? 2 * g.nt : g.nt; };
+        auto block_of = [&](const Segment &g, int u) -> int32_t {  // of the lane's copy of unit u: -1 none there, -2 zeros
+            const int p = (g.t0 * (g.two ? 2 : 1) + u) * 64 + lane * size;
+            if (lane * size >= 64 || u >= units(g) || p >= g.len) return -1;
+            const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
+            return block < 0 || block >= a.n_blocks ? -2 : block;
+        };
+        bool have = walk.next(a, TQ, g);
+        int32_t now = -1, soon = -1;
+        if (have) {
+            now = block_of(g, 0);
+            soon = block_of(g, 1);
+        }
+        while (ok && have) {
+            Segment next;
+            int32_t next0 = -1, next1 = -1;
+            bool more = false;
+            const int count = units(g);
+#pragma unroll 1
+            for (int u = 0; u < count; ++u) {
+                const int32_t later = block_of(g, u + 2);  // its latency passes under the wait
+                ok = __all_sync(0xffffffffu, wait_on(code_empty(unit), phase, failed));
+                if (!ok) break;
+                const int p = (g.t0 * (g.two ? 2 : 1) + u) * 64 + lane * size;
+                const uint32_t dst = codes + unit * Z::kCodeBytes, bar = code_full(unit), step = (size >> 4) * kPage;
+                const uint32_t bytes = now == -1 ? 0 : (min(size, g.len - p + 15) >> 4) * kPage;
+                if (__any_sync(0xffffffffu, now == -2)) {
+                    if (now == -2)
+                        for (uint32_t i = 0; i < bytes; i += 16) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + lane * step + i), "r"(0u) : "memory");
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                const uint32_t total = __reduce_add_sync(0xffffffffu, now >= 0 ? bytes : 0u);
+                if (elect_one()) bar_expect(bar, total);
+                __syncwarp();
+                const int64_t in = (p & ((1 << a.bs_shift) - 1)) >> 4;
+                const uint8_t *src = (const uint8_t *)a.k + ((((int64_t)max(now, 0) * a.kv_heads + g.h) << (a.bs_shift - 4)) + in) * kPage;
+#pragma unroll 1
+                for (int c = 0; c < 64 / size; ++c) {
+                    const uint64_t from = __shfl_sync(0xffffffffu, (unsigned long long)(uintptr_t)src, c);
+                    const uint32_t n = __shfl_sync(0xffffffffu, now >= 0 ? bytes : 0u, c);
+                    if (n && elect_one())
+                        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + c * step), "l"(from),
+                                     "r"(n), "r"(bar)
+                                     : "memory");
+                    __syncwarp();
+                }
+                ++it;
+                if (++unit == U) {
+                    unit = 0;
+                    phase ^= 1;
+                }
+                if (u == 0) {  // the next item's first blocks, looked up while this one's tiles are on their way
+                    more = walk.next(a, TQ, next);
+                    if (more) {
+                        next0 = block_of(next, 0);
+                        next1 = block_of(next, 1);
+                    }
+                }
+                now = soon;
+                soon = later;
+            }
+            g = next;
+            have = more;
+            now = next0;
+            soon = next1;
+        }
+        if (*failed)  // giving up: copies already asked for may still be landing
+            for (uint32_t back = 1; back <= U && back <= it; ++back) bar_drain(code_full((it - back) % U), ((it - back) / U) & 1);
+    } else if (!FOUR && warp == kSoftmaxWarps) {
         // ------------------------------------------------------------------ fetch: a lane per page looks its block up, one issues
         const bool paged = a.kv_len != nullptr;
         const int box = paged ? min(1 << a.bs_shift, kHalf) : kHalf;  // rows of one copy
@@ -455,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         while (ok && have) {
             // the queries: G heads of TQ tokens at a time, which is the row tile's order
-            if (items > 0) ok = __all_sync(0xffffffffu, bar_wait(q_empty, (items - 1) & 1, failed));
+            if (items > 0) ok = __all_sync(0xffffffffu, wait_on(q_empty, (items - 1) & 1, failed));
             if (!ok) break;
             ++items;
             if (elect_one()) {
@@ -482,7 +792,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int t = g.two ? j >> 1 : j, keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
                 const uint32_t s = stage;
                 const int32_t page3 = page_of(g, t + 3);  // its latency passes under the wait
-                ok = __all_sync(0xffffffffu, bar_wait(empty_bar(s), stage_phase, failed));
+                ok = __all_sync(0xffffffffu, wait_on(empty_bar(s), stage_phase, failed));
                 if (!ok) break;
                 if (++stage == S) {
                     stage = 0;
@@ -546,6 +856,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // Head dimension 128: one lane, elected once, waits and issues, which costs the fewest instructions between two
         // products (a prompt of 8192: 525 us with the warp waiting and a lane elected for each issue, 512 so).  64: the warp
         // waits (16 prompts of up to 1500: 101 us with one lane, 95 so: its code is the smaller).
+        if (FOUR) asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
         constexpr bool kOneLane = D == 128;
         auto issuing = [&]() { return kOneLane || elect_one(); };
         auto together = [&]() {
@@ -554,12 +865,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!kOneLane || elect_one()) {
             // stages in the order of their use, weights of a slot and queries: number (of a stage) and phase of the next
             uint32_t stage = 0, stage_phase = 0, h_phase = 0, p_phase0 = 0, p_phase1 = 0, q_phase = 0;
+            uint32_t q_used = 0, q_turn = 0;  // (4 bits) as the softmax's
             bool ok = true;
             auto wait = [&](uint32_t bar, uint32_t parity) {
                 if (kOneLane)
-                    ok = ok && bar_wait_hot(bar, parity, failed);
+                    ok = ok && wait_hot(bar, parity, failed);
                 else
-                    ok = ok && __all_sync(0xffffffffu, bar_wait(bar, parity, failed));
+                    ok = ok && __all_sync(0xffffffffu, wait_on(bar, parity, failed));
             };
             auto next_stage = [&]() {  // waits for it
                 const uint32_t s = stage;
@@ -571,7 +883,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                 return s;
             };
             const uint64_t qdesc = desc_k(qbuf), kdesc = desc_k(ring);
-            const uint64_t vdesc = desc_mn(ring, kTile), vdesc_half = desc_mn(ring + kTileBytes / 2, kHalf);
+            const uint64_t vdesc = FOUR ? kdesc : desc_mn(ring, kTile), vdesc_half = FOUR ? desc_k(ring + kTileBytes / 2) : desc_mn(ring + kTileBytes / 2, kHalf);
+            constexpr uint32_t kValueStep = FOUR ? 2 : 2048 >> 4, kValueHalf = FOUR ? (D * 128) >> 4 : 4 * (2048 >> 4);  // 16 keys, 64
             constexpr uint32_t kStep = kTileBytes >> 4;
             // All by the elected lane.  A slot's scores of 128 or 64 keys; 64 keys' weights, from column col on, with their values.
             auto scores = [&](int slot, uint64_t q, uint32_t s) {
@@ -581,29 +894,51 @@ __global__ void __launch_bounds__(kThreads, 1)
                     mma_ss(s_col(slot), q + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPart + (kk & 3) * 2, kIdescQK, kk > 0);
                 mma_commit(s_full(slot));
             };
-            auto scores_half = [&](int slot, uint32_t s) {
+            auto scores_half = [&](int slot, uint32_t s, uint64_t q) {
                 constexpr int kPart = (kTile * 128) >> 4, kPartK = (kHalf * 128) >> 4;
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                    mma_ss(s_col(slot), qdesc + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPartK + (kk & 3) * 2, kIdescQKHalf,
+                    mma_ss(s_col(slot), q + (kk >> 2) * kPart + (kk & 3) * 2, kdesc + s * kStep + (kk >> 2) * kPartK + (kk & 3) * 2, kIdescQKHalf,
                            kk > 0);
                 mma_commit(s_full(slot));
             };
             auto outputs = [&](int slot, int col, uint64_t v, bool begun) {
 #pragma unroll
                 for (int kk = 0; kk < kHalf / 16; ++kk)
-                    mma_ts(o_col(slot), s_col(slot) + col + kk * 8, v + kk * (2048 >> 4), kIdescPV, begun || kk > 0);
+                    mma_ts(o_col(slot), s_col(slot) + col + kk * 8, v + kk * kValueStep, kIdescPV, begun || kk > 0);
             };
             while (ok && walk.next(a, TQ, g)) {
-                wait(q_full, q_phase);
-                q_phase ^= 1;
+                uint32_t q_tile = 0;
+                if constexpr (FOUR) {
+                    q_tile = g.two ? 0 : q_turn;
+                    wait(tile_full(q_tile), q_used >> (16 * q_tile) & 1);
+                    if (g.two) wait(tile_full(1), q_used >> 16 & 1);
+                    q_used = (q_used + (g.two ? 0x10001u : 1u << (16 * q_tile))) & 0xff00ffu;
+                    if (!g.two) q_turn ^= 1;
+                } else {
+                    wait(q_full, q_phase);
+                    q_phase ^= 1;
+                }
+                auto queries_read = [&]() {  // when the products so far are complete
+                    if constexpr (FOUR) {
+                        mma_commit(tile_empty(q_tile));
+                        if (g.two) mma_commit(tile_empty(1));
+                    } else {
+                        mma_commit(q_empty);
+                    }
+                };
                 if (g.two) {
                     const uint32_t s = next_stage();
                     if (!ok) break;
                     fence_after();
                     for (int slot = 0; slot < 2; ++slot)
                         if (issuing()) scores(slot, qdesc + slot * kStep, s);
-                    if (issuing()) mma_commit(g.nt == 1 ? q_empty : empty_bar(s));  // (the last keys' stage is the softmax's)
+                    if (issuing()) {  // (the last keys' stage is the softmax's)
+                        if (g.nt == 1)
+                            queries_read();
+                        else
+                            mma_commit(empty_bar(s));
+                    }
                     together();
                     for (int t = 0; ok && t < g.nt; ++t) {
                         const uint32_t vs = next_stage();
@@ -625,10 +960,15 @@ __global__ void __launch_bounds__(kThreads, 1)
                             if (!ok) break;
                             fence_after();
                             if (issuing()) {
-                                outputs(slot, 32, v + 4 * (2048 >> 4), true);
+                                outputs(slot, 32, v + kValueHalf, true);
                                 if (more) {
                                     scores(slot, qdesc + slot * kStep, ks);
-                                    if (slot) mma_commit(t + 2 == g.nt ? q_empty : empty_bar(ks));
+                                    if (slot) {
+                                        if (t + 2 == g.nt)
+                                            queries_read();
+                                        else
+                                            mma_commit(empty_bar(ks));
+                                    }
                                 } else {
                                     mma_commit(o_full(slot));
                                 }
@@ -672,8 +1012,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                             else
                                 mine[0] = s;
                             if (issuing()) {
-                                scores_half(slot, s);
-                                if (t == g.nt - 1) mma_commit(q_empty);
+                                scores_half(slot, s, qdesc + q_tile * kStep);
+                                if (t == g.nt - 1) queries_read();
                             }
                             together();
                         }
@@ -729,23 +1069,33 @@ int few_tokens(int G, int TQ) {
     return want < group ? group : want;
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool FOUR = false>
 cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &few, const CUtensorMap &k, const CUtensorMap &v, void *ws, cudaStream_t stream) {
     static std::atomic<uint64_t> prepared{0};  // devices whose kernel has been given its shared memory
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && (dev > 63 || !(prepared.load(std::memory_order_relaxed) >> dev & 1))) {
-        e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D>::kSmem);
+        e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16, FOUR>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D, FOUR>::kSmem);
         if (e == cudaSuccess && dev <= 63) prepared.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     if (e == cudaSuccess)
-        e = launch_behind(attention_tc_kernel<D, BF16>, dim3(kMaxBlocks), kThreads, (size_t)Sizes<D>::kSmem, stream, a, q, few, k, v, ws);
+        e = launch_behind(attention_tc_kernel<D, BF16, FOUR>, dim3(kMaxBlocks), FOUR ? kFourbitThreads : kThreads, (size_t)Sizes<D, FOUR>::kSmem, stream, a, q, few, k, v, ws);
     if (e == cudaSuccess)
-        e = launch_behind(attention_combine_kernel<D, typename std::conditional<BF16, uint16_t, f16_t>::type>, dim3(kMaxBlocks, kCombineDims, kCombineRows), kCombineThreads, 0, stream, a, ws);
+        e = launch_behind(attention_combine_kernel<D, typename std::conditional<BF16, uint16_t, f16_t>::type, FOUR>, dim3(kMaxBlocks, kCombineDims, kCombineRows), kCombineThreads, 0, stream, a, ws);
     return e;
 }
 
 }  // namespace
+
+pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *ws, cudaStream_t stream) {
+    const CUtensorMap none = {};  // (a page is copied as it lies)
+    cudaError_t e;
+    if (a.d == 128)
+        e = dtype == PCG_BF16 ? launch<128, true, true>(a, none, none, none, none, ws, stream) : launch<128, false, true>(a, none, none, none, none, ws, stream);
+    else
+        e = dtype == PCG_BF16 ? launch<64, true, true>(a, none, none, none, none, ws, stream) : launch<64, false, true>(a, none, none, none, none, ws, stream);
+    return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
+}
 
 size_t attention_work_bytes(int32_t d) {
     return (kHeadBytes + (size_t)kMaxBlocks * 2 * kPartRows * (d + 2) * 4 + 255) / 256 * 256;

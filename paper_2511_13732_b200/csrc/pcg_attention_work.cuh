@@ -267,6 +267,23 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return r;
 }
 
+// A row of bfloat16 queries, 8 a lane, LANES neighbouring lanes: rounded to float16 after a multiplication by the power of two that
+// brings the row's largest finite value to 2^14 or above, so that float16 holds it exactly down to 2^-28 of that, and to 2^-39 of it
+// below.  Returns what takes the power of two back.
+template <int LANES>
+__device__ __forceinline__ float narrow_row(uint4 &w) {
+    float x[8], most = 0.f;
+    Elem<uint16_t>::unpack(w, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]) < __int_as_float(0x7f800000) ? fabsf(x[j]) : 0.f);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    const int up = max(-113, min(120, 14 + 127 - (int)(__float_as_uint(most) >> 23)));
+    const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+    w = make_uint4(pack2<false>(x[0] * f, x[1] * f), pack2<false>(x[2] * f, x[3] * f), pack2<false>(x[4] * f, x[5] * f), pack2<false>(x[6] * f, x[7] * f));
+    return __uint_as_float((uint32_t)(127 - up) << 23);
+}
+
 // ---------------------------------------------------------------------------------------------- combine
 // N values, rounded once.
 template <int N>
@@ -290,7 +307,7 @@ __device__ __forceinline__ void store_values(f16_t *p, const float (&x)[N]) {
 // of the parts' loads, which do not depend on each other.
 constexpr int kCombineThreads = 256, kCombineDims = 4, kCombineRows = 2;
 
-template <int D, typename T>
+template <int D, typename T, bool FOUR = false>
 __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(const __grid_constant__ AttnArgs a, void *ws) {
     constexpr int N = D / (8 * kCombineDims);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -345,7 +362,7 @@ __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(cons
         }
         const int t_row = next.pair * 2 * TQ + tok;
         const bool empty = len - n + t_row + 1 <= 0;
-        const float inv = 1.f / l;  // 0 / 0 where every score was -inf
+        const float inv = (FOUR ? a.v_scale : 1.f) / l;  // 0 / 0 where every score was -inf
 #pragma unroll
         for (int i = 0; i < N; ++i) o[i] = empty ? 0.f : o[i] * inv;
         store_values((T *)a.out + (((int64_t)begin + t_row) * a.q_heads + next.h * G + in % G) * D + dims, o);

@@ -37,8 +37,19 @@ static __device__ __noinline__ bool bar_wait_on(uint32_t bar, uint32_t parity, v
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *failed) {
     return bar_poll(bar, parity) || bar_wait_on(bar, parity, failed);
 }
+// In line, its loop not unrolled: for kernels that split their registers among warps, where calls do not go.
+__device__ __forceinline__ bool bar_wait_small(uint32_t bar, uint32_t parity, volatile int *failed) {
+#pragma unroll 1
+    for (uint32_t i = 0; i < kPolls; ++i) {
+        if (bar_poll(bar, parity)) return true;
+        if (*failed) return false;
+    }
+    *failed = 1;
+    return false;
+}
 // The same without a look at the failure flag: what is in flight is waited for after a failure too.
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+#pragma unroll 1
     for (uint32_t i = 0; i < kPolls; ++i)
         if (bar_poll(bar, parity)) return;
 }
