@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             uint32_t count = bar == p_full(0) || bar == p_full(1) || bar >= p_half(0) ? 4 : bar >= merge_full ? 8 : 1;
             if constexpr (FOUR) {  // stages, and codes read: by the warps that widen; a tile of queries read: by the softmax and products
                 if (bar < empty_bar(0) || bar >= code_empty(0)) count = kWidenWarps;
-                if (bar >= tile_full(0) && bar < code_empty(0)) count = bar == tile_empty(0) || bar == tile_empty(1) ? kSoftmaxWarps + 1 : 1;
+                if (bar >= tile_full(0) && bar < code_empty(0)) count = bar < tile_empty(0) ? 2 : bar < code_full(0) ? kSoftmaxWarps + 1 : 1;
             }
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
         }
@@ -515,21 +515,28 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 phase ^= 1;
             }
         };
-        // `dims` dimensions from d0 on of key number `key` of the tile, whose page starts at `page`
-        auto widen_key = [&](uint32_t tile, int keys, uint32_t page, int key, int d0, int dims) {
+        // (each in two steps, all loads first: they are not moved ahead of stores)
+        // 16 N dimensions from d0 on of key number `key` of the tile, whose page starts at `page`
+        auto widen_key = [&](auto count, uint32_t tile, int keys, uint32_t page, int key, int d0) {
+            constexpr int N = decltype(count)::value;
             const int tok = key & 15;
-#pragma unroll 1
-            for (int d = d0; d < d0 + dims; d += 16) {
-                uint32_t c[2], s[2], r[8];
-                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(page + (d >> 5) * 256 + tok * 16 + (d & 16) / 2) : "memory");
-                uint32_t one;
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(one) : "r"(page + key_scales_at(D) + tok * (D / 16) + d / 16) : "memory");
-                widen_scales(one, s);
+            uint32_t c[N][2], one[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int d = d0 + 16 * n;
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[n][0]), "=r"(c[n][1]) : "r"(page + (d >> 5) * 256 + tok * 16 + (d & 16) / 2) : "memory");
+                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(one[n]) : "r"(page + key_scales_at(D) + tok * (D / 16) + d / 16) : "memory");
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                const int d = d0 + 16 * n;
+                uint32_t s[2], r[8];
+                widen_scales(one[n], s);
                 const uint32_t by = __byte_perm(s[0], s[0], 0x1010);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t v[4];
-                    widen_codes(c[i], v);
+                    widen_codes(c[n][i], v);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) r[i * 4 + j] = mul_f16x2(v[j], by);
                 }
@@ -541,36 +548,50 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                                  : "memory");
             }
         };
-        // 16 values of dimension `dim`, of the page's tokens, `left` of which there are (scales behind them may be anything: 0)
-        auto widen_value = [&](uint32_t part, uint32_t page, int dim, int chunk, int left) {
-            uint32_t c[2], x[4], s[8], r[8];
-            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(page + value_codes_at(D) + dim * 8) : "memory");
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                         : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
-                         : "r"(page + value_scales_at(D) + (dim & ~15))
-                         : "memory");
-            if (left < 16) {
+        // 16 N values of dimension `dim`, from token k of the unit at `code` on; `left` tokens of the unit there are (the scales of
+        // others may be anything: 0)
+        auto widen_value = [&](auto count, uint32_t part, uint32_t code, int dim, int k, int left) {
+            constexpr int N = decltype(count)::value;
+            uint32_t c[N][2], x[N][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = left - 4 * i;
-                    x[i] = n >= 4 ? x[i] : n <= 0 ? 0u : x[i] & ((1u << (8 * n)) - 1);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) widen_scales(x[i], reinterpret_cast<uint32_t(&)[2]>(s[2 * i]));
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                uint32_t v[4];
-                widen_codes(c[i], v);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) r[i * 4 + j] = mul_f16x2(v[j], s[i * 4 + j]);
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part + dim * 128 + ((chunk + i) ^ (dim & 7)) * 16), "r"(r[4 * i]),
-                             "r"(r[4 * i + 1]), "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
+            for (int n = 0; n < N; ++n) {
+                const uint32_t page = code + ((k >> 4) + n) * page_bytes(D);
+                asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[n][0]), "=r"(c[n][1]) : "r"(page + value_codes_at(D) + dim * 8) : "memory");
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(x[n][0]), "=r"(x[n][1]), "=r"(x[n][2]), "=r"(x[n][3])
+                             : "r"(page + value_scales_at(D) + (dim & ~15))
                              : "memory");
+            }
+            if (__builtin_expect(left < k + 16 * N, 0)) {
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int there = left - k - 16 * n - 4 * i;
+                        x[n][i] = there >= 4 ? x[n][i] : there <= 0 ? 0u : x[n][i] & ((1u << (8 * there)) - 1);
+                    }
+            }
+#pragma unroll
+            for (int n = 0; n < N; ++n) {
+                uint32_t s[8], r[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) widen_scales(x[n][i], reinterpret_cast<uint32_t(&)[2]>(s[2 * i]));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    uint32_t v[4];
+                    widen_codes(c[n][i], v);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) r[i * 4 + j] = mul_f16x2(v[j], s[i * 4 + j]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part + dim * 128 + (((k >> 3) + 2 * n + i) ^ (dim & 7)) * 16), "r"(r[4 * i]),
+                                 "r"(r[4 * i + 1]), "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
+                                 : "memory");
+            }
         };
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
         auto arrive = [&](uint32_t bar) {
             __syncwarp();
             if (lane == 0) bar_arrive(bar);
@@ -592,15 +613,24 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     // two row tiles: 128 keys, half of the dimensions a thread; one: 64 keys, a quarter
                     const int key = w & (keys - 1), dims = g.two ? D / 2 : D / 4, d0 = w / keys * dims;
                     const uint32_t page = (key < 64 ? code0 : code1) + ((key & 63) >> 4) * page_bytes(D);
-                    if (dims >= 16) widen_key(tile, keys, page, key, d0, dims);
+                    if (D == 64 && !g.two) {
+                        widen_key(One(), tile, keys, page, key, d0);
+                    } else {
+#pragma unroll 1
+                        for (int d = 0; d < dims; d += 32) widen_key(Two(), tile, keys, page, key, d0 + d);
+                    }
                 }
                 if (do_values) {
                     // a dimension's keys, D / 256 of the tile's a thread
-                    const int dim = w & (D - 1), part_of = w / D, each = keys * D / 256;
+                    const int dim = w & (D - 1), each = keys * D / 256, first = w / D * each;
                     const uint32_t values = g.two ? tile : tile + kTileBytes / 2;
+                    if (D == 64 && !g.two) {
+                        widen_value(One(), values, code0, dim, first, g.len - k0);
+                    } else {
 #pragma unroll 1
-                    for (int k = part_of * each; k < (part_of + 1) * each; k += 16)
-                        widen_value(values + (k >> 6) * (D * 128), (k < 64 ? code0 : code1) + ((k & 63) >> 4) * page_bytes(D), dim, (k & 63) >> 3, g.len - k0 - k);
+                        for (int k = first; k < first + each; k += 32)
+                            widen_value(Two(), values + (k >> 6) * (D * 128), k < 64 ? code0 : code1, dim, k & 63, g.len - k0 - (k & 64));
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 arrive(full_bar(stage));
@@ -618,11 +648,12 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 }
             }
         }
-    } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps + 2) {
-        // ------------------------------------------------------------------ (4 bits) queries of the next item, rounded to float16
+    } else if (FOUR && warp >= kSoftmaxWarps + kWidenWarps + 2) {
+        // ------------------------------------------------------------------ (4 bits) queries of the next item, rounded to float16, by two warps
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
-        constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 4;  // 16 bytes a lane, loads in flight
-        const int sub = lane / kLanes, chunk = lane % kLanes;
+        constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 16 / kRowsAtOnce;  // 16 bytes a lane, 16 rows of loads in flight
+        const int sub = lane / kLanes, chunk = lane % kLanes, w = warp - kSoftmaxWarps - kWidenWarps - 2;
+        const uint32_t one_of = (65536 + G - 1) / G;  // r / G is r * one_of >> 16, for r < 128
         uint32_t used = 0, turn = 0;
         bool ok = true;
         while (ok && walk.next(a, TQ, g)) {
@@ -635,11 +666,11 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 const int t0 = g.pair * 2 * TQ + x * TQ, rows = min(tokens - x * TQ, TQ) * G;
                 const uint32_t to = qbuf + tile * kTileBytes + (chunk >> 3) * (kTile * 128);
 #pragma unroll 1
-                for (int r0 = 0; r0 < rows; r0 += kAhead * kRowsAtOnce) {
+                for (int r0 = w * 16; r0 < rows; r0 += 32) {
                     uint4 v[kAhead];
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
-                        const int r = r0 + i * kRowsAtOnce + sub, tok = r / G;
+                        const int r = r0 + i * kRowsAtOnce + sub, tok = r * one_of >> 16;
                         v[i] = make_uint4(0u, 0u, 0u, 0u);
                         if (r < rows)
                             v[i] = *reinterpret_cast<const uint4 *>((const uint16_t *)a.q + ((int64_t)g.begin + t0 + tok) * a.q_stride +
@@ -666,8 +697,6 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             }
             if (!g.two) turn ^= 1;
         }
-    } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps + 3) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
     } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps) {
         // ------------------------------------------------------------------ (4 bits) copies of 64 keys' pages: a lane per copy looks its block up
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
@@ -742,7 +771,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             soon = next1;
         }
         if (*failed)  // giving up: copies already asked for may still be landing
-            for (uint32_t back = 1; back <= U && back <= it; ++back) bar_drain(code_full((it - back) % U), ((it - back) / U) & 1);
+            for (uint32_t back = 1; back <= U && back <= it; ++back) bar_drain(code_full((it - back) % max(U, 1)), ((it - back) / max(U, 1)) & 1);
     } else if (!FOUR && warp == kSoftmaxWarps) {
         // ------------------------------------------------------------------ fetch: a lane per page looks its block up, one issues
         const bool paged = a.kv_len != nullptr;
