@@ -43,11 +43,11 @@ namespace pcg {
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
 // Over the cache that holds 4.5 bits a value: 8 warps between the fetch and the products widen codes to float16 tiles, and one
-// rounds queries to float16.  640 threads are launched with 96 registers each; the softmax's 8 warps take 152, which the other
-// 12 leave by keeping 56 (8 * 32 * 152 + 12 * 32 * 56 = 60,416 of 61,440).
+// rounds queries to float16.  640 threads are launched with 96 registers each; the softmax's 8 warps take 144, which the other
+// 12 leave by keeping 64 (8 * 32 * 144 + 12 * 32 * 64 = 640 * 96).
 constexpr int kWidenWarps = 8, kFourbitThreads = 32 * (kSoftmaxWarps + kWidenWarps + 4);
-#define PCG_SOFTMAX_REGISTERS "152"
-#define PCG_OTHER_REGISTERS "56"
+#define PCG_SOFTMAX_REGISTERS "144"
+#define PCG_OTHER_REGISTERS "64"
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
 
 // 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs.  All by the special-function unit: with
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     __shared__ uint32_t tmem_slot;
     __shared__ int failed_flag;
     volatile int *failed = &failed_flag;
-    auto wait_on = [](uint32_t bar, uint32_t parity, volatile int *failed) {
+    auto wait_on = [&](uint32_t bar, uint32_t parity, volatile int *failed) {
         if constexpr (FOUR)
             return bar_wait_small(bar, parity, failed);
         else
@@ -197,6 +197,29 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     Walk walk;
     walk.start(a, run[0], run[1]);
     Segment g;
+    // 4 bits: a warp's walk rests in shared memory between items.  (In registers it drove others out to local memory, which lies
+    // behind the L2 where shared memory has the L1: some 1,600 cycles a tile.)
+    __shared__ Walk rest[FOUR ? kAll / 32 : 1];
+    if (FOUR && lane == 0) rest[warp] = walk;
+    __syncwarp();
+    auto advance = [&](Segment &g, bool alone = false) {  // alone: by one lane
+        if constexpr (FOUR) {
+            Walk w = rest[warp];
+            if (!alone) __syncwarp();
+            const bool more = w.next(a, TQ, g);
+            if (alone || lane == 0) rest[warp] = w;
+            if (!alone) __syncwarp();
+            return more;
+        } else {
+            return walk.next(a, TQ, g);
+        }
+    };
+    // 4 bits: key tiles of 128 keys for one row tile too (HBM does not bound those items, a tile's latency does), which may end
+    // behind the part's last key.
+    auto big = [](const Segment &g) { return FOUR || g.two; };
+    auto tiles = [](const Segment &g) { return FOUR && !g.two ? (g.nt + 1) >> 1 : g.nt; };
+    auto first_key = [](const Segment &g, int t) { return FOUR && !g.two ? g.t0 * kHalf + t * kTile : (g.t0 + t) * (g.two ? kTile : kHalf); };
+    auto last_key = [](const Segment &g) { return g.two ? g.len : min(g.len, (g.t0 + g.nt) * kHalf); };
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax: thread = row of the slot's row tile
         if (FOUR) asm volatile("setmaxnreg.inc.sync.aligned.u32 " PCG_SOFTMAX_REGISTERS ";");
@@ -208,10 +231,11 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         uint32_t sn = 0, on = 0, on_other = 0, mn = 0, wn = 0;  // phases met so far
         uint32_t loads = 0;                             // stages filled so far
         bool ok = true;
-        while (ok && walk.next(a, TQ, g)) {
+        while (ok && advance(g)) {
             const int t_row = g.pair * 2 * TQ + (g.two ? slot * TQ : 0) + tok;  // the row's token in its sequence
             const bool valid = tok < TQ && t_row < g.n;
             const int lim = valid ? g.len - g.n + t_row + 1 : 0x7fffffff;  // padding rows never ask for masking
+            const int nt = tiles(g), sees = FOUR && valid ? min(lim, last_key(g)) : lim;  // keys of this part that the row sees
             const bool warp_valid = __any_sync(0xffffffffu, valid);
             const int first = g.two ? 0 : slot, step = g.two ? 1 : 2;
             float by_score = a.scale_log2;
@@ -229,11 +253,11 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             }
             float m = kNegInf, l = 0.f;
             bool bad = false;
-            for (int t = first; t < g.nt; t += step, ++sn) {
+            for (int t = first; t < nt; t += step, ++sn) {
                 ok = __all_sync(0xffffffffu, wait_on(s_full(slot), sn & 1, failed));
                 if (!ok) break;
                 fence_after();
-                const int keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
+                const int keys = big(g) ? kTile : kHalf, k0 = first_key(g, t);
                 if (!FOUR && t == g.nt - 1 && k0 + keys > g.len && (!g.two || slot == 0)) {
                     // Values behind the sequence's last token may hold anything, and 0 * NaN is NaN: they are zeroed
                     // where they lie.  This stage is the last of the part; the slot's weights are announced after it, and
@@ -255,12 +279,12 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 if (warp_valid) {
                     uint32_t v[64];
                     float top[4] = {kNegInf, kNegInf, kNegInf, kNegInf};
-                    if (__any_sync(0xffffffffu, lim < k0 + keys)) {
+                    if (__any_sync(0xffffffffu, sees < k0 + keys)) {
                         // Scores of keys that a row does not see become -inf where they lie, 16 columns at a time: first those
                         // that some of the warp's rows see, then those that none does.  (In line, over all columns, this took
                         // 2,000 cycles: code that runs once an item comes at some 6 cycles an instruction, being out of the
                         // instruction cache.  So does all else that an item has once, hence the small loops below.)
-                        const int seen = max(lim - k0, 0);
+                        const int seen = max(sees - k0, 0);
                         int c = __reduce_min_sync(0xffffffffu, seen) & ~15;
                         const int none = __reduce_max_sync(0xffffffffu, valid ? seen : 0);
                         uint32_t x[16];
@@ -288,7 +312,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     };
                     tmem_ld32(sc, v);
                     tmem_ld32(sc + 32, v + 32);
-                    if (g.two) {
+                    if (big(g)) {
                         if constexpr (FOUR) {  // 32 at a time: there are fewer registers
 #pragma unroll 1
                             for (int c = 64; c < 128; c += 32) {
@@ -342,19 +366,19 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     // loop of two turns keeps the code in the instruction cache, which 128 scores in line do not fit.  (The
                     // first half's weights lie where its own scores were.)
 #pragma unroll 1
-                    for (int h = 0; h < (g.two ? 2 : 1); ++h) {
+                    for (int h = 0; h < (big(g) ? 2 : 1); ++h) {
                         uint32_t p[32];
                         if (h) {
                             tmem_wait_ld();
                             tmem_loaded<64>(v);
                         }
                         weights<kWide>(v, scale2, by2, sum, p);
-                        if (!h && g.two) tmem_ld32(sc + 64, v);
+                        if (!h && big(g)) tmem_ld32(sc + 64, v);
                         weights<kWide>(v + 32, scale2, by2, sum, p + 16);
-                        if (!h && g.two) tmem_ld32(sc + 96, v + 32);
+                        if (!h && big(g)) tmem_ld32(sc + 96, v + 32);
                         tmem_st32(sc + h * 32, p);
                         tmem_wait_st();
-                        if (!h && g.two) {
+                        if (!h && big(g)) {
                             fence_before();
                             __syncwarp();
                             if (lane == 0) bar_arrive(p_half(slot));
@@ -363,7 +387,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     float s0, s1;
                     unpair(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])), s0, s1);
                     l += s0 + s1;
-                } else if (g.two) {
+                } else if (big(g)) {
                     __syncwarp();
                     if (lane == 0) bar_arrive(p_half(slot));
                 }
@@ -373,10 +397,10 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             }
             if (bad) l = __int_as_float(0x7fffffff);  // a score of +inf or NaN
             if (!ok) break;
-            loads += g.two ? 2 * g.nt : g.nt;
+            loads += big(g) ? 2 * nt : nt;
             // ---- end of the part
-            const bool mine = first < g.nt;                    // this slot has had a key tile
-            const bool shared = !g.two && g.nt > 1;            // both have, of one row tile
+            const bool mine = first < nt;                    // this slot has had a key tile
+            const bool shared = !g.two && nt > 1;            // both have, of one row tile
             if (mine) ok = __all_sync(0xffffffffu, wait_on(o_full(slot), on++ & 1, failed));
             if (!ok) break;
             if (shared) {  // the slots join their sums, each for one half of the head dimensions
@@ -516,9 +540,9 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             }
         };
         // (each in two steps, all loads first: they are not moved ahead of stores)
+        constexpr int N = 2;
         // 16 N dimensions from d0 on of key number `key` of the tile, whose page starts at `page`
-        auto widen_key = [&](auto count, uint32_t tile, int keys, uint32_t page, int key, int d0) {
-            constexpr int N = decltype(count)::value;
+        auto widen_key = [&](uint32_t tile, uint32_t page, int key, int d0) {
             const int tok = key & 15;
             uint32_t c[N][2], one[N];
 #pragma unroll
@@ -540,7 +564,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) r[i * 4 + j] = mul_f16x2(v[j], by);
                 }
-                const uint32_t to = tile + (d >> 6) * (keys * 128) + key * 128;
+                const uint32_t to = tile + (d >> 6) * (kTile * 128) + key * 128;
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((((d & 63) >> 3) + i) ^ (key & 7)) * 16), "r"(r[4 * i]),
@@ -550,8 +574,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         };
         // 16 N values of dimension `dim`, from token k of the unit at `code` on; `left` tokens of the unit there are (the scales of
         // others may be anything: 0)
-        auto widen_value = [&](auto count, uint32_t part, uint32_t code, int dim, int k, int left) {
-            constexpr int N = decltype(count)::value;
+        auto widen_value = [&](uint32_t part, uint32_t code, int dim, int k, int left) {
             uint32_t c[N][2], x[N][4];
 #pragma unroll
             for (int n = 0; n < N; ++n) {
@@ -590,54 +613,40 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                                  : "memory");
             }
         };
-        using One = std::integral_constant<int, 1>;
-        using Two = std::integral_constant<int, 2>;
         auto arrive = [&](uint32_t bar) {
             __syncwarp();
             if (lane == 0) bar_arrive(bar);
         };
-        while (ok && walk.next(a, TQ, g)) {
-            const int loads = g.two ? 2 * g.nt : g.nt;
+        while (ok && advance(g)) {
+            const int loads = 2 * tiles(g);
 #pragma unroll 1
-            for (int j = 0; j < loads; ++j) {
-                const int t = g.two ? j >> 1 : j, keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
-                const bool do_keys = !g.two || !(j & 1), do_values = !g.two || (j & 1);
+            for (int j = 0; j < loads; ++j) {  // the keys of a tile, its values
+                const int t = j >> 1;
+                const bool second = g.two || j + 1 < g.nt || (j & 1 && j < g.nt);  // whether the tile has more than 64 keys
                 ok = __all_sync(0xffffffffu, wait_on(empty_bar(stage), stage_phase, failed));
                 uint32_t u1 = unit, phase1 = unit_phase;  // the second 64 keys' codes
                 next_unit(u1, phase1);
                 ok = ok && __all_sync(0xffffffffu, wait_on(code_full(unit), unit_phase, failed));
-                if (g.two) ok = ok && __all_sync(0xffffffffu, wait_on(code_full(u1), phase1, failed));
+                if (second) ok = ok && __all_sync(0xffffffffu, wait_on(code_full(u1), phase1, failed));
                 if (!ok) break;
                 const uint32_t tile = ring + stage * kTileBytes, code0 = codes + unit * Z::kCodeBytes, code1 = codes + u1 * Z::kCodeBytes;
-                if (do_keys) {
-                    // two row tiles: 128 keys, half of the dimensions a thread; one: 64 keys, a quarter
-                    const int key = w & (keys - 1), dims = g.two ? D / 2 : D / 4, d0 = w / keys * dims;
+                if (!(j & 1)) {  // a key, half of its dimensions a thread
+                    const int key = w & (kTile - 1), d0 = w / kTile * (D / 2);
                     const uint32_t page = (key < 64 ? code0 : code1) + ((key & 63) >> 4) * page_bytes(D);
-                    if (D == 64 && !g.two) {
-                        widen_key(One(), tile, keys, page, key, d0);
-                    } else {
 #pragma unroll 1
-                        for (int d = 0; d < dims; d += 32) widen_key(Two(), tile, keys, page, key, d0 + d);
-                    }
-                }
-                if (do_values) {
-                    // a dimension's keys, D / 256 of the tile's a thread
-                    const int dim = w & (D - 1), each = keys * D / 256, first = w / D * each;
-                    const uint32_t values = g.two ? tile : tile + kTileBytes / 2;
-                    if (D == 64 && !g.two) {
-                        widen_value(One(), values, code0, dim, first, g.len - k0);
-                    } else {
+                    for (int d = d0; d < d0 + D / 2; d += 32) widen_key(tile, page, key, d);
+                } else {  // a dimension, D / 2 of the tile's keys a thread
+                    const int dim = w & (D - 1), first = w / D * (D / 2), left = last_key(g) - first_key(g, t);
 #pragma unroll 1
-                        for (int k = first; k < first + each; k += 32)
-                            widen_value(Two(), values + (k >> 6) * (D * 128), k < 64 ? code0 : code1, dim, k & 63, g.len - k0 - (k & 64));
-                    }
+                    for (int k = first; k < first + D / 2; k += 32)
+                        widen_value(tile + (k >> 6) * (D * 128), k < 64 ? code0 : code1, dim, k & 63, left - (k & 64));
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 arrive(full_bar(stage));
-                if (do_values) {  // the codes have been read
+                if (j & 1) {  // the codes have been read
                     if (lane == 0) bar_arrive(code_empty(unit));
                     next_unit(unit, unit_phase);
-                    if (g.two) {
+                    if (second) {
                         if (lane == 0) bar_arrive(code_empty(unit));
                         next_unit(unit, unit_phase);
                     }
@@ -651,12 +660,12 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     } else if (FOUR && warp >= kSoftmaxWarps + kWidenWarps + 2) {
         // ------------------------------------------------------------------ (4 bits) queries of the next item, rounded to float16, by two warps
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
-        constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 16 / kRowsAtOnce;  // 16 bytes a lane, 16 rows of loads in flight
+        constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 4;  // 16 bytes a lane, loads in flight
         const int sub = lane / kLanes, chunk = lane % kLanes, w = warp - kSoftmaxWarps - kWidenWarps - 2;
         const uint32_t one_of = (65536 + G - 1) / G;  // r / G is r * one_of >> 16, for r < 128
         uint32_t used = 0, turn = 0;
         bool ok = true;
-        while (ok && walk.next(a, TQ, g)) {
+        while (ok && advance(g)) {
             const int tokens = min(g.n - g.pair * 2 * TQ, 2 * TQ);
 #pragma unroll 1
             for (int x = 0; ok && x < (g.two ? 2 : 1); ++x) {
@@ -666,7 +675,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 const int t0 = g.pair * 2 * TQ + x * TQ, rows = min(tokens - x * TQ, TQ) * G;
                 const uint32_t to = qbuf + tile * kTileBytes + (chunk >> 3) * (kTile * 128);
 #pragma unroll 1
-                for (int r0 = w * 16; r0 < rows; r0 += 32) {
+                for (int r0 = w * kAhead * kRowsAtOnce; r0 < rows; r0 += 2 * kAhead * kRowsAtOnce) {
                     uint4 v[kAhead];
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
@@ -711,7 +720,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
             return block < 0 || block >= a.n_blocks ? -2 : block;
         };
-        bool have = walk.next(a, TQ, g);
+        bool have = advance(g);
         int32_t now = -1, soon = -1;
         if (have) {
             now = block_of(g, 0);
@@ -756,7 +765,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     phase ^= 1;
                 }
                 if (u == 0) {  // the next item's first blocks, looked up while this one's tiles are on their way
-                    more = walk.next(a, TQ, next);
+                    more = advance(next);
                     if (more) {
                         next0 = block_of(next, 0);
                         next1 = block_of(next, 1);
@@ -785,7 +794,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
             return block < 0 || block >= a.n_blocks ? a.n_blocks : block;  // behind the tensor: reads zeros
         };
-        bool have = walk.next(a, TQ, g);
+        bool have = advance(g);
         int32_t page0 = -1, page1 = -1, page2 = -1;  // blocks of the tiles t .. t + 2
         if (have) {
             page0 = page_of(g, 0);
@@ -858,7 +867,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     c0 += 4;
                 } while (c0 < copies);
                 if (j == 0) {  // the next item's lengths and first blocks, looked up while this one's tiles are on their way
-                    have = walk.next(a, TQ, next);
+                    have = advance(next);
                     if (have) {
                         next0 = page_of(next, 0);
                         next1 = page_of(next, 1);
@@ -886,7 +895,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         // products (a prompt of 8192: 525 us with the warp waiting and a lane elected for each issue, 512 so).  64: the warp
         // waits (16 prompts of up to 1500: 101 us with one lane, 95 so: its code is the smaller).
         if (FOUR) asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
-        constexpr bool kOneLane = D == 128;
+        constexpr bool kOneLane = D == 128 && !FOUR;
         auto issuing = [&]() { return kOneLane || elect_one(); };
         auto together = [&]() {
             if (!kOneLane) __syncwarp();
@@ -936,7 +945,8 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 for (int kk = 0; kk < kHalf / 16; ++kk)
                     mma_ts(o_col(slot), s_col(slot) + col + kk * 8, v + kk * kValueStep, kIdescPV, begun || kk > 0);
             };
-            while (ok && walk.next(a, TQ, g)) {
+            uint32_t halves = 0;  // (4 bits) the slots' first halves of weights met so far
+            while (ok && advance(g, kOneLane)) {
                 uint32_t q_tile = 0;
                 if constexpr (FOUR) {
                     q_tile = g.two ? 0 : q_turn;
@@ -978,7 +988,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                         // key tile
 #pragma unroll
                         for (int slot = 0; slot < 2; ++slot) {
-                            wait(p_half(slot), h_phase);
+                            wait(p_half(slot), FOUR ? halves >> slot & 1 : h_phase);
                             if (!ok) break;
                             fence_after();
                             const uint64_t v = vdesc + vs * kStep;
@@ -1006,8 +1016,61 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                             together();
                         }
                         h_phase ^= 1;
+                        halves ^= 3;
                         p_phase0 ^= 1;
                         p_phase1 ^= 1;
+                    }
+                } else if constexpr (FOUR) {
+                    // one row tile: key tile t goes to slot t & 1, before tile t - 1's weights meet its values
+                    const int nt = tiles(g);
+                    uint32_t vs = stage, v_phase = stage_phase;
+                    auto step = [](uint32_t &s, uint32_t &phase, uint32_t by) {
+                        if ((s += by) >= S) {
+                            s -= S;
+                            phase ^= 1;
+                        }
+                    };
+                    step(vs, v_phase, 1);
+                    for (int t = 0; ok && t <= nt; ++t) {
+                        if (t < nt) {
+                            const int slot = t & 1;
+                            wait(full_bar(stage), stage_phase);
+                            if (!ok) break;
+                            fence_after();
+                            // (the slot's scores before have been read, and their weights used: those products were issued first)
+                            if (issuing()) {
+                                scores(slot, qdesc + q_tile * kStep, stage);
+                                mma_commit(empty_bar(stage));
+                                if (t == nt - 1) queries_read();
+                            }
+                            together();
+                            step(stage, stage_phase, 2);
+                        }
+                        if (t > 0) {
+                            const int slot = (t - 1) & 1;
+                            wait(full_bar(vs), v_phase);
+                            wait(p_half(slot), halves >> slot & 1);
+                            if (!ok) break;
+                            fence_after();
+                            const uint64_t v = vdesc + vs * kStep;
+                            if (issuing()) outputs(slot, 0, v, t > 2);
+                            together();
+                            wait(p_full(slot), slot ? p_phase1 : p_phase0);
+                            if (!ok) break;
+                            fence_after();
+                            if (issuing()) {
+                                outputs(slot, 32, v + kValueHalf, true);
+                                mma_commit(empty_bar(vs));
+                                if (t - 1 + 2 >= nt) mma_commit(o_full(slot));
+                            }
+                            together();
+                            halves ^= 1u << slot;
+                            if (slot)
+                                p_phase1 ^= 1;
+                            else
+                                p_phase0 ^= 1;
+                            step(vs, v_phase, 2);
+                        }
                     }
                 } else {
                     uint32_t mine[2] = {0, 0};  // the stages of the slots' key tiles
