@@ -14,7 +14,7 @@ struct Eight {
     uint4 r[sizeof(T) / 2];
     __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[i] = reinterpret_cast<const uint4 *>(p)[i];
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) r[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);  // (read once)
     }
     __device__ __forceinline__ void store(T *p) const {
 #pragma unroll
@@ -106,20 +106,38 @@ struct RotaryArgs {
 };
 
 // A block is a row.  Its heads are cut into units of 8 pairs (16 elements); a thread keeps one unit's angles in registers and
-// takes that unit of head after head, two heads at a time (their loads are in flight together).  With `keys` also the keys, to
-// the cache and k_out, and the values, which are copied.
+// takes that unit of head after head, three heads at a time.  The first three and the first of its values are asked for
+// before the row's position is known, which says whether they are needed and where the angles lie.  With `keys` also the
+// keys, to the cache and k_out, and the values, which are copied.
 // What bounds it: HBM -- 2 (q_heads + 2 kv_heads) head_dim elements a row.
-constexpr int kRotaryThreads = 128;
+constexpr int kRotaryThreads = 128, kHeadsAtOnce = 3;
 
 template <typename T>
 __device__ __forceinline__ void rotary_row(const RotaryArgs &a, int64_t r, bool keys) {
     const int pos = a.positions[r];
-    if (pos < 0) return;
     const int64_t slot = keys ? a.slots[r] : -1;
     const bool held = slot >= 0 && slot < a.n_slots;
     const int tid = threadIdx.x, d = a.d, dim = a.turn.dim, heads = a.q_heads + (keys ? a.kv_heads : 0);
+    const T *q = (const T *)a.q + r * a.q_stride, *k = (const T *)a.k + r * a.k_stride, *v = (const T *)a.v + r * a.v_stride;
+    auto get = [&](int h, int o, Eight<T> &x) { x.load(h < a.q_heads ? q + h * d + o : k + (h - a.q_heads) * d + o); };
+    const int nu = dim / 16, step = kRotaryThreads / nu;  // units of a head; heads side by side
+    const bool adjacent = a.turn.interleaved, turning = tid < step * nu;
+    const int u = tid % nu, o1 = adjacent ? 16 * u : 8 * u, o2 = adjacent ? o1 + 8 : dim / 2 + o1;
+    int h = turning ? tid / nu : heads;
+    Eight<T> r1[kHeadsAtOnce], r2[kHeadsAtOnce], v0;
+    auto ask = [&]() {
+#pragma unroll
+        for (int i = 0; i < kHeadsAtOnce; ++i)
+            if (h + i * step < heads) {
+                get(h + i * step, o1, r1[i]);
+                get(h + i * step, o2, r2[i]);
+            }
+    };
+    const int vecs = keys ? a.kv_heads * (d / 8) : 0;
+    ask();
+    if (tid < vecs) v0.load(v + tid * 8);
+    if (pos < 0) return;
     const int64_t at = held ? (((slot >> a.bs_shift) * a.kv_heads) << a.bs_shift) + (slot & ((1 << a.bs_shift) - 1)) : 0;
-    const T *q = (const T *)a.q + r * a.q_stride, *k = (const T *)a.k + r * a.k_stride;
     T *qo = (T *)a.q_out + r * a.q_out_stride, *ko = a.k_out ? (T *)a.k_out + r * a.k_out_stride : nullptr;
     // a head's rows in the cache are 1 << bs_shift apart
     auto cached = [&](void *cache, int h) { return (T *)cache + (at + ((int64_t)h << a.bs_shift)) * d; };
@@ -131,25 +149,12 @@ __device__ __forceinline__ void rotary_row(const RotaryArgs &a, int64_t r, bool 
             if (ko) x.store(ko + (h - a.q_heads) * d + o);
         }
     };
-    auto get = [&](int h, int o, Eight<T> &x) { x.load(h < a.q_heads ? q + h * d + o : k + (h - a.q_heads) * d + o); };
-
-    const int nu = dim / 16, step = kRotaryThreads / nu;  // units of a head; heads side by side
-    if (tid < step * nu) {
-        const int u = tid % nu;
-        const bool adjacent = a.turn.interleaved;
-        const int o1 = adjacent ? 16 * u : 8 * u, o2 = adjacent ? o1 + 8 : dim / 2 + o1;
-        Eight<T> r1[2], r2[2];
+    if (h < heads) {
         float c[8], s[8];
         load_angles<8>(a.turn, pos, 8 * u, c, s);
-        for (int h = tid / nu; h < heads; h += 2 * step) {
+        while (true) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (h + i * step < heads) {
-                    get(h + i * step, o1, r1[i]);
-                    get(h + i * step, o2, r2[i]);
-                }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < kHeadsAtOnce; ++i)
                 if (h + i * step < heads) {
                     float x1[8], x2[8];
                     r1[i].widen(x1);
@@ -160,54 +165,67 @@ __device__ __forceinline__ void rotary_row(const RotaryArgs &a, int64_t r, bool 
                     put(h + i * step, o1, r1[i]);
                     put(h + i * step, o2, r2[i]);
                 }
+            h += kHeadsAtOnce * step;
+            if (h >= heads) break;
+            ask();
         }
     }
-    const int rest = (d - dim) / 8;
-    for (int i = tid; i < heads * rest; i += kRotaryThreads) {
-        const int h = i / rest, o = dim + (i - h * rest) * 8;
-        Eight<T> x;
-        get(h, o, x);
-        put(h, o, x);
+    if (dim < d) {
+        const int rest = (d - dim) / 8;
+        for (int i = tid; i < heads * rest; i += kRotaryThreads) {
+            const int h = i / rest, o = dim + (i - h * rest) * 8;
+            Eight<T> x;
+            get(h, o, x);
+            put(h, o, x);
+        }
     }
     if (held) {
-        const T *v = (const T *)a.v + r * a.v_stride;
-        for (int i = tid; i < a.kv_heads * (d / 8); i += kRotaryThreads) {
+        for (int i = tid; i < vecs; i += kRotaryThreads) {
             const int h = i / (d / 8), o = (i - h * (d / 8)) * 8;
-            Eight<T> x;
-            x.load(v + i * 8);
-            x.store(cached(a.vc, h) + o);
+            if (i != tid) v0.load(v + i * 8);
+            v0.store(cached(a.vc, h) + o);
         }
     }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kRotaryThreads) cache_append_rotary_kernel(const __grid_constant__ RotaryArgs a) {
+__global__ void __launch_bounds__(kRotaryThreads, sizeof(T) == 2 ? 8 : 4) cache_append_rotary_kernel(const __grid_constant__ RotaryArgs a) {
     rotary_row<T>(a, blockIdx.x, true);
 }
 
 // ---------------------------------------------------------------------------------------------- 4 bits
-// 16 dimensions: their codes (dimension i in nibble i), the scale, and the float32 factor of a code's value.
-__device__ __forceinline__ void quantise(const float (&x)[16], float g, uint32_t (&code)[2], uint32_t &scale, float &by) {
+// 16 dimensions: their codes (dimension i in nibble i) and the scale.
+__device__ __forceinline__ void quantise(float (&x)[16], float g, uint32_t (&code)[2], uint32_t &scale) {
     float m = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(x[i])));
+    for (int i = 0; i < 16; i += 2) asm("max.NaN.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(fabsf(x[i])), "f"(fabsf(x[i + 1])));
     uint16_t s8;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s8) : "f"(0.f), "f"(__fdiv_rn(m, __fmul_rn(6.f, g))));
     scale = s8 & 0xffu;
-    by = __fmul_rn(widen_scale(scale), g);
-    const bool none = scale == 0;
+    const float by = __fmul_rn(widen_scale(scale), g), inverse = __frcp_rn(by);
+    if (m > 16.f * by) {  // a scale that ends at its largest value: beyond 16 codes do so too
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = fminf(fmaxf(x[i], -16.f * by), 16.f * by);
+    }
+    const uint32_t some = scale == 0 ? 0u : 0xffffffffu;  // a scale of 0 holds zeros
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         float y[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = none ? 0.f : __fdiv_rn(x[8 * j + i], by);
+        for (int i = 0; i < 8; ++i) {
+            // x / by, as rounded as a division's: a product with the rounded reciprocal, and its remainder (exact in one fma) once
+            // more (Markstein's correction; the signs so that -0 stays -0).  Remainders are far from float32's least values
+            // wherever the quotient is near a border of two codes (a quarter at the least, by 2^-69 or more).
+            const float z = x[8 * j + i], q = __fmul_rn(z, inverse);
+            y[i] = __fmaf_rn(-__fmaf_rn(q, by, -z), inverse, q);
+        }
         // (each byte widened to a register of its own: packed from four 8-bit registers and unpacked again by widen_codes, the
         // upper two came out 0 with the compiler of CUDA 12.9)
         uint32_t b[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             asm("{\n\t.reg .b8 a;\n\tcvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.u32.u8 %0, a;\n\t}" : "=r"(b[i]) : "f"(y[2 * i]), "f"(y[2 * i + 1]));
-        code[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+        code[j] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410) & some;
     }
 }
 // What is held of 8 of them: code * scale is exact, its product with the cache's scale rounded to float32, then to the type.
@@ -245,7 +263,7 @@ struct FourbitArgs {
 constexpr int kFourbitThreads = kRotaryThreads;
 
 template <typename T>
-__global__ void __launch_bounds__(kFourbitThreads) cache_append_fourbit_kernel(const __grid_constant__ FourbitArgs f, int windows) {
+__global__ void __launch_bounds__(kFourbitThreads, sizeof(T) == 2 ? 8 : 4) cache_append_fourbit_kernel(const __grid_constant__ FourbitArgs f, int windows) {
     extern __shared__ __align__(16) uint8_t codes[];  // [32][d + 16]: value codes of the rows, a byte each
     __shared__ int32_t slot_of[32];
     __shared__ uint32_t begins;
@@ -302,9 +320,28 @@ __global__ void __launch_bounds__(kFourbitThreads) cache_append_fourbit_kernel(c
                 for (int e = 0; e < 8; ++e) x[j >> 1][(j & 1) * 8 + e] = y[e];
             }
             if (turned) {
-                float c[16], s[16];
-                load_angles<16>(a.turn, a.positions[r], 16 * u, c, s);
-                turn<16>(x[0], x[1], c, s, adjacent);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {  // (registers)
+                    float c[8], s[8], x1[8], x2[8];
+                    load_angles<8>(a.turn, a.positions[r], 16 * u + 8 * half, c, s);
+                    // adjacent: pairs 8 half .. of the 16 lie in one group; else across the two
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        x1[e] = adjacent ? x[half][e] : x[0][8 * half + e];
+                        x2[e] = adjacent ? x[half][8 + e] : x[1][8 * half + e];
+                    }
+                    turn<8>(x1, x2, c, s, adjacent);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (adjacent) {
+                            x[half][e] = x1[e];
+                            x[half][8 + e] = x2[e];
+                        } else {
+                            x[0][8 * half + e] = x1[e];
+                            x[1][8 * half + e] = x2[e];
+                        }
+                    }
+                }
             }
             T *out = (T *)(keys ? a.k_out : f.v_out);
             uint8_t *page = (uint8_t *)a.kc;
@@ -318,8 +355,7 @@ __global__ void __launch_bounds__(kFourbitThreads) cache_append_fourbit_kernel(c
             for (int j = 0; j < 2; ++j) {
                 const int o = j ? o2 : o1;
                 uint32_t code[2], scale;
-                float by;
-                quantise(x[j], g, code, scale, by);
+                quantise(x[j], g, code, scale);
                 if (out) {
                     T *to = out + (r * a.kv_heads + h) * d + o;
                     store_held<T>(to, code[0], scale, g);
