@@ -86,9 +86,10 @@ template <int D, bool FOUR>
 struct Sizes {
     static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
     // Ring, 160 KB: a stage holds 128 keys or their values, or 64 keys and then their values, each as D / 64 parts.
-    // (4 bits: 128 KB; the codes of 64 keys and their values lie in one of three stages before it)
-    static constexpr int kStages = FOUR ? (D == 128 ? 4 : 9) : D == 128 ? 5 : 10;
-    static constexpr int kCodeStages = FOUR ? (D == 128 ? 3 : 6) : 0, kCodeBytes = 4 * page_bytes(D);
+    // (4 bits: 96 KB; the codes of 64 keys and their values lie in one of six stages before it.  With three of those and 128 KB a
+    // copy's latency showed: 256 chunks of 17, 375 us.)
+    static constexpr int kStages = FOUR ? (D == 128 ? 3 : 7) : D == 128 ? 5 : 10;
+    static constexpr int kCodeStages = FOUR ? (D == 128 ? 6 : 12) : 0, kCodeBytes = 4 * page_bytes(D);
     static constexpr int kSmem = (2 + kStages) * kTileBytes + kCodeStages * kCodeBytes;  // 219 or 224 KB; 3 KB are left for all else
     static_assert(kSmem >= kAttnMaxB * 12, "the cut's scratch");
 };
