@@ -86,10 +86,10 @@ template <int D, bool FOUR>
 struct Sizes {
     static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
     // Ring, 160 KB: a stage holds 128 keys or their values, or 64 keys and then their values, each as D / 64 parts.
-    // (4 bits: 96 KB; the codes of 64 keys and their values lie in one of six stages before it.  With three of those and 128 KB a
-    // copy's latency showed: 256 chunks of 17, 375 us.)
+    // (4 bits: 96 KB; the codes of a tile's keys and values lie in one of three stages before it.  With half of those and 128 KB a
+    // copy's latency showed: 256 chunks of 17, 375 us, so 343.)
     static constexpr int kStages = FOUR ? (D == 128 ? 3 : 7) : D == 128 ? 5 : 10;
-    static constexpr int kCodeStages = FOUR ? (D == 128 ? 6 : 12) : 0, kCodeBytes = 4 * page_bytes(D);
+    static constexpr int kCodeStages = FOUR ? (D == 128 ? 3 : 6) : 0, kCodeBytes = 8 * page_bytes(D);
     static constexpr int kSmem = (2 + kStages) * kTileBytes + kCodeStages * kCodeBytes;  // 219 or 224 KB; 3 KB are left for all else
     static_assert(kSmem >= kAttnMaxB * 12, "the cut's scratch");
 };
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     auto p_half = [&](int s) { return q_full + 88u + 8u * s; };   // ... those of the first 64 keys
     const uint32_t merge_full = q_full + 72, merge_done = q_full + 80;  // both slots' references and sums are there, read
     // 4 bits: the queries' two tiles have their own barriers, for an item with one row tile takes one of them, in turn, and the next
-    // item's are rounded meanwhile; codes of 64 keys have landed, been read
+    // item's are rounded meanwhile; the codes of a tile have landed, been read
     auto tile_full = [&](int i) { return q_full + 120u + 8u * i; };
     auto tile_empty = [&](int i) { return q_full + 136u + 8u * i; };
     auto code_full = [&](int i) { return q_full + 152u + 8u * i; };
@@ -534,12 +534,6 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         const int w = tid - 32 * kSoftmaxWarps;
         uint32_t stage = 0, stage_phase = 1, unit = 0, unit_phase = 0;
         bool ok = true;
-        auto next_unit = [&](uint32_t &u, uint32_t &phase) {
-            if (++u == U) {
-                u = 0;
-                phase ^= 1;
-            }
-        };
         // (each in two steps, all loads first: they are not moved ahead of stores)
         constexpr int N = 2;
         // 16 N dimensions from d0 on of key number `key` of the tile, whose page starts at `page`
@@ -573,7 +567,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                                  : "memory");
             }
         };
-        // 16 N values of dimension `dim`, from token k of the unit at `code` on; `left` tokens of the unit there are (the scales of
+        // 16 N values of dimension `dim`, from token k of the tile at `code` on; `left` tokens of the tile there are (the scales of
         // others may be anything: 0)
         auto widen_value = [&](uint32_t part, uint32_t code, int dim, int k, int left) {
             uint32_t c[N][2], x[N][4];
@@ -609,7 +603,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part + dim * 128 + (((k >> 3) + 2 * n + i) ^ (dim & 7)) * 16), "r"(r[4 * i]),
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(part + dim * 128 + ((((k & 63) >> 3) + 2 * n + i) ^ (dim & 7)) * 16), "r"(r[4 * i]),
                                  "r"(r[4 * i + 1]), "r"(r[4 * i + 2]), "r"(r[4 * i + 3])
                                  : "memory");
             }
@@ -623,33 +617,26 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
 #pragma unroll 1
             for (int j = 0; j < loads; ++j) {  // the keys of a tile, its values
                 const int t = j >> 1;
-                const bool second = g.two || j + 1 < g.nt || (j & 1 && j < g.nt);  // whether the tile has more than 64 keys
                 ok = __all_sync(0xffffffffu, wait_on(empty_bar(stage), stage_phase, failed));
-                uint32_t u1 = unit, phase1 = unit_phase;  // the second 64 keys' codes
-                next_unit(u1, phase1);
                 ok = ok && __all_sync(0xffffffffu, wait_on(code_full(unit), unit_phase, failed));
-                if (second) ok = ok && __all_sync(0xffffffffu, wait_on(code_full(u1), phase1, failed));
                 if (!ok) break;
-                const uint32_t tile = ring + stage * kTileBytes, code0 = codes + unit * Z::kCodeBytes, code1 = codes + u1 * Z::kCodeBytes;
+                const uint32_t tile = ring + stage * kTileBytes, code = codes + unit * Z::kCodeBytes;
                 if (!(j & 1)) {  // a key, half of its dimensions a thread
                     const int key = w & (kTile - 1), d0 = w / kTile * (D / 2);
-                    const uint32_t page = (key < 64 ? code0 : code1) + ((key & 63) >> 4) * page_bytes(D);
 #pragma unroll 1
-                    for (int d = d0; d < d0 + D / 2; d += 32) widen_key(tile, page, key, d);
+                    for (int d = d0; d < d0 + D / 2; d += 32) widen_key(tile, code + (key >> 4) * page_bytes(D), key, d);
                 } else {  // a dimension, D / 2 of the tile's keys a thread
                     const int dim = w & (D - 1), first = w / D * (D / 2), left = last_key(g) - first_key(g, t);
 #pragma unroll 1
-                    for (int k = first; k < first + D / 2; k += 32)
-                        widen_value(tile + (k >> 6) * (D * 128), k < 64 ? code0 : code1, dim, k & 63, left - (k & 64));
+                    for (int k = first; k < first + D / 2; k += 32) widen_value(tile + (k >> 6) * (D * 128), code, dim, k, left);
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 arrive(full_bar(stage));
                 if (j & 1) {  // the codes have been read
                     if (lane == 0) bar_arrive(code_empty(unit));
-                    next_unit(unit, unit_phase);
-                    if (second) {
-                        if (lane == 0) bar_arrive(code_empty(unit));
-                        next_unit(unit, unit_phase);
+                    if (++unit == U) {
+                        unit = 0;
+                        unit_phase ^= 1;
                     }
                 }
                 if (++stage == S) {
@@ -708,16 +695,15 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             if (!g.two) turn ^= 1;
         }
     } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps) {
-        // ------------------------------------------------------------------ (4 bits) copies of 64 keys' pages: a lane per copy looks its block up
+        // ------------------------------------------------------------------ (4 bits) copies of a tile's pages: a lane per copy looks its block up
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
         const int size = min(1 << a.bs_shift, 64);  // tokens of one copy
         constexpr int kPage = page_bytes(D);
         uint32_t it = 0, unit = 0, phase = 1;
         bool ok = true;
-        auto units = [](const Segment &g) { return g.two ? 2 * g.nt : g.nt; };
-        auto block_of = [&](const Segment &g, int u) -> int32_t {  // of the lane's copy of unit u: -1 none there, -2 zeros
-            const int p = (g.t0 * (g.two ? 2 : 1) + u) * 64 + lane * size;
-            if (lane * size >= 64 || u >= units(g) || p >= g.len) return -1;
+        auto block_of = [&](const Segment &g, int t) -> int32_t {  // of the lane's copy of tile t: -1 none there, -2 zeros
+            const int p = first_key(g, t) + lane * size;
+            if (lane * size >= kTile || t >= tiles(g) || p >= last_key(g)) return -1;
             const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
             return block < 0 || block >= a.n_blocks ? -2 : block;
         };
@@ -727,33 +713,34 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             now = block_of(g, 0);
             soon = block_of(g, 1);
         }
+        const uint32_t step = (size >> 4) * kPage;
         while (ok && have) {
             Segment next;
             int32_t next0 = -1, next1 = -1;
             bool more = false;
-            const int count = units(g);
+            const int count = tiles(g);
 #pragma unroll 1
-            for (int u = 0; u < count; ++u) {
-                const int32_t later = block_of(g, u + 2);  // its latency passes under the wait
+            for (int t = 0; t < count; ++t) {
+                const int32_t later = block_of(g, t + 2);  // its latency passes under the wait
+                const int p = first_key(g, t) + lane * size;
+                const uint32_t bytes = now == -1 ? 0 : (min(size, last_key(g) - p + 15) >> 4) * kPage;
+                const uint32_t there = now >= 0 ? bytes : 0, total = __reduce_add_sync(0xffffffffu, there);
+                const int64_t in = (p & ((1 << a.bs_shift) - 1)) >> 4;
+                const uint8_t *src = (const uint8_t *)a.k + ((((int64_t)max(now, 0) * a.kv_heads + g.h) << (a.bs_shift - 4)) + in) * kPage;
+                const uint32_t dst = codes + unit * Z::kCodeBytes, bar = code_full(unit);
                 ok = __all_sync(0xffffffffu, wait_on(code_empty(unit), phase, failed));
                 if (!ok) break;
-                const int p = (g.t0 * (g.two ? 2 : 1) + u) * 64 + lane * size;
-                const uint32_t dst = codes + unit * Z::kCodeBytes, bar = code_full(unit), step = (size >> 4) * kPage;
-                const uint32_t bytes = now == -1 ? 0 : (min(size, g.len - p + 15) >> 4) * kPage;
                 if (__any_sync(0xffffffffu, now == -2)) {
                     if (now == -2)
                         for (uint32_t i = 0; i < bytes; i += 16) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + lane * step + i), "r"(0u) : "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                const uint32_t total = __reduce_add_sync(0xffffffffu, now >= 0 ? bytes : 0u);
                 if (elect_one()) bar_expect(bar, total);
                 __syncwarp();
-                const int64_t in = (p & ((1 << a.bs_shift) - 1)) >> 4;
-                const uint8_t *src = (const uint8_t *)a.k + ((((int64_t)max(now, 0) * a.kv_heads + g.h) << (a.bs_shift - 4)) + in) * kPage;
 #pragma unroll 1
-                for (int c = 0; c < 64 / size; ++c) {
+                for (int c = 0; c < kTile / size; ++c) {
                     const uint64_t from = __shfl_sync(0xffffffffu, (unsigned long long)(uintptr_t)src, c);
-                    const uint32_t n = __shfl_sync(0xffffffffu, now >= 0 ? bytes : 0u, c);
+                    const uint32_t n = __shfl_sync(0xffffffffu, there, c);
                     if (n && elect_one())
                         asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst + c * step), "l"(from),
                                      "r"(n), "r"(bar)
@@ -765,7 +752,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     unit = 0;
                     phase ^= 1;
                 }
-                if (u == 0) {  // the next item's first blocks, looked up while this one's tiles are on their way
+                if (t == 0) {  // the next item's first blocks, looked up while this one's tiles are on their way
                     more = advance(next);
                     if (more) {
                         next0 = block_of(next, 0);
