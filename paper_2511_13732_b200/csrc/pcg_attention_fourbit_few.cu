@@ -4,8 +4,9 @@
 // Each warp works alone, on 64 keys at a time, with warp-level products whose operands are widened codes straight in registers:
 //     S^T[key][row] = K[key][dim] Q^T[dim][row],   O^T[dim][row] += V^T[dim][key] P^T[key][row]
 // with 16 keys, or 16 value dimensions, to 8 rows a product.  What bounds a call is then reading the cache and widening it, and
-// no warp waits for another: on the tensor-memory path (pcg_attention_fourbit_tc.cu) four rows cost the hand-overs of five roles
-// for every 128 keys (64 tokens over up to 32,000: 440 us there, see below here).
+// no warp waits for another.  (64 single tokens of 32 query heads over up to 32,000, 128 dimensions: 247 us, 82 % of the
+// measured copy's rate; with keys on the lanes of tensor memory and 16 columns for the four rows, where five roles hand over to
+// one another for every 128 keys, 440 us.  The other path's tiles have 128 rows: from 25 rows on, or 33, it is the faster one.)
 //
 // What a lane holds of an operand is free where both sides agree, so lanes take what lies together in a page.  With g = lane / 4,
 // i = lane % 4, and a chunk of four pages of 16 keys:
@@ -34,7 +35,8 @@ namespace {
 constexpr int kChunk = 64;      // keys of a warp's turn
 constexpr float kSlack = 8.f;   // the reference may lag the maximum by a factor 2^8 before sums are scaled
 constexpr float kLift = 7.f;    // float16 weights are kept 2^7 higher, out of the range where they lose bits
-constexpr int kFewItemUnits = 2, kFewLeast = 2;
+// (joining costs little: one stream of 5 tokens over 3001 takes 21.2 us with runs of one chunk, 21.5 of two, 25.4 of three)
+constexpr int kFewItemUnits = 1, kFewLeast = 1;
 
 template <int D, int NT>
 struct Few {
@@ -452,9 +454,11 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
 }
 
 // Joins the items that several runs had a part in.  Every block lists them for itself (the heads of all runs, out of L2); a warp
-// takes a row of one, a lane D / 32 dimensions.  What bounds it is the latency of two rounds of loads: heads, then parts, which
-// do not depend on each other.  (A block for each run, most of which have nothing to join, took 14 us to come and go.)
-constexpr int kJoinThreads = 1024;
+// takes a row of one, a lane D / 32 dimensions; rows lie over all SMs first.  What bounds it is the latency of three rounds of
+// loads: heads, references, sums, of eight parts at a time.  (One stream of 5 tokens over 3001, 47 parts an item: 6 us of 21;
+// rows packed into few blocks and sums behind their references 13 of 28.  A block for each run, most of which have nothing to
+// join, took 14 us to come and go.)
+constexpr int kJoinThreads = 1024, kAtOnce = 8;  // parts whose sums are asked for together
 
 template <int D, int NT, typename T>
 __global__ void __launch_bounds__(kJoinThreads) attention_fourbit_few_join_kernel(const __grid_constant__ AttnArgs a, void *ws) {
@@ -514,7 +518,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_fourbit_few_join_kerne
     for (; mine; mine &= mine - 1) begins[before++] = (int16_t)(lo + __ffs(mine) - 1);
     __syncthreads();
     const int G = a.q_heads / a.kv_heads, TQ = Z::kRows / G;
-    for (int w = blockIdx.x * (kJoinThreads / 32) + warp; w < items * Z::kRows; w += gridDim.x * (kJoinThreads / 32)) {
+    for (int w = warp * gridDim.x + blockIdx.x; w < items * Z::kRows; w += gridDim.x * (kJoinThreads / 32)) {
         const int c = begins[w / Z::kRows], r = w % Z::kRows;
         const Run next = head->run[c + 1];
         int begin, n, len;
@@ -538,24 +542,39 @@ __global__ void __launch_bounds__(kJoinThreads) attention_fourbit_few_join_kerne
         for (int k = lane; k < parts; k += 32) m = fmaxf(m, rest[k * kStride + kM + r]);
 #pragma unroll
         for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-        float f = m0 == kNegInf ? 0.f : m0 == m ? 1.f : ex2(m0 - m);
-        float l = first[kL + r] * f, o[N];
+        auto factor = [&](float mk) { return mk == kNegInf ? 0.f : mk == m ? 1.f : ex2(mk - m); };
+        const float f0 = factor(m0);
+        float l = lane == 0 ? first[kL + r] * f0 : 0.f, o[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) o[i] = first[(int64_t)r * D + dim + i] * f;
-#pragma unroll 4
-        for (int k = 0; k < parts; ++k) {
-            const float *p = rest + k * kStride;
-            const float mk = p[kM + r];
-            f = mk == kNegInf ? 0.f : mk == m ? 1.f : ex2(mk - m);
-            l += p[kL + r] * f;
-            const float2 *v = reinterpret_cast<const float2 *>(p + (int64_t)r * D + dim);
+        for (int i = 0; i < N; ++i) o[i] = first[(int64_t)r * D + dim + i] * f0;
+#pragma unroll 1
+        for (int k0 = 0; k0 < parts; k0 += 32) {  // a part's factor and sum of weights a lane
+            const float *mine = rest + (k0 + lane) * kStride + r;
+            const bool there = k0 + lane < parts;
+            const float f = there ? factor(mine[kM]) : 0.f;
+            if (there) l += mine[kL] * f;
+#pragma unroll 1
+            for (int k = k0; k < min(k0 + 32, parts); k += kAtOnce) {
+                float2 x[kAtOnce][N / 2];
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i) {
-                const float2 x = v[i];
-                o[2 * i] += x.x * f;
-                o[2 * i + 1] += x.y * f;
+                for (int e = 0; e < kAtOnce; ++e) {
+                    const float2 *v = reinterpret_cast<const float2 *>(rest + (k + e) * kStride + (int64_t)r * D + dim);
+#pragma unroll
+                    for (int i = 0; i < N / 2; ++i) x[e][i] = k + e < parts ? v[i] : make_float2(0.f, 0.f);
+                }
+#pragma unroll
+                for (int e = 0; e < kAtOnce; ++e) {
+                    const float fe = __shfl_sync(0xffffffffu, f, k - k0 + e);
+#pragma unroll
+                    for (int i = 0; i < N / 2; ++i) {
+                        o[2 * i] += x[e][i].x * fe;
+                        o[2 * i + 1] += x[e][i].y * fe;
+                    }
+                }
             }
         }
+#pragma unroll
+        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
         const int tok = r / G, t_row = next.pair * TQ + tok;
         const bool empty = len - n + t_row + 1 <= 0;
         uint32_t *to = reinterpret_cast<uint32_t *>((T *)a.out + (((int64_t)begin + t_row) * a.q_heads + (int64_t)next.h * G + (r - tok * G)) * D + dim);
