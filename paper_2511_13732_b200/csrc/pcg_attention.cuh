@@ -29,9 +29,16 @@ pcg_status attention_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, voi
 pcg_status attention_f32(const char *who, const AttnArgs &a, void *workspace, cudaStream_t stream);
 
 // Over the cache that holds 4.5 bits a value (k: its pages): 16-bit types, head dimensions 64 and 128, attention_work_bytes(d) of
-// workspace.  Calls of few rows, `rows` of a sequence and key head on average, up to few_rows(d), have a kernel of their own.
-inline int few_rows(int d) { return d == 64 ? 32 : 24; }
-pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int rows, void *workspace, cudaStream_t stream);
+// workspace.  Calls of few rows have a kernel of their own: `few_tile` says how many rows its row tiles are to have, for n tokens
+// a sequence and G query heads a key head, 0 where the other kernel is the faster one.  (n = 4, 5 and 6, 7 and 8 of G = 4 over up
+// to 8000, 64 sequences, 8 key heads x 128: 104, 165, 192 us, and 238 to 240 with the other; x 64: 73, 107, 132, and 171 to 173.
+// Two tiles of 16 rows are faster than one of 32, whose sums no longer fit a lane's registers at head dimension 128, and three
+// slower than the other kernel.)
+inline int few_tile(int d, int64_t n, int G) {
+    if (n * G <= (d == 64 ? 32 : 24)) return (int)n * G;
+    return d == 128 && G <= 16 && n <= 2 * (16 / G) ? 16 : 0;
+}
+pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int tile_rows, void *workspace, cudaStream_t stream);
 pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream);
 
 #ifdef __CUDACC__

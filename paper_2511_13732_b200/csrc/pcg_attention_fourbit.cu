@@ -199,8 +199,8 @@ extern "C" pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_strid
     if (st != PCG_OK) return st;
     if (dtype != PCG_F32 && (a.d == 64 || a.d == 128)) {
         // how many rows a sequence has is on the GPU: their average is known here
-        const int64_t few = ((int64_t)rows + B - 1) / B * (q_heads / a.kv_heads);
-        if (few <= few_rows(a.d)) return attention_fourbit_few(who, a, dtype, (int)few, workspace, (cudaStream_t)stream);
+        const int few = few_tile(a.d, ((int64_t)rows + B - 1) / B, q_heads / a.kv_heads);
+        if (few) return attention_fourbit_few(who, a, dtype, few, workspace, (cudaStream_t)stream);
         return attention_fourbit_tc(who, a, dtype, workspace, (cudaStream_t)stream);
     }
     PCG_DISPATCH_DTYPE(dtype, launch_fourbit_simple<LogitT>(a, (cudaStream_t)stream));

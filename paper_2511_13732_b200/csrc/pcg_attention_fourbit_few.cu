@@ -1,12 +1,12 @@
-// Attention over the cache that holds 4.5 bits a value for few rows: single tokens and short drafts, up to 24 rows (32 at head
-// dimension 64) of a key head; bfloat16 and float16 queries, head dimensions 64 and 128.
+// Attention over the cache that holds 4.5 bits a value for few rows: single tokens and short drafts, up to 32 rows of a
+// key head; bfloat16 and float16 queries, head dimensions 64 and 128.
 //
 // Each warp works alone, on 64 keys at a time, with warp-level products whose operands are widened codes straight in registers:
 //     S^T[key][row] = K[key][dim] Q^T[dim][row],   O^T[dim][row] += V^T[dim][key] P^T[key][row]
 // with 16 keys, or 16 value dimensions, to 8 rows a product.  What bounds a call is then reading the cache and widening it, and
 // no warp waits for another.  (64 single tokens of 32 query heads over up to 32,000, 128 dimensions: 247 us, 82 % of the
 // measured copy's rate; with keys on the lanes of tensor memory and 16 columns for the four rows, where five roles hand over to
-// one another for every 128 keys, 440 us.  The other path's tiles have 128 rows: from 25 rows on, or 33, it is the faster one.)
+// one another for every 128 keys, 440 us.  The other path's tiles have 128 rows: beyond 32 it is the faster one.)
 //
 // What a lane holds of an operand is free where both sides agree, so lanes take what lies together in a page.  With g = lane / 4,
 // i = lane % 4, and a chunk of four pages of 16 keys:
@@ -603,22 +603,22 @@ cudaError_t launch(const AttnArgs &a, void *ws, cudaStream_t stream) {
 }
 
 template <int D, typename T>
-cudaError_t dispatch(const AttnArgs &a, int rows, void *ws, cudaStream_t stream) {
-    if (rows <= 8) return launch<D, 1, T>(a, ws, stream);
-    if (rows <= 16) return launch<D, 2, T>(a, ws, stream);
+cudaError_t dispatch(const AttnArgs &a, int tile_rows, void *ws, cudaStream_t stream) {
+    if (tile_rows <= 8) return launch<D, 1, T>(a, ws, stream);
+    if (tile_rows <= 16) return launch<D, 2, T>(a, ws, stream);
     if constexpr (D == 64)
-        if (rows > 24) return launch<D, 4, T>(a, ws, stream);
+        if (tile_rows > 24) return launch<D, 4, T>(a, ws, stream);
     return launch<D, 3, T>(a, ws, stream);
 }
 
 }  // namespace
 
-pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int rows, void *ws, cudaStream_t stream) {
+pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int tile_rows, void *ws, cudaStream_t stream) {
     cudaError_t e;
     if (a.d == 128)
-        e = dtype == PCG_BF16 ? dispatch<128, uint16_t>(a, rows, ws, stream) : dispatch<128, f16_t>(a, rows, ws, stream);
+        e = dtype == PCG_BF16 ? dispatch<128, uint16_t>(a, tile_rows, ws, stream) : dispatch<128, f16_t>(a, tile_rows, ws, stream);
     else
-        e = dtype == PCG_BF16 ? dispatch<64, uint16_t>(a, rows, ws, stream) : dispatch<64, f16_t>(a, rows, ws, stream);
+        e = dtype == PCG_BF16 ? dispatch<64, uint16_t>(a, tile_rows, ws, stream) : dispatch<64, f16_t>(a, tile_rows, ws, stream);
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
 }
 

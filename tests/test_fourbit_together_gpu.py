@@ -25,6 +25,15 @@ def test_a_single_token_among_chunks(d):
     _check(s, _run(s))
 
 
+@pytest.mark.parametrize("G,n", [(1, 25), (1, 32), (2, 16), (3, 9), (4, 7), (4, 8), (5, 5), (5, 6), (9, 3), (13, 2), (16, 2), (28, 1), (8, 4)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_around_a_tile_of_few_rows(G, n, d):
+    s = _build([n, 129, 40, 700, 64 + n], [n, n, 0, n, n], 2 * G, 2, d, 16, torch.bfloat16)
+    _check(s, _run(s))
+    s = _build([n, 129, 700, 64 + n], [n, n, n, n], 2 * G, 2, d, 64, torch.float16)
+    _check(s, _run(s))
+
+
 @pytest.mark.parametrize("G", [25, 33, 49, 100, 127, 128])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
