@@ -538,9 +538,10 @@ pcg_status pcg_cache_append_fourbit(const void *q, int64_t q_stride, int32_t q_h
 
 /*
  * pcg_cache_attention over such a cache: the same arguments and rules, with q and out of `dtype`, over the values that the
- * cache holds.  Scores, the softmax and the sums are kept in 32 bits; of the 16-bit types, head dimensions 64 and 128 with at
- * most 48 query heads a key head run on the tensor cores, where keys and values are held exactly, queries with 11 significant
- * bits at least, and the weights are rounded to 11 before they meet the values.
+ * cache holds.  Scores, the softmax and the sums are kept in 32 bits; of the 16-bit types, head dimensions 64 and 128 run on
+ * the tensor cores, where keys and values are held exactly, queries too (bfloat16's down to 2^-28 of the largest of their row
+ * and head), and the weights are rounded to 11 bits before they meet the values.  A NaN held in a value may reach rows of
+ * its own sequence that do not see it, too.
  */
 pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_stride, pcg_dtype dtype, int32_t rows, int32_t q_heads,
                                        const int32_t *row_start, const int32_t *kv_len, const int32_t *block_table, int32_t B,

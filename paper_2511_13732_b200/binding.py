@@ -194,10 +194,12 @@ def _beside(stream, dev: int):
 
 def _empty(like, shape, dtype, beside):
     """A new tensor on the device of `like`, for a call on the current stream or on the one `beside` it."""
+    if torch is None:
+        _import_torch()
     if beside is None:
+        if dtype is like.dtype and shape == like.shape:  # (0.9 us less of the host's time)
+            return torch.empty_like(like, memory_format=torch.contiguous_format)
         return like.new_empty(shape, dtype=dtype)
-    import torch
-
     with torch.cuda.stream(beside):
         t = like.new_empty(shape, dtype=dtype)
     t.record_stream(torch.cuda.current_stream(like.device))  # a caller who waits for the call may read it there
@@ -669,7 +671,8 @@ def _rotary_struct(table, interleaved: bool, dev: int) -> _Rotary:
 def _rows_out(t, name: str, shape, dtype, dev: int):
     """Stride of a given output [rows, heads, head_dim] whose heads are dense."""
     got, stride = _packed(t, name, dtype, dev)
-    _need(got == shape, f"{name} must be {tuple(shape)}")
+    if got != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}")
     return stride
 
 
@@ -728,7 +731,8 @@ def _fourbit_struct(cache, k_scale: float, v_scale: float, dev: int) -> _Fourbit
 def _held_out(t, name: str, shape, dtype, dev: int):
     if t is None:
         return None
-    _need(t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev, f"{name} must be contiguous, of k's shape, type and device")
+    if t.shape != shape or t.dtype is not dtype or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{name} must be contiguous, of k's shape, type and device")
     return t.data_ptr()
 
 

@@ -14,6 +14,7 @@ namespace pcg {
 // the warp sums the 32 weighted values with lane = head dimension, whose codes of a page are 8 bytes.  The warps'
 // running sums meet in shared memory at the end.
 // What bounds it: every key is read again for each row and each query head of its group, and products run on the FMA pipes.
+// (64 single tokens of 32 query heads over up to 2000, 8 key heads, bfloat16: 139 us for 96 dimensions, 490 for 256.)
 constexpr int kSimpleThreads = 256;
 
 template <typename T>

@@ -45,6 +45,9 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
 // Over the cache that holds 4.5 bits a value: 8 warps between the fetch and the products widen codes to float16 tiles, and one
 // rounds queries to float16.  640 threads are launched with 96 registers each; the softmax's 8 warps take 144, which the other
 // 12 leave by keeping 64 (8 * 32 * 144 + 12 * 32 * 64 = 640 * 96).
+// Measured: 2 chunks of 2048 over 16,000, 32 / 8 heads x 128, 1128 us = 1013 TFLOP/s (62 % of the measured burst); 256 chunks of
+// 17 over up to 2000, 326 us, where HBM would allow 62.  What bounds those: an item's ends (some 10,000 cycles, 14 items a block)
+// and the hand-overs of a key tile between five roles (2,900 cycles with neither codes widened nor a softmax computed, 3,800 with).
 constexpr int kWidenWarps = 8, kFourbitThreads = 32 * (kSoftmaxWarps + kWidenWarps + 4);
 #define PCG_SOFTMAX_REGISTERS "144"
 #define PCG_OTHER_REGISTERS "64"
