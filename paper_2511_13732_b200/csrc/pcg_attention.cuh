@@ -39,7 +39,7 @@ inline int few_tile(int d, int64_t n, int G) {
     return d == 128 && G <= 16 && n <= 2 * (16 / G) ? 16 : 0;
 }
 pcg_status attention_fourbit_few(const char *who, const AttnArgs &a, pcg_dtype dtype, int tile_rows, void *workspace, cudaStream_t stream);
-pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *workspace, cudaStream_t stream);
+pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, int64_t rows, void *workspace, cudaStream_t stream);
 
 #ifdef __CUDACC__
 

@@ -200,9 +200,10 @@ extern "C" pcg_status pcg_cache_attention_fourbit(const void *q, int64_t q_strid
     if (st != PCG_OK) return st;
     if (dtype != PCG_F32 && (a.d == 64 || a.d == 128)) {
         // how many rows a sequence has is on the GPU: their average is known here
-        const int few = few_tile(a.d, ((int64_t)rows + B - 1) / B, q_heads / a.kv_heads);
+        const int64_t n = ((int64_t)rows + B - 1) / B;
+        const int G = q_heads / a.kv_heads, few = few_tile(a.d, n, G);
         if (few) return attention_fourbit_few(who, a, dtype, few, workspace, (cudaStream_t)stream);
-        return attention_fourbit_tc(who, a, dtype, workspace, (cudaStream_t)stream);
+        return attention_fourbit_tc(who, a, dtype, n * G, workspace, (cudaStream_t)stream);
     }
     PCG_DISPATCH_DTYPE(dtype, launch_fourbit_simple<LogitT>(a, (cudaStream_t)stream));
     const cudaError_t e = cudaGetLastError();

@@ -49,6 +49,8 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
 // 17 over up to 2000, 326 us, where HBM would allow 62.  What bounds those: an item's ends (some 10,000 cycles, 14 items a block)
 // and the hand-overs of a key tile between five roles (2,900 cycles with neither codes widened nor a softmax computed, 3,800 with).
 constexpr int kWidenWarps = 8, kFourbitThreads = 32 * (kSoftmaxWarps + kWidenWarps + 4);
+// What an item with one row tile costs there (256 chunks of 17: 306 us with four units, 288 with six, 292 with eight).
+constexpr int kOneTileItemUnits = 6;
 #define PCG_SOFTMAX_REGISTERS "144"
 #define PCG_OTHER_REGISTERS "64"
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
@@ -100,7 +102,7 @@ struct Sizes {
 // FOUR: over the cache that holds 4.5 bits a value.  Operands are float16 whatever the queries' type: codes times scales have six
 // significant bits, bfloat16 queries are multiplied by a power of two, a row's own, that brings them into range.  Values are
 // K-major there (a dimension's keys together, as the codes are): parts of D rows of 64 keys.
-template <int D, bool BF16, bool FOUR>
+template <int D, bool BF16, bool FOUR, int P>
 __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap qmap,
                         const __grid_constant__ CUtensorMap qmap_few, const __grid_constant__ CUtensorMap kmap,
@@ -187,7 +189,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
-    cut_work(a, TQ, reinterpret_cast<int64_t *>(smem_raw), warp_units, warp_items, run);
+    cut_work<P == 1 ? kOneTileItemUnits : kItemUnits, kLeast, P>(a, TQ, reinterpret_cast<int64_t *>(smem_raw), warp_units, warp_items, run);
     // In a long run, rows of the first queries' tile that no item with one row tile loads are zero: the products of padding
     // then cost little power, which the clock of a call bound by HBM depends on (64 tokens over 8000, call after call at
     // 1000 W: 247 -> 227 us).
@@ -210,20 +212,21 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         if constexpr (FOUR) {
             Walk w = rest[warp];
             if (!alone) __syncwarp();
-            const bool more = w.next(a, TQ, g);
+            const bool more = w.next<P>(a, TQ, g);
             if (alone || lane == 0) rest[warp] = w;
             if (!alone) __syncwarp();
             return more;
         } else {
-            return walk.next(a, TQ, g);
+            return walk.next<P>(a, TQ, g);
         }
     };
     // 4 bits: key tiles of 128 keys for one row tile too (HBM does not bound those items, a tile's latency does), which may end
     // behind the part's last key.
-    auto big = [](const Segment &g) { return FOUR || g.two; };
-    auto tiles = [](const Segment &g) { return FOUR && !g.two ? (g.nt + 1) >> 1 : g.nt; };
-    auto first_key = [](const Segment &g, int t) { return FOUR && !g.two ? g.t0 * kHalf + t * kTile : (g.t0 + t) * (g.two ? kTile : kHalf); };
-    auto last_key = [](const Segment &g) { return g.two ? g.len : min(g.len, (g.t0 + g.nt) * kHalf); };
+    auto two = [](const Segment &g) { return P == 2 && g.two; };
+    auto big = [&](const Segment &g) { return FOUR || two(g); };
+    auto tiles = [&](const Segment &g) { return FOUR && !two(g) ? (g.nt + 1) >> 1 : g.nt; };
+    auto first_key = [&](const Segment &g, int t) { return FOUR && !two(g) ? g.t0 * kHalf + t * kTile : (g.t0 + t) * (two(g) ? kTile : kHalf); };
+    auto last_key = [&](const Segment &g) { return two(g) ? g.len : min(g.len, (g.t0 + g.nt) * kHalf); };
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax: thread = row of the slot's row tile
         if (FOUR) asm volatile("setmaxnreg.inc.sync.aligned.u32 " PCG_SOFTMAX_REGISTERS ";");
@@ -236,24 +239,24 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         uint32_t loads = 0;                             // stages filled so far
         bool ok = true;
         while (ok && advance(g)) {
-            const int t_row = g.pair * 2 * TQ + (g.two ? slot * TQ : 0) + tok;  // the row's token in its sequence
+            const int t_row = g.pair * P * TQ + (two(g) ? slot * TQ : 0) + tok;  // the row's token in its sequence
             const bool valid = tok < TQ && t_row < g.n;
             const int lim = valid ? g.len - g.n + t_row + 1 : 0x7fffffff;  // padding rows never ask for masking
             const int nt = tiles(g), sees = FOUR && valid ? min(lim, last_key(g)) : lim;  // keys of this part that the row sees
             const bool warp_valid = __any_sync(0xffffffffu, valid);
-            const int first = g.two ? 0 : slot, step = g.two ? 1 : 2;
+            const int first = two(g) ? 0 : slot, step = two(g) ? 1 : 2;
             float by_score = a.scale_log2;
             if constexpr (FOUR) {
-                const uint32_t tile = g.two ? slot : q_turn, other = tile ^ 1;
+                const uint32_t tile = two(g) ? slot : q_turn, other = tile ^ 1;
                 ok = __all_sync(0xffffffffu, wait_on(tile_full(tile), q_used >> (16 * tile) & 1, failed));
                 if (!ok) break;
                 by_score = valid ? q_by[tile][row] : 0.f;
                 __syncwarp();
                 if (lane == 0) bar_arrive(tile_empty(tile));
-                if (g.two && lane == 0) bar_arrive(tile_empty(other));  // (the other slot's: read there)
-                q_used += g.two ? 0x10001u : 1u << (16 * tile);
+                if (two(g) && lane == 0) bar_arrive(tile_empty(other));  // (the other slot's: read there)
+                q_used += two(g) ? 0x10001u : 1u << (16 * tile);
                 q_used &= 0xff00ffu;
-                if (!g.two) q_turn ^= 1;
+                if (!two(g)) q_turn ^= 1;
             }
             float m = kNegInf, l = 0.f;
             bool bad = false;
@@ -262,15 +265,15 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 if (!ok) break;
                 fence_after();
                 const int keys = big(g) ? kTile : kHalf, k0 = first_key(g, t);
-                if (!FOUR && t == g.nt - 1 && k0 + keys > g.len && (!g.two || slot == 0)) {
+                if (!FOUR && t == g.nt - 1 && k0 + keys > g.len && (!two(g) || slot == 0)) {
                     // Values behind the sequence's last token may hold anything, and 0 * NaN is NaN: they are zeroed
                     // where they lie.  This stage is the last of the part; the slot's weights are announced after it, and
                     // slot 1's product comes behind slot 0's.
-                    const uint32_t i = loads + (g.two ? 2 * g.nt : g.nt) - 1;
+                    const uint32_t i = loads + (two(g) ? 2 * g.nt : g.nt) - 1;
                     ok = __all_sync(0xffffffffu, wait_on(full_bar(i % S), (i / S) & 1, failed));
                     if (!ok) break;
                     if (row < keys && k0 + row >= g.len) {
-                        const uint32_t at = ring + (i % S) * kTileBytes + (g.two ? 0 : kTileBytes / 2) + row * 128;
+                        const uint32_t at = ring + (i % S) * kTileBytes + (two(g) ? 0 : kTileBytes / 2) + row * 128;
 #pragma unroll 1
                         for (int part = 0; part < kParts; ++part)
 #pragma unroll
@@ -404,7 +407,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             loads += big(g) ? 2 * nt : nt;
             // ---- end of the part
             const bool mine = first < nt;                    // this slot has had a key tile
-            const bool shared = !g.two && nt > 1;            // both have, of one row tile
+            const bool shared = !two(g) && nt > 1;            // both have, of one row tile
             if (mine) ok = __all_sync(0xffffffffu, wait_on(o_full(slot), on++ & 1, failed));
             if (!ok) break;
             if (shared) {  // the slots join their sums, each for one half of the head dimensions
@@ -415,7 +418,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 ok = __all_sync(0xffffffffu, wait_on(merge_full, mn & 1, failed)) &&
                      __all_sync(0xffffffffu, wait_on(o_full(slot ^ 1), on_other++ & 1, failed));
                 if (!ok) break;
-            } else if (g.two || !mine) {
+            } else if (two(g) || !mine) {
                 ++on_other;
             }
             // With two row tiles, outputs are staged in the item's last two stages of the ring (slot 0 in the keys', slot 1 in
@@ -438,7 +441,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                         f0 *= inv;
                         f1 *= inv;
                     }
-                    const int prow = (g.two ? slot * kTile : 0) + row;
+                    const int prow = (two(g) ? slot * kTile : 0) + row;
                     float *part = part_base(ws, blockIdx.x, g.t0 == 0 ? 1 : 0, D);
                     const uint32_t stage_row = staged + row * (D * 2);
                     const int64_t offset = valid ? (((int64_t)g.begin + t_row) * a.q_heads + g.h * G + head) * (D * 2) : -1;
@@ -467,7 +470,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
 #pragma unroll
                             for (int j = 0; j < 8; ++j)
                                 w[j] = lim <= 0 ? 0u : pack2<BF16>(__uint_as_float(o[2 * j]), __uint_as_float(o[2 * j + 1]));
-                            if (g.two) {
+                            if (two(g)) {
                                 // 16-byte chunks of the row, permuted by its number: a warp's lanes meet all banks alike
 #pragma unroll
                                 for (int i = 0; i < 2; ++i)
@@ -487,7 +490,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                         part[(size_t)D * kPartRows + prow] = m;
                         part[(size_t)(D + 1) * kPartRows + prow] = l;
                     }
-                    if (g.whole && g.two) {
+                    if (g.whole && two(g)) {
                         // whole rows to memory, 32 / (D / 8) at a time: a row a lane would touch 32 lines a store, which took
                         // 4,400 cycles a tile of head dimension 128
                         constexpr int kChunks = D / 8, kRowsAtOnce = 32 / kChunks;
@@ -518,7 +521,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 }
                 fence_before();
                 __syncwarp();
-                if (g.two) {
+                if (two(g)) {
                     if (lane == 0) bar_arrive(written(slot));
                     if ((warp & 3) == 0) {  // the stage is free when all four warps are through
                         ok = __all_sync(0xffffffffu, wait_on(written(slot), wn & 1, failed));
@@ -542,19 +545,20 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         // 16 N dimensions from d0 on of key number `key` of the tile, whose page starts at `page`
         auto widen_key = [&](uint32_t tile, uint32_t page, int key, int d0) {
             const int tok = key & 15;
-            uint32_t c[N][2], one[N];
+            uint32_t c[N][2], both;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int d = d0 + 16 * n;
                 asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(c[n][0]), "=r"(c[n][1]) : "r"(page + (d >> 5) * 256 + tok * 16 + (d & 16) / 2) : "memory");
-                asm volatile("ld.shared.u8 %0, [%1];" : "=r"(one[n]) : "r"(page + key_scales_at(D) + tok * (D / 16) + d / 16) : "memory");
             }
+            uint32_t s[2];
+            asm volatile("{\n\t.reg .u16 t;\n\tld.shared.u16 t, [%1];\n\tcvt.u32.u16 %0, t;\n\t}" : "=r"(both) : "r"(page + key_scales_at(D) + tok * (D / 16) + d0 / 16) : "memory");
+            widen_scales(both, s);
 #pragma unroll
             for (int n = 0; n < N; ++n) {
                 const int d = d0 + 16 * n;
-                uint32_t s[2], r[8];
-                widen_scales(one[n], s);
-                const uint32_t by = __byte_perm(s[0], s[0], 0x1010);
+                uint32_t r[8];
+                const uint32_t by = __byte_perm(s[0], s[0], n & 1 ? 0x3232 : 0x1010);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     uint32_t v[4];
@@ -657,13 +661,13 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         uint32_t used = 0, turn = 0;
         bool ok = true;
         while (ok && advance(g)) {
-            const int tokens = min(g.n - g.pair * 2 * TQ, 2 * TQ);
+            const int tokens = min(g.n - g.pair * P * TQ, P * TQ);
 #pragma unroll 1
-            for (int x = 0; ok && x < (g.two ? 2 : 1); ++x) {
-                const uint32_t tile = g.two ? x : turn;
+            for (int x = 0; ok && x < (two(g) ? 2 : 1); ++x) {
+                const uint32_t tile = two(g) ? x : turn;
                 ok = __all_sync(0xffffffffu, wait_on(tile_empty(tile), (used >> (16 * tile) & 1) ^ 1, failed));
                 if (!ok) break;
-                const int t0 = g.pair * 2 * TQ + x * TQ, rows = min(tokens - x * TQ, TQ) * G;
+                const int t0 = g.pair * P * TQ + x * TQ, rows = min(tokens - x * TQ, TQ) * G;
                 const uint32_t to = qbuf + tile * kTileBytes + (chunk >> 3) * (kTile * 128);
 #pragma unroll 1
                 for (int r0 = w * kAhead * kRowsAtOnce; r0 < rows; r0 += 2 * kAhead * kRowsAtOnce) {
@@ -695,7 +699,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 used += 1u << (16 * tile);
                 used &= 0xff00ffu;
             }
-            if (!g.two) turn ^= 1;
+            if (!two(g)) turn ^= 1;
         }
     } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps) {
         // ------------------------------------------------------------------ (4 bits) copies of a tile's pages: a lane per copy looks its block up
@@ -780,7 +784,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         uint32_t it = 0, stage = 0, stage_phase = 1, items = 0;  // a stage's first fill waits for nothing: parity 1 has passed
         bool ok = true;
         auto page_of = [&](const Segment &g, int t) -> int32_t {  // the block of key tile t's rows from lane * box on
-            const int p = (g.t0 + t) * (g.two ? kTile : kHalf) + lane * box;
+            const int p = (g.t0 + t) * (two(g) ? kTile : kHalf) + lane * box;
             if (!paged || lane >= 8 || t >= g.nt || p >= g.len) return -1;
             const int32_t block = a.block_table[(int64_t)g.b * a.max_blocks + (p >> a.bs_shift)];
             return block < 0 || block >= a.n_blocks ? a.n_blocks : block;  // behind the tensor: reads zeros
@@ -799,26 +803,26 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             ++items;
             if (elect_one()) {
                 // two row tiles, or the tokens of one, `few` at a time; all in one where the last copy would end behind the tile
-                const uint32_t tokens = g.n - g.pair * 2 * TQ, few_copies = (tokens + few - 1) / few;
-                const bool all = g.two || few_copies * few_rows > kTile;
-                const uint32_t rows = all ? G * TQ : few_rows, step = g.two ? kTile : few_rows, copies = g.two ? 2 : all ? 1 : few_copies;
+                const uint32_t tokens = g.n - g.pair * P * TQ, few_copies = (tokens + few - 1) / few;
+                const bool all = two(g) || few_copies * few_rows > kTile;
+                const uint32_t rows = all ? G * TQ : few_rows, step = two(g) ? kTile : few_rows, copies = two(g) ? 2 : all ? 1 : few_copies;
                 bar_expect(q_full, copies * rows * kParts * 128);
 #pragma unroll 1
                 for (uint32_t c = 0; c < copies; ++c)
 #pragma unroll
                     for (int part = 0; part < kParts; ++part)  // (the second row tile's parts lie behind the first's)
-                        tma_load(qbuf + part * (kTile * 128) + c * step * 128 * (g.two ? kParts : 1), all ? &qmap : &qmap_few, part * 64, 0,
-                                 g.h, g.begin + g.pair * 2 * TQ + c * (all ? TQ : few), q_full);
+                        tma_load(qbuf + part * (kTile * 128) + c * step * 128 * (two(g) ? kParts : 1), all ? &qmap : &qmap_few, part * 64, 0,
+                                 g.h, g.begin + g.pair * P * TQ + c * (all ? TQ : few), q_full);
             }
             __syncwarp();
             // Two row tiles: the keys of tile 0, its values, the keys of tile 1, and so on, a stage each.  One: the keys and
             // values of a tile in one stage.
             Segment next;
             int32_t next0 = -1, next1 = -1, next2 = -1;
-            const int loads = g.two ? 2 * g.nt : g.nt;
+            const int loads = two(g) ? 2 * g.nt : g.nt;
 #pragma unroll 1
             for (int j = 0; j < loads; ++j) {
-                const int t = g.two ? j >> 1 : j, keys = g.two ? kTile : kHalf, k0 = (g.t0 + t) * keys;
+                const int t = two(g) ? j >> 1 : j, keys = two(g) ? kTile : kHalf, k0 = (g.t0 + t) * keys;
                 const uint32_t s = stage;
                 const int32_t page3 = page_of(g, t + 3);  // its latency passes under the wait
                 ok = __all_sync(0xffffffffu, wait_on(empty_bar(s), stage_phase, failed));
@@ -830,7 +834,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 ++it;
                 // rows behind the sequence's pages are not fetched: their scores are masked, their values zeroed
                 const int copies = min(keys / box, (max(g.len - k0, 0) + box - 1) / box);
-                const CUtensorMap *map = g.two && (j & 1) ? &vmap : &kmap;
+                const CUtensorMap *map = two(g) && (j & 1) ? &vmap : &kmap;
                 const uint32_t bar = full_bar(s);
                 int c0 = 0;
 #pragma unroll 1
@@ -839,7 +843,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) block[c] = paged ? __shfl_sync(0xffffffffu, page0, c0 + c) : 0;
                     if (elect_one()) {
-                        if (c0 == 0) bar_expect(bar, copies * box * (g.two ? 1 : 2) * D * 2);
+                        if (c0 == 0) bar_expect(bar, copies * box * (two(g) ? 1 : 2) * D * 2);
 #pragma unroll
                         for (int c = 0; c < 4; ++c) {
                             if (c0 + c >= copies) break;
@@ -849,7 +853,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
 #pragma unroll
                             for (int part = 0; part < kParts; ++part) {
                                 tma_load(dst + part * (keys * 128), map, part * 64, c1, c2, block[c], bar);
-                                if (!g.two)
+                                if (!two(g))
                                     tma_load(dst + kTileBytes / 2 + part * (keys * 128), &vmap, part * 64, c1, c2, block[c], bar);
                             }
                         }
@@ -865,7 +869,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                         next2 = page_of(next, 2);
                     }
                 }
-                if (!g.two || (j & 1)) {
+                if (!two(g) || (j & 1)) {
                     page0 = page1;
                     page1 = page2;
                     page2 = page3;
@@ -886,7 +890,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         // products (a prompt of 8192: 525 us with the warp waiting and a lane elected for each issue, 512 so).  64: the warp
         // waits (16 prompts of up to 1500: 101 us with one lane, 95 so: its code is the smaller).
         if (FOUR) asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
-        constexpr bool kOneLane = D == 128 && !FOUR;
+        constexpr bool kOneLane = D == 128 && (!FOUR || P == 1);
         auto issuing = [&]() { return kOneLane || elect_one(); };
         auto together = [&]() {
             if (!kOneLane) __syncwarp();
@@ -940,11 +944,11 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             while (ok && advance(g, kOneLane)) {
                 uint32_t q_tile = 0;
                 if constexpr (FOUR) {
-                    q_tile = g.two ? 0 : q_turn;
+                    q_tile = two(g) ? 0 : q_turn;
                     wait(tile_full(q_tile), q_used >> (16 * q_tile) & 1);
-                    if (g.two) wait(tile_full(1), q_used >> 16 & 1);
-                    q_used = (q_used + (g.two ? 0x10001u : 1u << (16 * q_tile))) & 0xff00ffu;
-                    if (!g.two) q_turn ^= 1;
+                    if (two(g)) wait(tile_full(1), q_used >> 16 & 1);
+                    q_used = (q_used + (two(g) ? 0x10001u : 1u << (16 * q_tile))) & 0xff00ffu;
+                    if (!two(g)) q_turn ^= 1;
                 } else {
                     wait(q_full, q_phase);
                     q_phase ^= 1;
@@ -952,12 +956,12 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 auto queries_read = [&]() {  // when the products so far are complete
                     if constexpr (FOUR) {
                         mma_commit(tile_empty(q_tile));
-                        if (g.two) mma_commit(tile_empty(1));
+                        if (two(g)) mma_commit(tile_empty(1));
                     } else {
                         mma_commit(q_empty);
                     }
                 };
-                if (g.two) {
+                if (two(g)) {
                     const uint32_t s = next_stage();
                     if (!ok) break;
                     fence_after();
@@ -1152,31 +1156,36 @@ int few_tokens(int G, int TQ) {
     return want < group ? group : want;
 }
 
-template <int D, bool BF16, bool FOUR = false>
+template <int D, bool BF16, bool FOUR = false, int P = 2>
 cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &few, const CUtensorMap &k, const CUtensorMap &v, void *ws, cudaStream_t stream) {
     static std::atomic<uint64_t> prepared{0};  // devices whose kernel has been given its shared memory
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && (dev > 63 || !(prepared.load(std::memory_order_relaxed) >> dev & 1))) {
-        e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16, FOUR>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D, FOUR>::kSmem);
+        e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16, FOUR, P>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D, FOUR>::kSmem);
         if (e == cudaSuccess && dev <= 63) prepared.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     if (e == cudaSuccess)
-        e = launch_behind(attention_tc_kernel<D, BF16, FOUR>, dim3(kMaxBlocks), FOUR ? kFourbitThreads : kThreads, (size_t)Sizes<D, FOUR>::kSmem, stream, a, q, few, k, v, ws);
+        e = launch_behind(attention_tc_kernel<D, BF16, FOUR, P>, dim3(kMaxBlocks), FOUR ? kFourbitThreads : kThreads, (size_t)Sizes<D, FOUR>::kSmem, stream, a, q, few, k, v, ws);
     if (e == cudaSuccess)
-        e = launch_behind(attention_combine_kernel<D, typename std::conditional<BF16, uint16_t, f16_t>::type, FOUR>, dim3(kMaxBlocks, kCombineDims, kCombineRows), kCombineThreads, 0, stream, a, ws);
+        e = launch_behind(attention_combine_kernel<D, typename std::conditional<BF16, uint16_t, f16_t>::type, FOUR, P>, dim3(kMaxBlocks, kCombineDims, kCombineRows), kCombineThreads, 0, stream, a, ws);
     return e;
 }
 
 }  // namespace
 
-pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, void *ws, cudaStream_t stream) {
+template <int D, bool BF16>
+static cudaError_t launch_fourbit(const AttnArgs &a, int64_t rows, void *ws, cudaStream_t stream) {
     const CUtensorMap none = {};  // (a page is copied as it lies)
+    return rows <= kTile ? launch<D, BF16, true, 1>(a, none, none, none, none, ws, stream) : launch<D, BF16, true, 2>(a, none, none, none, none, ws, stream);
+}
+
+pcg_status attention_fourbit_tc(const char *who, const AttnArgs &a, pcg_dtype dtype, int64_t rows, void *ws, cudaStream_t stream) {
     cudaError_t e;
     if (a.d == 128)
-        e = dtype == PCG_BF16 ? launch<128, true, true>(a, none, none, none, none, ws, stream) : launch<128, false, true>(a, none, none, none, none, ws, stream);
+        e = dtype == PCG_BF16 ? launch_fourbit<128, true>(a, rows, ws, stream) : launch_fourbit<128, false>(a, rows, ws, stream);
     else
-        e = dtype == PCG_BF16 ? launch<64, true, true>(a, none, none, none, none, ws, stream) : launch<64, false, true>(a, none, none, none, none, ws, stream);
+        e = dtype == PCG_BF16 ? launch_fourbit<64, true>(a, rows, ws, stream) : launch_fourbit<64, false>(a, rows, ws, stream);
     return e == cudaSuccess ? PCG_OK : cuda_fail(e, who);
 }
 

@@ -307,7 +307,7 @@ __device__ __forceinline__ void store_values(f16_t *p, const float (&x)[N]) {
 // of the parts' loads, which do not depend on each other.
 constexpr int kCombineThreads = 256, kCombineDims = 4, kCombineRows = 2;
 
-template <int D, typename T, bool FOUR = false>
+template <int D, typename T, bool FOUR = false, int P = 2>
 __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(const __grid_constant__ AttnArgs a, void *ws) {
     constexpr int N = D / (8 * kCombineDims);
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -329,10 +329,10 @@ __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(cons
     const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
     int begin, n, len;
     attn_sequence(a, next.b, begin, n, len);
-    const int64_t end = next.first - next.tile + tiles_of(n, len, TQ, next.pair);
+    const int64_t end = next.first - next.tile + tiles_of<P>(n, len, TQ, next.pair);
     int last = c + 1;  // the block that ends the item
     while (last + 1 < kMaxBlocks && head->run[last + 1].first < end) ++last;
-    const int tokens = min(n - next.pair * 2 * TQ, 2 * TQ);
+    const int tokens = min(n - next.pair * P * TQ, P * TQ);
     const int rows = tokens > TQ ? kPartRows : kTile;
     // the first part lies among its block's parts that begin an item, the others among those that do not
     const float *first = part_base(ws, c, 1, D), *rest = part_base(ws, c + 1, 0, D);
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kCombineThreads) attention_combine_kernel(cons
 #pragma unroll
             for (int i = 0; i < N; ++i) o[i] += p[(dims + i) * kPartRows + r] * f;
         }
-        const int t_row = next.pair * 2 * TQ + tok;
+        const int t_row = next.pair * P * TQ + tok;
         const bool empty = len - n + t_row + 1 <= 0;
         const float inv = (FOUR ? a.v_scale : 1.f) / l;  // 0 / 0 where every score was -inf
 #pragma unroll
