@@ -42,15 +42,16 @@ namespace pcg {
 
 constexpr int kSoftmaxWarps = 8;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
-// Over the cache that holds 4.5 bits a value: 8 warps between the fetch and the products widen codes to float16 tiles, and one
-// rounds queries to float16.  640 threads are launched with 96 registers each; the softmax's 8 warps take 144, which the other
-// 12 leave by keeping 64 (8 * 32 * 144 + 12 * 32 * 64 = 640 * 96).
+// Over the cache that holds 4.5 bits a value: 8 warps between the fetch and the products round queries and widen codes to float16
+// tiles.  640 threads are launched with 96 registers each, 480 for the five warps of each quarter of an SM, whose registers are its
+// own: the softmax's two take 144, which the other three leave by keeping 64 (2 * 144 + 3 * 64 = 480).  Two of the 20 warps have
+// no part; without them, 18 would be launched with 96 as well and have less to share.
 // Measured: 2 chunks of 2048 over 16,000, 32 / 8 heads x 128, 1128 us = 1013 TFLOP/s (62 % of the measured burst); 256 chunks of
 // 17 over up to 2000, 326 us, where HBM would allow 62.  What bounds those: an item's ends (some 10,000 cycles, 14 items a block)
 // and the hand-overs of a key tile between five roles (2,900 cycles with neither codes widened nor a softmax computed, 3,800 with).
 constexpr int kWidenWarps = 8, kFourbitThreads = 32 * (kSoftmaxWarps + kWidenWarps + 4);
-// What an item with one row tile costs there (256 chunks of 17: 306 us with four units, 288 with six, 292 with eight).
-constexpr int kOneTileItemUnits = 6;
+// What an item costs there (256 chunks of 17: 306 us with four units, 288 with six, 292 with eight; 32 of 64 over 500: 76, 69, 67 with nine).
+constexpr int kFourbitItemUnits = 6;
 #define PCG_SOFTMAX_REGISTERS "144"
 #define PCG_OTHER_REGISTERS "64"
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
@@ -167,7 +168,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             uint32_t count = bar == p_full(0) || bar == p_full(1) || bar >= p_half(0) ? 4 : bar >= merge_full ? 8 : 1;
             if constexpr (FOUR) {  // stages, and codes read: by the warps that widen; a tile of queries read: by the softmax and products
                 if (bar < empty_bar(0) || bar >= code_empty(0)) count = kWidenWarps;
-                if (bar >= tile_full(0) && bar < code_empty(0)) count = bar < tile_empty(0) ? 2 : bar < code_full(0) ? kSoftmaxWarps + 1 : 1;
+                if (bar >= tile_full(0) && bar < code_empty(0)) count = bar < tile_empty(0) ? kWidenWarps : bar < code_full(0) ? kSoftmaxWarps + 1 : 1;
             }
             asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
         }
@@ -189,7 +190,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;");
     const int G = a.q_heads / a.kv_heads, TQ = kTile / G;
-    cut_work<P == 1 ? kOneTileItemUnits : kItemUnits, kLeast, P>(a, TQ, reinterpret_cast<int64_t *>(smem_raw), warp_units, warp_items, run);
+    cut_work<FOUR ? kFourbitItemUnits : kItemUnits, kLeast, P>(a, TQ, reinterpret_cast<int64_t *>(smem_raw), warp_units, warp_items, run);
     // In a long run, rows of the first queries' tile that no item with one row tile loads are zero: the products of padding
     // then cost little power, which the clock of a call bound by HBM depends on (64 tokens over 8000, call after call at
     // 1000 W: 247 -> 227 us).
@@ -619,8 +620,57 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             __syncwarp();
             if (lane == 0) bar_arrive(bar);
         };
+        uint32_t used = 0, turn = 0;  // uses of the queries' tiles so far (16 bits each), the next to take
+        // An item's queries, rounded to float16.  (Two warps of their own, an item ahead, were too slow for two row tiles, which
+        // cannot be fetched ahead, by some 20 us an item, and for short contexts; for others this costs the same.)
+        auto queries = [&](const Segment &g) {
+            constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 4;  // 16 bytes a lane, loads in flight
+            const int sub = lane / kLanes, chunk = lane % kLanes;
+            const uint32_t one_of = (65536 + G - 1) / G;  // r / G is r * one_of >> 16, for r < 128
+            const int tokens = min(g.n - g.pair * P * TQ, P * TQ);
+#pragma unroll 1
+            for (int x = 0; x < (two(g) ? 2 : 1); ++x) {
+                const uint32_t tile = two(g) ? x : turn;
+                if (!__all_sync(0xffffffffu, wait_on(tile_empty(tile), (used >> (16 * tile) & 1) ^ 1, failed))) return false;
+                const int t0 = g.pair * P * TQ + x * TQ, rows = min(tokens - x * TQ, TQ) * G;
+                const uint32_t to = qbuf + tile * kTileBytes + (chunk >> 3) * (kTile * 128);
+#pragma unroll 1
+                for (int r0 = (warp - kSoftmaxWarps) * kAhead * kRowsAtOnce; r0 < rows; r0 += kWidenWarps * kAhead * kRowsAtOnce) {
+                    uint4 v[kAhead];
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        const int r = r0 + i * kRowsAtOnce + sub, tok = r * one_of >> 16;
+                        v[i] = make_uint4(0u, 0u, 0u, 0u);
+                        if (r < rows)
+                            v[i] = *reinterpret_cast<const uint4 *>((const uint16_t *)a.q + ((int64_t)g.begin + t0 + tok) * a.q_stride +
+                                                                    ((int64_t)g.h * G + (r - tok * G)) * D + chunk * 8);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        const int r = r0 + i * kRowsAtOnce + sub;
+                        const float by = BF16 ? narrow_row<kLanes>(v[i]) * a.scale_log2 : a.scale_log2;
+                        if (r < rows) {
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + r * 128 + ((chunk & 7) ^ (r & 7)) * 16), "r"(v[i].x),
+                                         "r"(v[i].y), "r"(v[i].z), "r"(v[i].w)
+                                         : "memory");
+                            // (never 0: 0 times a masked score would be NaN)
+                            if (chunk == 0) q_by[tile][r] = fminf(fmaxf(by, 1.17549435e-38f), 3.40282347e38f);
+                        }
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) bar_arrive(tile_full(tile));
+                used += 1u << (16 * tile);
+                used &= 0xff00ffu;
+            }
+            if (!two(g)) turn ^= 1;
+            return true;
+        };
         while (ok && advance(g)) {
             const int loads = 2 * tiles(g);
+            ok = queries(g);
+            if (!ok) break;
 #pragma unroll 1
             for (int j = 0; j < loads; ++j) {  // the keys of a tile, its values
                 const int t = j >> 1;
@@ -653,54 +703,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             }
         }
     } else if (FOUR && warp >= kSoftmaxWarps + kWidenWarps + 2) {
-        // ------------------------------------------------------------------ (4 bits) queries of the next item, rounded to float16, by two warps
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
-        constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 4;  // 16 bytes a lane, loads in flight
-        const int sub = lane / kLanes, chunk = lane % kLanes, w = warp - kSoftmaxWarps - kWidenWarps - 2;
-        const uint32_t one_of = (65536 + G - 1) / G;  // r / G is r * one_of >> 16, for r < 128
-        uint32_t used = 0, turn = 0;
-        bool ok = true;
-        while (ok && advance(g)) {
-            const int tokens = min(g.n - g.pair * P * TQ, P * TQ);
-#pragma unroll 1
-            for (int x = 0; ok && x < (two(g) ? 2 : 1); ++x) {
-                const uint32_t tile = two(g) ? x : turn;
-                ok = __all_sync(0xffffffffu, wait_on(tile_empty(tile), (used >> (16 * tile) & 1) ^ 1, failed));
-                if (!ok) break;
-                const int t0 = g.pair * P * TQ + x * TQ, rows = min(tokens - x * TQ, TQ) * G;
-                const uint32_t to = qbuf + tile * kTileBytes + (chunk >> 3) * (kTile * 128);
-#pragma unroll 1
-                for (int r0 = w * kAhead * kRowsAtOnce; r0 < rows; r0 += 2 * kAhead * kRowsAtOnce) {
-                    uint4 v[kAhead];
-#pragma unroll
-                    for (int i = 0; i < kAhead; ++i) {
-                        const int r = r0 + i * kRowsAtOnce + sub, tok = r * one_of >> 16;
-                        v[i] = make_uint4(0u, 0u, 0u, 0u);
-                        if (r < rows)
-                            v[i] = *reinterpret_cast<const uint4 *>((const uint16_t *)a.q + ((int64_t)g.begin + t0 + tok) * a.q_stride +
-                                                                    ((int64_t)g.h * G + (r - tok * G)) * D + chunk * 8);
-                    }
-#pragma unroll
-                    for (int i = 0; i < kAhead; ++i) {
-                        const int r = r0 + i * kRowsAtOnce + sub;
-                        const float by = BF16 ? narrow_row<kLanes>(v[i]) * a.scale_log2 : a.scale_log2;
-                        if (r < rows) {
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + r * 128 + ((chunk & 7) ^ (r & 7)) * 16), "r"(v[i].x),
-                                         "r"(v[i].y), "r"(v[i].z), "r"(v[i].w)
-                                         : "memory");
-                            // (never 0: 0 times a masked score would be NaN)
-                            if (chunk == 0) q_by[tile][r] = fminf(fmaxf(by, 1.17549435e-38f), 3.40282347e38f);
-                        }
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) bar_arrive(tile_full(tile));
-                used += 1u << (16 * tile);
-                used &= 0xff00ffu;
-            }
-            if (!two(g)) turn ^= 1;
-        }
     } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps) {
         // ------------------------------------------------------------------ (4 bits) copies of a tile's pages: a lane per copy looks its block up
         asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
