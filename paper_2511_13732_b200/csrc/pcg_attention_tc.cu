@@ -88,15 +88,18 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
 }
 
 // ---------------------------------------------------------------------------------------------- main kernel
-template <int D, bool FOUR>
+template <int D, bool FOUR, int P>
 struct Sizes {
     static constexpr int kTileBytes = kTile * D * 2;         // a row tile or a key tile: D / 64 parts of 128 rows x 128 bytes
+    // Tiles of queries: two, one row tile each, or an item's in turn; over 4 bits and with one row tile an item one, which leaves the
+    // ring a stage more (256 chunks of 17: 292 us, so 278: the next item's queries come behind this one's last values anyway).
+    static constexpr int kQueryTiles = FOUR ? P : 2;
     // Ring, 160 KB: a stage holds 128 keys or their values, or 64 keys and then their values, each as D / 64 parts.
-    // (4 bits: 96 KB; the codes of a tile's keys and values lie in one of three stages before it.  With half of those and 128 KB a
-    // copy's latency showed: 256 chunks of 17, 375 us, so 343.)
-    static constexpr int kStages = FOUR ? (D == 128 ? 3 : 7) : D == 128 ? 5 : 10;
+    // (4 bits: 96 or 128 KB; the codes of a tile's keys and values lie in one of three stages before it.  With half of those
+    // a copy's latency showed: 256 chunks of 17, 375 us, so 343.)
+    static constexpr int kStages = FOUR ? (D == 128 ? 5 : 10) - kQueryTiles : D == 128 ? 5 : 10;
     static constexpr int kCodeStages = FOUR ? (D == 128 ? 3 : 6) : 0, kCodeBytes = 8 * page_bytes(D);
-    static constexpr int kSmem = (2 + kStages) * kTileBytes + kCodeStages * kCodeBytes;  // 219 or 224 KB; 3 KB are left for all else
+    static constexpr int kSmem = (kQueryTiles + kStages) * kTileBytes + kCodeStages * kCodeBytes;  // 214 or 224 KB; 3 KB are left for all else
     static_assert(kSmem >= kAttnMaxB * 12, "the cut's scratch");
 };
 
@@ -108,7 +111,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     attention_tc_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap qmap,
                         const __grid_constant__ CUtensorMap qmap_few, const __grid_constant__ CUtensorMap kmap,
                         const __grid_constant__ CUtensorMap vmap, void *ws) {
-    using Z = Sizes<D, FOUR>;
+    using Z = Sizes<D, FOUR, P>;
     constexpr int S = Z::kStages, kParts = D / 64, kTileBytes = Z::kTileBytes, U = Z::kCodeStages, kAll = FOUR ? kFourbitThreads : kThreads;
     constexpr bool kWide = BF16 && !FOUR;  // bfloat16 operands
     // instruction descriptors: D = fp32, A and B of one 16-bit type, M = 128; N = 128 keys, B K-major; N = D, B MN-major
@@ -142,7 +145,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             return bar_wait_hot(bar, parity, failed);
     };
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t qbuf = smem_u32(smem_raw), ring = qbuf + 2 * kTileBytes, bar0 = smem_u32(bars);
+    const uint32_t qbuf = smem_u32(smem_raw), ring = qbuf + Z::kQueryTiles * kTileBytes, bar0 = smem_u32(bars);
     auto full_bar = [&](int s) { return bar0 + 8u * s; };         // a stage has landed
     auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };  // a stage has been read
     const uint32_t q_full = bar0 + 8u * (2 * S), q_empty = q_full + 8, drain = q_full + 16;
@@ -152,8 +155,8 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     auto written = [&](int s) { return q_full + 104u + 8u * s; };  // a slot's outputs of an item are out of its stage
     auto p_half = [&](int s) { return q_full + 88u + 8u * s; };   // ... those of the first 64 keys
     const uint32_t merge_full = q_full + 72, merge_done = q_full + 80;  // both slots' references and sums are there, read
-    // 4 bits: the queries' two tiles have their own barriers, for an item with one row tile takes one of them, in turn, and the next
-    // item's are rounded meanwhile; the codes of a tile have landed, been read
+    // 4 bits: the queries' tiles have barriers each (an item with one row tile takes one of two in turn); the codes of a tile have
+    // landed, been read
     auto tile_full = [&](int i) { return q_full + 120u + 8u * i; };
     auto tile_empty = [&](int i) { return q_full + 136u + 8u * i; };
     auto code_full = [&](int i) { return q_full + 152u + 8u * i; };
@@ -257,7 +260,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 if (two(g) && lane == 0) bar_arrive(tile_empty(other));  // (the other slot's: read there)
                 q_used += two(g) ? 0x10001u : 1u << (16 * tile);
                 q_used &= 0xff00ffu;
-                if (!two(g)) q_turn ^= 1;
+                if (!two(g)) q_turn ^= Z::kQueryTiles - 1;
             }
             float m = kNegInf, l = 0.f;
             bool bad = false;
@@ -664,7 +667,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                 used += 1u << (16 * tile);
                 used &= 0xff00ffu;
             }
-            if (!two(g)) turn ^= 1;
+            if (!two(g)) turn ^= Z::kQueryTiles - 1;
             return true;
         };
         while (ok && advance(g)) {
@@ -951,7 +954,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     wait(tile_full(q_tile), q_used >> (16 * q_tile) & 1);
                     if (two(g)) wait(tile_full(1), q_used >> 16 & 1);
                     q_used = (q_used + (two(g) ? 0x10001u : 1u << (16 * q_tile))) & 0xff00ffu;
-                    if (!two(g)) q_turn ^= 1;
+                    if (!two(g)) q_turn ^= Z::kQueryTiles - 1;
                 } else {
                     wait(q_full, q_phase);
                     q_phase ^= 1;
@@ -1165,11 +1168,11 @@ cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &f
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && (dev > 63 || !(prepared.load(std::memory_order_relaxed) >> dev & 1))) {
-        e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16, FOUR, P>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D, FOUR>::kSmem);
+        e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16, FOUR, P>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D, FOUR, P>::kSmem);
         if (e == cudaSuccess && dev <= 63) prepared.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     if (e == cudaSuccess)
-        e = launch_behind(attention_tc_kernel<D, BF16, FOUR, P>, dim3(kMaxBlocks), FOUR ? kFourbitThreads : kThreads, (size_t)Sizes<D, FOUR>::kSmem, stream, a, q, few, k, v, ws);
+        e = launch_behind(attention_tc_kernel<D, BF16, FOUR, P>, dim3(kMaxBlocks), FOUR ? kFourbitThreads : kThreads, (size_t)Sizes<D, FOUR, P>::kSmem, stream, a, q, few, k, v, ws);
     if (e == cudaSuccess)
         e = launch_behind(attention_combine_kernel<D, typename std::conditional<BF16, uint16_t, f16_t>::type, FOUR, P>, dim3(kMaxBlocks, kCombineDims, kCombineRows), kCombineThreads, 0, stream, a, ws);
     return e;
