@@ -31,7 +31,7 @@ pcg_status attention_f32(const char *who, const AttnArgs &a, void *workspace, cu
 // Over the cache that holds 4.5 bits a value (k: its pages): 16-bit types, head dimensions 64 and 128, attention_work_bytes(d) of
 // workspace.  Calls of few rows have a kernel of their own: `few_tile` says how many rows its row tiles are to have, for n tokens
 // a sequence and G query heads a key head, 0 where the other kernel is the faster one.  (n = 4, 5 and 6, 7 and 8 of G = 4 over up
-// to 8000, 64 sequences, 8 key heads x 128: 104, 165, 192 us, and 238 to 240 with the other; x 64: 73, 107, 132, and 171 to 173.
+// to 8000, 64 sequences, 8 key heads x 128: 105, 165, 192 us, and 211 with the other; x 64: 73, 107, 132, and 168.
 // Two tiles of 16 rows are faster than one of 32, whose sums no longer fit a lane's registers at head dimension 128, and three
 // slower than the other kernel.)
 inline int few_tile(int d, int64_t n, int G) {

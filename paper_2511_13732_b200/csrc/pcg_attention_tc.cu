@@ -46,14 +46,14 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
 // tiles.  640 threads are launched with 96 registers each, 480 for the five warps of each quarter of an SM, whose registers are its
 // own: the softmax's two take 144, which the other three leave by keeping 64 (2 * 144 + 3 * 64 = 480).  Two of the 20 warps have
 // no part; without them, 18 would be launched with 96 as well and have less to share.
-// Measured: 2 chunks of 2048 over 16,000, 32 / 8 heads x 128, 1128 us = 1013 TFLOP/s (62 % of the measured burst); 256 chunks of
-// 17 over up to 2000, 326 us, where HBM would allow 62.  What bounds those: an item's ends (some 10,000 cycles, 14 items a block)
-// and the hand-overs of a key tile between five roles (2,900 cycles with neither codes widened nor a softmax computed, 3,800 with).
+// Measured: 2 chunks of 2048 over 16,000, 32 / 8 heads x 128, 1077 us = 1061 TFLOP/s (65 % of the measured burst); 256 chunks of
+// 17 over up to 2000, 278 us, where HBM would allow 62.  What bounds those: an item's ends (14 items a block) and the hand-overs of
+// a key tile from copy to widening, products, softmax and products, some 3,500 cycles a tile.
 constexpr int kWidenWarps = 8, kFourbitThreads = 32 * (kSoftmaxWarps + kWidenWarps + 4);
 // What an item costs there (256 chunks of 17: 306 us with four units, 288 with six, 292 with eight; 32 of 64 over 500: 76, 69, 67 with nine).
 constexpr int kFourbitItemUnits = 6;
-#define PCG_SOFTMAX_REGISTERS "144"
-#define PCG_OTHER_REGISTERS "64"
+constexpr int kLaunchRegisters = 96, kSoftmaxRegisters = 144, kOtherRegisters = 64;
+static_assert(2 * kSoftmaxRegisters + 3 * kOtherRegisters <= 5 * kLaunchRegisters, "the wait for more than there are would not end");
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
 
 // 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs.  All by the special-function unit: with
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
     auto last_key = [&](const Segment &g) { return two(g) ? g.len : min(g.len, (g.t0 + g.nt) * kHalf); };
     if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax: thread = row of the slot's row tile
-        if (FOUR) asm volatile("setmaxnreg.inc.sync.aligned.u32 " PCG_SOFTMAX_REGISTERS ";");
+        if (FOUR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegisters));
         uint32_t q_used = 0, q_turn = 0;  // (4 bits) uses of the queries' tiles so far (16 bits each), the next to take
         const int slot = warp >> 2, row = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         }
     } else if (FOUR && warp < kSoftmaxWarps + kWidenWarps) {
         // ------------------------------------------------------------------ (4 bits) codes to tiles, by all eight warps each
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
         const int w = tid - 32 * kSoftmaxWarps;
         uint32_t stage = 0, stage_phase = 1, unit = 0, unit_phase = 0;
         bool ok = true;
@@ -706,10 +706,10 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             }
         }
     } else if (FOUR && warp >= kSoftmaxWarps + kWidenWarps + 2) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
     } else if (FOUR && warp == kSoftmaxWarps + kWidenWarps) {
         // ------------------------------------------------------------------ (4 bits) copies of a tile's pages: a lane per copy looks its block up
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
         const int size = min(1 << a.bs_shift, 64);  // tokens of one copy
         constexpr int kPage = page_bytes(D);
         uint32_t it = 0, unit = 0, phase = 1;
@@ -895,7 +895,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         // Head dimension 128: one lane, elected once, waits and issues, which costs the fewest instructions between two
         // products (a prompt of 8192: 525 us with the warp waiting and a lane elected for each issue, 512 so).  64: the warp
         // waits (16 prompts of up to 1500: 101 us with one lane, 95 so: its code is the smaller).
-        if (FOUR) asm volatile("setmaxnreg.dec.sync.aligned.u32 " PCG_OTHER_REGISTERS ";");
+        if (FOUR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
         constexpr bool kOneLane = D == 128 && (!FOUR || P == 1);
         auto issuing = [&]() { return kOneLane || elect_one(); };
         auto together = [&]() {
@@ -1169,6 +1169,11 @@ cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &f
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess && (dev > 63 || !(prepared.load(std::memory_order_relaxed) >> dev & 1))) {
         e = cudaFuncSetAttribute(attention_tc_kernel<D, BF16, FOUR, P>, cudaFuncAttributeMaxDynamicSharedMemorySize, Sizes<D, FOUR, P>::kSmem);
+        if (FOUR && e == cudaSuccess) {  // registers are shared out as if launched with so many
+            cudaFuncAttributes f;
+            e = cudaFuncGetAttributes(&f, attention_tc_kernel<D, BF16, FOUR, P>);
+            if (e == cudaSuccess && f.numRegs < kLaunchRegisters) e = cudaErrorInvalidConfiguration;
+        }
         if (e == cudaSuccess && dev <= 63) prepared.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
     if (e == cudaSuccess)
@@ -1180,6 +1185,8 @@ cudaError_t launch(const AttnArgs &a, const CUtensorMap &q, const CUtensorMap &f
 
 }  // namespace
 
+// `rows` of a sequence and key head on average.  Up to one row tile the kernel for such items alone is the faster one, whose code
+// fits the instruction caches better (64 chunks of 32 over 4000, 32 / 8 heads x 128: 227 us, and 240 with the other; of 34: 400, 299).
 template <int D, bool BF16>
 static cudaError_t launch_fourbit(const AttnArgs &a, int64_t rows, void *ws, cudaStream_t stream) {
     const CUtensorMap none = {};  // (a page is copied as it lies)
