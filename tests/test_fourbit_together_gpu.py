@@ -34,6 +34,16 @@ def test_around_a_tile_of_few_rows(G, n, d):
     _check(s, _run(s))
 
 
+@pytest.mark.parametrize("G,n", [(128, 1), (100, 1), (64, 2), (33, 3), (5, 24), (1, 128), (1, 100), (3, 86), (128, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_around_one_row_tile(G, n, d):
+    """Items of one row tile, long ones cut between blocks, and the first that have two."""
+    s = _build([3000, 77 + n, 640, n], [n] * 4, G, 1, d, 32, torch.bfloat16, seed=G)
+    _check(s, _run(s))
+    s = _build([300, 77 + n, 1, 2500], [n, 0, 1, 2 * n - 1], 2 * G, 2, d, 16, torch.float16, ks=2.0, vs=0.5, seed=n)
+    _check(s, _run(s))
+
+
 @pytest.mark.parametrize("G", [25, 33, 49, 100, 127, 128])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
