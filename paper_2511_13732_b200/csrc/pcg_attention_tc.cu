@@ -47,7 +47,7 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + 2);
 // own: the softmax's two take 144, which the other three leave by keeping 64 (2 * 144 + 3 * 64 = 480).  Two of the 20 warps have
 // no part; without them, 18 would be launched with 96 as well and have less to share.
 // Measured: 2 chunks of 2048 over 16,000, 32 / 8 heads x 128, 1077 us = 1061 TFLOP/s (65 % of the measured burst); 256 chunks of
-// 17 over up to 2000, 278 us, where HBM would allow 62.  What bounds those: an item's ends (14 items a block) and the hand-overs of
+// 17 over up to 2000, 270 us, where HBM would allow 62.  What bounds those: an item's ends (14 items a block) and the hand-overs of
 // a key tile from copy to widening, products, softmax and products, some 3,500 cycles a tile.
 constexpr int kWidenWarps = 8, kFourbitThreads = 32 * (kSoftmaxWarps + kWidenWarps + 4);
 // What an item costs there (256 chunks of 17: 306 us with four units, 288 with six, 292 with eight; 32 of 64 over 500: 76, 69, 67 with nine).
@@ -627,7 +627,8 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
         // An item's queries, rounded to float16.  (Two warps of their own, an item ahead, were too slow for two row tiles, which
         // cannot be fetched ahead, by some 20 us an item, and for short contexts; for others this costs the same.)
         auto queries = [&](const Segment &g) {
-            constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes, kAhead = 4;  // 16 bytes a lane, loads in flight
+            constexpr int kLanes = D / 8, kRowsAtOnce = 32 / kLanes;  // 16 bytes a lane
+            constexpr int kAhead = 2;  // loads in flight (256 chunks of 17: 270 us, with one 286, with four, which spread fewer rows over the warps, 278)
             const int sub = lane / kLanes, chunk = lane % kLanes;
             const uint32_t one_of = (65536 + G - 1) / G;  // r / G is r * one_of >> 16, for r < 128
             const int tokens = min(g.n - g.pair * P * TQ, P * TQ);
