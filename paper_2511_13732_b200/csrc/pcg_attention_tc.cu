@@ -253,11 +253,14 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
             if constexpr (FOUR) {
                 const uint32_t tile = two(g) ? slot : q_turn, other = tile ^ 1;
                 ok = __all_sync(0xffffffffu, wait_on(tile_full(tile), q_used >> (16 * tile) & 1, failed));
+                // The other slot's tile is read there, but its turn has to have begun before this warp says that it is through with
+                // it: while the other slot is behind, in an item without a key tile for it, the arrival would count for that one.
+                if (two(g)) ok = ok && __all_sync(0xffffffffu, wait_on(tile_full(other), q_used >> (16 * other) & 1, failed));
                 if (!ok) break;
                 by_score = valid ? q_by[tile][row] : 0.f;
                 __syncwarp();
                 if (lane == 0) bar_arrive(tile_empty(tile));
-                if (two(g) && lane == 0) bar_arrive(tile_empty(other));  // (the other slot's: read there)
+                if (two(g) && lane == 0) bar_arrive(tile_empty(other));
                 q_used += two(g) ? 0x10001u : 1u << (16 * tile);
                 q_used &= 0xff00ffu;
                 if (!two(g)) q_turn ^= Z::kQueryTiles - 1;
