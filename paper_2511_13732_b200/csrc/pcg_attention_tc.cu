@@ -751,6 +751,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
                     if (now == -2)
                         for (uint32_t i = 0; i < bytes; i += 16) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + lane * step + i), "r"(0u) : "memory");
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();  // (the arrival below is one lane's, and lets all lanes' zeros be read)
                 }
                 if (elect_one()) bar_expect(bar, total);
                 __syncwarp();

@@ -47,3 +47,25 @@ def test_the_same_with_contexts_of_several_key_tiles(d):
     _check(_some(s, 4), want)
     for _ in range(20):
         assert torch.equal(_run(s), want)
+
+
+@pytest.mark.parametrize("n", [2, 17, 40])
+@pytest.mark.parametrize("d", [64, 128])
+def test_key_tiles_that_are_zeros_between_others(d, n):
+    """Tiles of which no block is in the pool (nothing is copied for them, so they are complete as soon as their zeros are written)
+    and tiles of which some are, in the stages where other tiles' codes have been; values far from zero."""
+    bs, B = 16, 24
+    lens = [n + 90 * b % 1500 + 200 for b in range(B)]
+    s = _build(lens, [n] * B, 8, 2, d, bs, torch.bfloat16, vs=50.0, seed=n)
+    zero = torch.zeros(1, *s["cache"].shape[1:], dtype=torch.uint8, device="cuda")
+    at = torch.cat([s["cache"], zero]), s["cache"].shape[0]
+    for b in range(B):
+        used = (lens[b] + bs - 1) // bs
+        for j in range(used):
+            if j // 8 % 3 == 1 or j % 5 == b % 5:  # every third tile of 128 keys, and some blocks of the others
+                s["table"][b, j] = (-1, at[1], 2 ** 31 - 1)[j % 3]
+                s["slots"][b][j * bs:(j + 1) * bs] = at[1] * bs + torch.arange(bs, device="cuda")[:lens[b] - j * bs]
+    want = _run(s)
+    _check(dict(s, cache=at[0]), want)
+    for _ in range(20):
+        assert torch.equal(_run(s), want)
