@@ -3,13 +3,14 @@
 #include <cuda_bf16.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "pcg_attention.cuh"
 #include "pcg_fourbit.cuh"
 
 namespace pcg {
 
-// ---------------------------------------------------------------------------------------------- any type and head size
+// ---------------------------------------------------------------------------------------------- float32, other head sizes
 // One block per (row, query head): its eight warps take keys 32 at a time (two pages) in turn, a lane scores one key, and
 // the warp sums the 32 weighted values with lane = head dimension, whose codes of a page are 8 bytes.  The warps'
 // running sums meet in shared memory at the end.
@@ -151,11 +152,12 @@ __global__ void __launch_bounds__(kSimpleThreads) attention_fourbit_simple_kerne
 template <typename T>
 void launch_fourbit_simple(const AttnArgs &a, cudaStream_t s) {
     const dim3 grid(a.rows, a.q_heads);
+    constexpr bool kAll = std::is_same<T, float>::value;  // 16-bit types have other kernels for 64 and 128 dimensions
     switch (a.d / 32) {
         case 1: attention_fourbit_simple_kernel<T, 1><<<grid, kSimpleThreads, 0, s>>>(a); break;
-        case 2: attention_fourbit_simple_kernel<T, 2><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 2: if constexpr (kAll) attention_fourbit_simple_kernel<T, 2><<<grid, kSimpleThreads, 0, s>>>(a); break;
         case 3: attention_fourbit_simple_kernel<T, 3><<<grid, kSimpleThreads, 0, s>>>(a); break;
-        case 4: attention_fourbit_simple_kernel<T, 4><<<grid, kSimpleThreads, 0, s>>>(a); break;
+        case 4: if constexpr (kAll) attention_fourbit_simple_kernel<T, 4><<<grid, kSimpleThreads, 0, s>>>(a); break;
         case 5: attention_fourbit_simple_kernel<T, 5><<<grid, kSimpleThreads, 0, s>>>(a); break;
         case 6: attention_fourbit_simple_kernel<T, 6><<<grid, kSimpleThreads, 0, s>>>(a); break;
         case 7: attention_fourbit_simple_kernel<T, 7><<<grid, kSimpleThreads, 0, s>>>(a); break;
