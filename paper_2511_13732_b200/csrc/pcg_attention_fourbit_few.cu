@@ -67,10 +67,6 @@ constexpr size_t few_bytes() {
     return (sizeof(FewHead<Few<D, NT>::kRuns>) + 255) / 256 * 256 + (size_t)Few<D, NT>::kRuns * 2 * Few<D, NT>::kRows * (D + 2) * 4;
 }
 
-__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
-    const __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
 // c[16][8] += a[16][16] b[16][8]
 __device__ __forceinline__ void product(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -186,8 +182,7 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
     while (ok && walk.next<1>(a, TQ, g)) {
         const int tokens = min(g.n - g.pair * TQ, TQ), rows = tokens * G, k_end = last_key(g);
         const int seen0 = g.len - g.n + g.pair * TQ + 1;  // keys that the first token sees
-        // ---- queries: row 8 j + g, the lane's dimensions; bfloat16 is multiplied by the power of two, a row's own, that brings
-        // its largest finite value to 2^14 or above: float16 then holds it exactly down to 2^-28 of that, and to 2^-39 of it below
+        // ---- queries: row 8 j + g, the lane's dimensions
         uint32_t q[NT][QR];
         float by_q[NT][2], ref[NT][2];  // of rows 2 i and 2 i + 1: what products are multiplied by, references (0 until there is one)
         int lim[NT][2];
@@ -199,35 +194,13 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
             uint4 w[D / 32];
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) w[c] = r < rows ? reinterpret_cast<const uint4 *>(src)[c] : make_uint4(0u, 0u, 0u, 0u);
-            if constexpr (std::is_same<T, uint16_t>::value) {
-                float most = 0.f;
+            if constexpr (std::is_same<T, uint16_t>::value) by *= narrow_row<4>(w);
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    float x[8];
-                    Elem<uint16_t>::unpack(w[c], x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(x[e]) < __int_as_float(0x7f800000) ? fabsf(x[e]) : 0.f);
-                }
-                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-                const int up = max(-113, min(120, 14 + 127 - (int)(__float_as_uint(most) >> 23)));
-                const float by_row = __uint_as_float((uint32_t)(127 + up) << 23);
-                by *= __uint_as_float((uint32_t)(127 - up) << 23);
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    float x[8];
-                    Elem<uint16_t>::unpack(w[c], x);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) q[j][c * 4 + e] = pack2<false>(x[2 * e] * by_row, x[2 * e + 1] * by_row);
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    q[j][c * 4] = w[c].x;
-                    q[j][c * 4 + 1] = w[c].y;
-                    q[j][c * 4 + 2] = w[c].z;
-                    q[j][c * 4 + 3] = w[c].w;
-                }
+            for (int c = 0; c < D / 32; ++c) {
+                q[j][c * 4] = w[c].x;
+                q[j][c * 4 + 1] = w[c].y;
+                q[j][c * 4 + 2] = w[c].z;
+                q[j][c * 4 + 3] = w[c].w;
             }
             by = fminf(fmaxf(by, 1.17549435e-38f), 3.40282347e38f);  // (never 0: 0 times a masked score would be NaN)
 #pragma unroll
@@ -295,8 +268,8 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
                         const int half = D == 128 ? x >> 1 : 0;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            v0[e] = mul2(v0[e], by[0][half]);
-                            v1[e] = mul2(v1[e], by[1][half]);
+                            v0[e] = mul_f16x2(v0[e], by[0][half]);
+                            v1[e] = mul_f16x2(v1[e], by[1][half]);
                         }
 #pragma unroll
                         for (int e = 0; e < 4; e += 2)
@@ -391,8 +364,8 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
                         widen_codes(c1[y], v1);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            v0[e] = mul2(v0[e], by[e]);
-                            v1[e] = mul2(v1[e], by[e]);
+                            v0[e] = mul_f16x2(v0[e], by[e]);
+                            v1[e] = mul_f16x2(v1[e], by[e]);
                         }
 #pragma unroll
                         for (int e = 0; e < 4; e += 2)

@@ -82,11 +82,6 @@ __device__ __forceinline__ void store_row(void *p, const uint32_t (&w)[8], bool 
     }
 }
 
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-    const __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-
 // ---------------------------------------------------------------------------------------------- main kernel
 template <int D, bool FOUR, int P>
 struct Sizes {
@@ -655,7 +650,7 @@ __global__ void __launch_bounds__(FOUR ? kFourbitThreads : kThreads, 1)
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i) {
                         const int r = r0 + i * kRowsAtOnce + sub;
-                        const float by = BF16 ? narrow_row<kLanes>(v[i]) * a.scale_log2 : a.scale_log2;
+                        const float by = BF16 ? narrow_row<kLanes>(reinterpret_cast<uint4(&)[1]>(v[i])) * a.scale_log2 : a.scale_log2;
                         if (r < rows) {
                             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + r * 128 + ((chunk & 7) ^ (r & 7)) * 16), "r"(v[i].x),
                                          "r"(v[i].y), "r"(v[i].z), "r"(v[i].w)

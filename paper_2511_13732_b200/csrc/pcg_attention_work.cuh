@@ -267,20 +267,29 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return r;
 }
 
-// A row of bfloat16 queries, 8 a lane, LANES neighbouring lanes: rounded to float16 after a multiplication by the power of two that
+// A row of bfloat16 queries, 8 N a lane, LANES neighbouring lanes: rounded to float16 after a multiplication by the power of two that
 // brings the row's largest finite value to 2^14 or above, so that float16 holds it exactly down to 2^-28 of that, and to 2^-39 of it
 // below.  Returns what takes the power of two back.
-template <int LANES>
-__device__ __forceinline__ float narrow_row(uint4 &w) {
-    float x[8], most = 0.f;
-    Elem<uint16_t>::unpack(w, x);
+template <int LANES, int N>
+__device__ __forceinline__ float narrow_row(uint4 (&w)[N]) {
+    float most = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]) < __int_as_float(0x7f800000) ? fabsf(x[j]) : 0.f);
+    for (int i = 0; i < N; ++i) {
+        float x[8];
+        Elem<uint16_t>::unpack(w[i], x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(x[j]) < __int_as_float(0x7f800000) ? fabsf(x[j]) : 0.f);
+    }
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     const int up = max(-113, min(120, 14 + 127 - (int)(__float_as_uint(most) >> 23)));
     const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-    w = make_uint4(pack2<false>(x[0] * f, x[1] * f), pack2<false>(x[2] * f, x[3] * f), pack2<false>(x[4] * f, x[5] * f), pack2<false>(x[6] * f, x[7] * f));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float x[8];
+        Elem<uint16_t>::unpack(w[i], x);
+        w[i] = make_uint4(pack2<false>(x[0] * f, x[1] * f), pack2<false>(x[2] * f, x[3] * f), pack2<false>(x[4] * f, x[5] * f), pack2<false>(x[6] * f, x[7] * f));
+    }
     return __uint_as_float((uint32_t)(127 - up) << 23);
 }
 

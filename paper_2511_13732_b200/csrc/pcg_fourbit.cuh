@@ -33,6 +33,11 @@ __device__ __forceinline__ float widen_scale(uint32_t byte) {
     widen_scales(byte, r);
     return __low2float(*reinterpret_cast<__half2 *>(&r[0]));
 }
+// Two float16 products.
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
 __device__ __forceinline__ float2 both_halves(uint32_t h2) { return __half22float2(*reinterpret_cast<__half2 *>(&h2)); }
 
 #endif  // __CUDACC__
