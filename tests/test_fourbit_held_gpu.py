@@ -113,3 +113,35 @@ def test_a_held_nan_value_stays_in_its_sequence_and_its_dimensions(n, d, dtype):
     assert torch.equal(out[~touched], want[~touched])
     early = out[:seen, 4:, 16:32]
     assert bool((early.isnan() | (early == want[:seen, 4:, 16:32])).all())
+
+
+def test_two_rows_with_one_slot_leave_the_others_alone():
+    """A slot that several rows name holds a mixture of them; every other byte is what it is without them."""
+    from paper_2511_13732_b200 import binding
+
+    gen = torch.Generator().manual_seed(6)
+    rows, kvh, d, bs = 90, 2, 64, 32
+    k, v = (torch.randn(rows, kvh, d, generator=gen).cuda() for _ in range(2))
+    slots = torch.arange(7, rows + 7, dtype=torch.int32)
+    slots[50], slots[60], slots[61], slots[3] = 20, 20, 33, 33  # beside the rows 13 and 26, whose slots these are
+    twice = (20, 33)
+    start = torch.randint(0, 256, binding.pcg_fourbit_cache_shape(4, kvh, bs, d), generator=gen, dtype=torch.uint8).cuda()
+    mine, alone = start.clone(), start.clone()
+    binding.pcg_cache_append_fourbit(None, k, v, slots.cuda(), mine)
+    only = slots.clone()
+    only[[3, 13, 26, 50, 60, 61]] = -1
+    binding.pcg_cache_append_fourbit(None, k, v, only.cuda(), alone)
+    code, s8 = zip(*(R.quantise32(x.cpu(), 1.0) for x in (k, v)))
+    for s in range(4 * bs):
+        for h in range(kvh):
+            for values in (False, True):
+                page, t = [c[s // bs, h, s % bs // 16].cpu() for c in (mine, alone)], s % 16
+                dims = torch.arange(d)
+                at, up = (9 * d + dims * 8 + t // 2, t % 2 * 4 + 0 * dims) if values else (dims // 32 * 256 + t * 16 + dims % 32 // 2, dims % 2 * 4)
+                got, want = ((p[at] >> up) & 15 for p in page)
+                if s not in twice:
+                    assert torch.equal(got, want), (s, h, values)
+                elif not values:  # words of 16 codes are one row's or another's (value codes may mix within a code)
+                    names = [r for r in range(rows) if int(slots[r]) == s]
+                    for j in range(0, d, 16):
+                        assert any(torch.equal(got[j:j + 16], code[0][r, h, j:j + 16]) for r in names), (s, h, j)
