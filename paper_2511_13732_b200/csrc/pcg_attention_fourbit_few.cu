@@ -4,9 +4,10 @@
 // Each warp works alone, on 64 keys at a time, with warp-level products whose operands are widened codes straight in registers:
 //     S^T[key][row] = K[key][dim] Q^T[dim][row],   O^T[dim][row] += V^T[dim][key] P^T[key][row]
 // with 16 keys, or 16 value dimensions, to 8 rows a product.  What bounds a call is then reading the cache and widening it, and
-// no warp waits for another.  (64 single tokens of 32 query heads over up to 32,000, 128 dimensions: 247 us, 82 % of the
+// no warp waits for another.  (64 single tokens of 32 query heads over up to 32,000, 128 dimensions: 246 us, 82 % of the
 // measured copy's rate; with keys on the lanes of tensor memory and 16 columns for the four rows, where five roles hand over to
-// one another for every 128 keys, 440 us.  The other path's tiles have 128 rows: beyond 32 it is the faster one.)
+// one another for every 128 keys, 440 us.  The other path's tiles have 128 rows.  At 128 dimensions it is the faster one beyond 32;
+// at 64, 32 rows are what a lane's registers hold here, and the faster there still.)
 //
 // What a lane holds of an operand is free where both sides agree, so lanes take what lies together in a page.  With g = lane / 4,
 // i = lane % 4, and a chunk of four pages of 16 keys:
@@ -319,6 +320,10 @@ __global__ void __launch_bounds__(32 * Few<D, NT>::kWarps, 1)
                             }
                         }
                 }
+                // Weights are rounded to float16, the type of the other operand: the products take two of one 16-bit type, and of
+                // those it has the most bits.  That is off by 2^-12 of a weight at most, which an output in float16 shows (2.8e-4
+                // in 2-norm where its own rounding gives 2.1e-4) and one in bfloat16 does not (1.7e-3 either way).  Their sum is
+                // float32, of the weights before the rounding.
                 uint32_t p[2 * M][NT];  // of block 2 M h + b: (row g, tokens 2 b and 2 b + 1 behind 4 M h of page i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {

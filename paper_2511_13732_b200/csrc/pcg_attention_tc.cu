@@ -56,7 +56,8 @@ constexpr int kLaunchRegisters = 96, kSoftmaxRegisters = 144, kOtherRegisters = 
 static_assert(2 * kSoftmaxRegisters + 3 * kOtherRegisters <= 5 * kLaunchRegisters, "the wait for more than there are would not end");
 constexpr float kSlack = 8.f;    // the reference may lag the maximum by a factor 2^8 before sums are scaled
 
-// 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs.  All by the special-function unit: with
+// 32 weights 2^(score * scale + shift), packed to 16 bits; their sums, in pairs, in float32 and of the weights before the rounding.
+// (16 bits are what the product with the values takes, of the values' type: float16 over 4 bits, whatever the queries are.)  All by the special-function unit: with
 // 6, 10, 13 or 16 of 32 computed by a polynomial on the FMA pipes a prompt of 8192 tokens took 2 to 9 % longer, since a
 // tile's time is the latency of its steps rather than the unit's rate.
 template <bool BF16>

@@ -38,7 +38,8 @@ class DecodeRounds:
     holds ``max_blocks`` at most.
 
     ``rotary``: a table [positions, dim] float32 of the cosines, then the sines, of each position's angles; queries and keys
-    are then turned by the angles of their tokens' positions (pairs of adjacent dimensions where ``interleaved``).
+    are then turned by the angles of their tokens' positions (pairs of adjacent dimensions where ``interleaved``); at a position
+    that the table does not have they become NaN.
     ``fourbit``: the cache holds 4.5 bits a value, with ``k_scale`` and ``v_scale`` as ``pcg_cache_append_fourbit`` says;
     ``dtype`` is then not used, q, k and v may be of any type."""
 
